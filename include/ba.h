@@ -381,6 +381,105 @@ size_t ba_block_attention_prompts_backward_workspace_bytes(const ba_heads *heads
                                                            const int32_t *block_offsets);
 
 /*
+ * Norms of queries and keys for each head, with the rotation of Eq. 1 in the same pass, for models that norm
+ * them ahead of attention.  A head vector x of token t becomes
+ *   y = R(positions[t]) (w o x / sqrt(mean(x^2) + eps)),   the mean over its head_dim elements,
+ * in 32 bits, rounded once.  q [T, n_q_heads, D] with gains w = norm->q_weight into q_out, k [T, n_kv_heads, D] with
+ * norm->k_weight into k_out; q and q_out, or k and k_out, may be null.  bf16 or fp32 (one type for all of them).
+ * An output may be exactly its input (in place); any other overlap is an error.
+ * rope_mode BA_ROPE_NONE norms only: in front of the entry points that rotate by themselves, and of
+ * ba_block_attention_prompts with its backward.  With BA_ROPE_APPLY the rows are ready for BA_ROPE_NONE there.
+ * positions: DEVICE, n_tokens ints, null -> a token's number.
+ */
+typedef struct ba_head_norm {
+  const void *q_weight; /* device, [head_dim], nullable -> ones */
+  const void *k_weight; /* device, [head_dim], nullable -> ones */
+  int32_t dtype;        /* BA_DTYPE_* of the gains               */
+  float eps;            /* > 0                                   */
+} ba_head_norm;
+int32_t ba_norm_rotate(const ba_heads *heads, const ba_head_norm *norm, const ba_tensor *q,
+                       const ba_tensor *k, const ba_tensor *q_out, const ba_tensor *k_out,
+                       int32_t n_tokens, const int32_t *positions, int32_t rope_mode, void *stream);
+
+/*
+ * Backward pass of ba_norm_rotate.  With n = x / sqrt(mean(x^2) + eps) and g = R(positions[t])^T dy:
+ *   dw = sum over tokens and heads of g o n,   dx = (w o g - n mean(w o g o n)) / sqrt(mean(x^2) + eps).
+ * q, k: the inputs of the forward call; d_q_out, d_k_out: the gradients of its outputs; dq, dk like q and k, which
+ * may be exactly d_q_out or q (d_k_out or k).  dq_weight, dk_weight: device, [head_dim] floats, nullable; zeros
+ * without tokens.  Deterministic: every sum is added up in a fixed order.
+ * ws: 256-byte aligned, at least ba_norm_rotate_backward_workspace_bytes() bytes (1 MB at most).
+ */
+int32_t ba_norm_rotate_backward(const ba_heads *heads, const ba_head_norm *norm, const ba_tensor *q,
+                                const ba_tensor *k, const ba_tensor *d_q_out,
+                                const ba_tensor *d_k_out, const ba_tensor *dq, const ba_tensor *dk,
+                                float *dq_weight, float *dk_weight, int32_t n_tokens,
+                                const int32_t *positions, int32_t rope_mode, void *ws,
+                                size_t ws_bytes, void *stream);
+size_t ba_norm_rotate_backward_workspace_bytes(const ba_heads *heads, int32_t n_tokens);
+
+/*
+ * A cache of keys and values in pages, for answering after the final block (Section 2.5): a sequence's token i lies in
+ * row i % page_rows of page page_table[sequence][i / page_rows].  Several sequences may name the same page: the
+ * passages that their prompts have in common.
+ * Unlike the host arrays of the other entry points the page table, and the lengths and positions of the calls below,
+ * are DEVICE memory: they change with every token, and a captured graph reads the new ones.  The kernels check what they
+ * read there: a page number outside 0 .. n_pages - 1 is a page that is not there.
+ */
+typedef struct ba_paged_cache {
+  ba_tensor k, v;            /* page 0, row 0, head 0; stride_tok: from row to row of a page; bf16 */
+  int64_t k_stride_page;     /* elements from page to page                                          */
+  int64_t v_stride_page;
+  int32_t n_pages;
+  int32_t page_rows;         /* tokens of a page, any number                                        */
+  const int32_t *page_table; /* device, [n_seqs][stride_table], the first max_pages of a row count   */
+  int64_t stride_table;
+  int32_t n_seqs;
+  int32_t max_pages;
+} ba_paged_cache;
+
+/*
+ * Keys and values of new tokens into their pages, normed and rotated on the way (Section 2.3: the cached key is the
+ * rotated one); with q also the tokens' queries, as ba_paged_attention wants them, into q_out.
+ * Token t belongs to sequence seq_of_token[t] (null -> t) and becomes its token cache_pos[t]; q and k are rotated at
+ * rope_pos[t] (null -> cache_pos[t]), v is copied.  norm null: no norm.  rope_mode BA_ROPE_NONE: no rotation.
+ * Keys of cached passages, which carry the rotation of their local positions, are re-encoded on the way by
+ * rope_pos[t] = the shift of the token's passage, without norm.
+ * A token whose sequence, position or page is not there (a negative position, say) is not kept; its query is written all
+ * the same.  No two tokens of a call may go to the same row.  Nothing else of the cache changes.
+ * q, k, v, q_out: bf16, q_out may be exactly q.  cache_pos, seq_of_token, rope_pos: device, n_tokens ints.
+ */
+int32_t ba_paged_append(const ba_heads *heads, const ba_head_norm *norm, const ba_paged_cache *cache,
+                        const ba_tensor *q, const ba_tensor *k, const ba_tensor *v,
+                        const ba_tensor *q_out, int32_t n_tokens, const int32_t *cache_pos,
+                        const int32_t *seq_of_token, const int32_t *rope_pos, int32_t rope_mode,
+                        void *stream);
+
+/*
+ * Attention of the newest tokens of every sequence over its pages: an answer's next token, or a few drafted ones.
+ * Sequence s has seq_len[s] tokens in the cache (device; taken as at most max_len, which is the host's bound), the last
+ * q_per_seq of them are rows [s * q_per_seq, (s + 1) * q_per_seq) of q and o_out ([n_seqs * q_per_seq, n_q_heads, D], bf16,
+ * rotated).  Token i of them is the sequence's token p = seq_len[s] - q_per_seq + i and sees tokens 0 .. p:
+ *   o[i, h] = sum_{t <= p} softmax_t(scale * <q[i, h], k_t>) v_t.
+ * A row that sees nothing (p < 0, or no page is there) is zero.  Tokens that a row does not see, and rows of a page that
+ * no token has, have no part in it, whatever bits they hold.  lse_out: device, nullable, [n_seqs * q_per_seq][n_q_heads]
+ * floats, the natural log of the sum of exp(scale * <q, k>); -infinity for such a row.
+ *
+ * Groups: host arrays, cu_group [n_groups + 1] (cu_group[0] = 0, cu_group[n_groups] = n_seqs) and prefix_len [n_groups]
+ * (at most max_len).  The first prefix_len[g] tokens of sequences cu_group[g] .. cu_group[g + 1] - 1 are the same, and are
+ * read, for all of the group's rows at once, from the pages of its first sequence.  n_groups 0 (arrays null): nothing is shared.
+ * ws: 256-byte aligned, at least ba_paged_attention_workspace_bytes() bytes for the same arguments (may be null when that is
+ * 0).  Two calls with the same arguments give the same bits; in another batch the last bits may differ.
+ */
+int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, const ba_tensor *q,
+                           const ba_tensor *o_out, float *lse_out, int32_t q_per_seq,
+                           const int32_t *seq_len, int32_t max_len, int32_t n_groups,
+                           const int32_t *cu_group, const int32_t *prefix_len, void *ws,
+                           size_t ws_bytes, void *stream);
+size_t ba_paged_attention_workspace_bytes(const ba_heads *heads, int32_t n_seqs, int32_t q_per_seq,
+                                          int32_t max_len, int32_t n_groups,
+                                          const int32_t *cu_group, const int32_t *prefix_len);
+
+/*
  * The schedule of a call, for inspection and tests: the work items the host planner hands to the
  * kernels, computed by the code the calls themselves use.  Host only: no device is touched, so
  * these run on a machine without a GPU.

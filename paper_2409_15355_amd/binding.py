@@ -32,6 +32,8 @@ EXPORTS = ["ba_version", "ba_status_string", "ba_last_error", "ba_profile_begin"
            "ba_final_block_attention_cached", "ba_final_block_attention_cached_workspace_bytes",
            "ba_block_attention_prompts", "ba_block_attention_prompts_workspace_bytes",
            "ba_block_attention_prompts_backward", "ba_block_attention_prompts_backward_workspace_bytes",
+           "ba_norm_rotate", "ba_norm_rotate_backward", "ba_norm_rotate_backward_workspace_bytes",
+           "ba_paged_append", "ba_paged_attention", "ba_paged_attention_workspace_bytes",
            "ba_schedule_final_block", "ba_schedule_encode_blocks", "ba_schedule_prompts",
            "ba_measure_xcd_speed", "ba_measure_xcd_speed_workspace_bytes", "ba_diag_final_block_phases",
            "ba_diag_mfma_ceiling", "ba_diag_mfma_ceiling_workspace_bytes"]
@@ -54,6 +56,16 @@ class BaWorkItem(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("launch", "problem", "first_token", "tile_rows", "tile_keys", "row_begin",
                                                "row_end", "split", "n_splits", "ctx_begin", "ctx_end", "self_begin",
                                                "self_end", "kv_head", "xcd")]
+
+
+class BaHeadNorm(ctypes.Structure):
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class BaPagedCache(ctypes.Structure):
+    _fields_ = [("k", BaTensor), ("v", BaTensor), ("k_stride_page", ctypes.c_int64), ("v_stride_page", ctypes.c_int64),
+                ("n_pages", ctypes.c_int32), ("page_rows", ctypes.c_int32), ("page_table", ctypes.c_void_p),
+                ("stride_table", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
 
 
 class BaError(RuntimeError):
@@ -127,6 +139,21 @@ def load():
     lib.ba_block_attention_prompts_workspace_bytes.restype = ctypes.c_size_t
     lib.ba_block_attention_prompts_workspace_bytes.argtypes = [_HP, ctypes.c_int32, _I32P, _I32P, ctypes.c_int32,
                                                                ctypes.c_int32]
+    _NP, _CP, _VP = ctypes.POINTER(BaHeadNorm), ctypes.POINTER(BaPagedCache), ctypes.c_void_p
+    lib.ba_norm_rotate.restype = ctypes.c_int32
+    lib.ba_norm_rotate.argtypes = [_HP, _NP, _TP, _TP, _TP, _TP, ctypes.c_int32, _VP, ctypes.c_int32, _VP]
+    lib.ba_norm_rotate_backward.restype = ctypes.c_int32
+    lib.ba_norm_rotate_backward.argtypes = [_HP, _NP, _TP, _TP, _TP, _TP, _TP, _TP, _VP, _VP, ctypes.c_int32, _VP, ctypes.c_int32, _VP,
+                                            ctypes.c_size_t, _VP]
+    lib.ba_norm_rotate_backward_workspace_bytes.restype = ctypes.c_size_t
+    lib.ba_norm_rotate_backward_workspace_bytes.argtypes = [_HP, ctypes.c_int32]
+    lib.ba_paged_append.restype = ctypes.c_int32
+    lib.ba_paged_append.argtypes = [_HP, _NP, _CP, _TP, _TP, _TP, _TP, ctypes.c_int32, _VP, _VP, _VP, ctypes.c_int32, _VP]
+    lib.ba_paged_attention.restype = ctypes.c_int32
+    lib.ba_paged_attention.argtypes = [_HP, _CP, _TP, _TP, _VP, ctypes.c_int32, _VP, ctypes.c_int32, ctypes.c_int32, _I32P, _I32P, _VP,
+                                       ctypes.c_size_t, _VP]
+    lib.ba_paged_attention_workspace_bytes.restype = ctypes.c_size_t
+    lib.ba_paged_attention_workspace_bytes.argtypes = [_HP, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _I32P, _I32P]
     _WP = ctypes.POINTER(BaWorkItem)
     lib.ba_schedule_final_block.restype = ctypes.c_int64
     lib.ba_schedule_final_block.argtypes = [_HP, ctypes.c_int32, _I32P, _I32P, ctypes.c_int32, _WP, ctypes.c_int64]
@@ -226,6 +253,59 @@ class Heads:
         self.n_q_heads, self.n_kv_heads, self.head_dim = n_q_heads, n_kv_heads, head_dim
 
 
+class HeadNorm:
+    """Gains and epsilon of the query and key norms (ba_head_norm); keeps the gains alive.  None: gains of one."""
+
+    def __init__(self, q_weight=None, k_weight=None, eps: float = 1e-6):
+        import torch
+        dtype = None
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is None:
+                continue
+            if not w.is_cuda or w.dtype not in (torch.bfloat16, torch.float32) or w.dim() != 1 or not w.is_contiguous():
+                raise ValueError(f"{name}: expected a contiguous bfloat16 or float32 [head_dim] tensor in GPU memory")
+            if dtype is not None and w.dtype != dtype:
+                raise ValueError("q_weight and k_weight: one dtype for both")
+            dtype = w.dtype
+        self.q_weight, self.k_weight, self.eps = q_weight, k_weight, float(eps)
+        self.c = BaHeadNorm(None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+                            DTYPE_F32 if dtype is None or dtype == torch.float32 else DTYPE_BF16, self.eps)
+
+    def _check(self, head_dim: int) -> None:
+        for name, w in (("q_weight", self.q_weight), ("k_weight", self.k_weight)):
+            if w is not None and w.shape[0] != head_dim:
+                raise ValueError(f"{name}: {w.shape[0]} gains, the call's head description says {head_dim}")
+
+
+class PagedCache:
+    """Keys and values in pages (ba_paged_cache): ``k_pages`` and ``v_pages`` [pages, rows, KV heads, D] bfloat16 tensors of any
+    strides, D contiguous; ``page_table`` int32 [sequences, pages of a sequence], all on the GPU.  Keeps them alive; what is
+    written into them later counts."""
+
+    def __init__(self, k_pages, v_pages, page_table):
+        import torch
+        for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+            if t.dim() != 4 or t.shape[0] < 1 or t.shape[1] < 1:
+                raise ValueError(f"{name}: expected a [pages, rows, heads, head_dim] tensor of at least one page")
+        if k_pages.shape != v_pages.shape:
+            raise ValueError("k_pages and v_pages: shapes differ")
+        if (not page_table.is_cuda or page_table.dtype != torch.int32 or page_table.dim() != 2
+                or (page_table.shape[1] > 1 and page_table.stride(1) != 1)):
+            raise ValueError("page_table: expected an int32 [sequences, pages] tensor in GPU memory, its rows contiguous")
+        self.k_pages, self.v_pages, self.page_table = k_pages, v_pages, page_table
+        n_pages, rows, self.n_kv_heads, self.head_dim = k_pages.shape
+        self.n_seqs, max_pages = page_table.shape
+        k, v = (_tensor(t, name, layers=True) for name, t in (("k_pages", k_pages), ("v_pages", v_pages)))
+        self.max_rows = max_pages * rows
+        self.c = BaPagedCache(k, v, k_pages.stride(0), v_pages.stride(0), n_pages, rows, page_table.data_ptr(), page_table.stride(0),
+                              self.n_seqs, max_pages)
+
+    def _check(self, heads: "Heads") -> None:
+        if (self.n_kv_heads, self.head_dim) != (heads.n_kv_heads, heads.head_dim):
+            raise ValueError(f"cache: {self.n_kv_heads} heads of {self.head_dim}, the call's head description says "
+                             f"{heads.n_kv_heads} of {heads.head_dim}")
+
+
 _dtype_codes = None  # torch dtype -> BA_DTYPE_*, filled on first use (torch is imported lazily)
 
 
@@ -295,6 +375,27 @@ def _lse(t, name: str, tokens: int, n_q_heads: int):
         raise ValueError(f"{name}: expected a contiguous float32 [tokens, n_q_heads] tensor in GPU memory")
     if t.shape[1] != n_q_heads or t.shape[0] < tokens:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, the call needs [{tokens}, {n_q_heads}]")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _dev_ints(t, name: str, n: int):
+    """int32 [n] or longer, contiguous, on the GPU -> pointer (None stays None)."""
+    if t is None:
+        return None
+    import torch
+    if not t.is_cuda or t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous int32 tensor of one dimension in GPU memory")
+    if t.shape[0] < n:
+        raise ValueError(f"{name}: {t.shape[0]} entries, the call needs {n}")
+    return ctypes.c_void_p(t.data_ptr())
+
+
+def _gain_grad(t, name: str, head_dim: int):
+    if t is None:
+        return None
+    import torch
+    if not t.is_cuda or t.dtype != torch.float32 or tuple(t.shape) != (head_dim,) or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous float32 [{head_dim}] tensor in GPU memory")
     return ctypes.c_void_p(t.data_ptr())
 
 
@@ -530,6 +631,83 @@ def ba_block_attention_prompts_backward(heads: Heads, q, k, v, o, lse, d_out, dq
                                                       _ref(ts[3]), _lse(lse, "lse", T, hq), _ref(ts[4]),
                                                       _ref(ts[5]), _ref(ts[6]), _ref(ts[7]), len(cb) - 1, _ip(cb),
                                                       _ip(offs), wp, wb, _stream_handle(stream)))
+
+
+def _tokens_of(*tensors) -> int:
+    for t in tensors:
+        if t is not None:
+            return int(t.shape[0])
+    raise ValueError("q and k: both None")
+
+
+def ba_norm_rotate(heads: Heads, norm: HeadNorm, q, k, q_out, k_out, positions=None, rope_mode: int = ROPE_APPLY, stream=None) -> None:
+    """All tokens of ``q`` and ``k`` (either may be None); positions: int32 on the GPU."""
+    norm._check(heads.head_dim)
+    n = _tokens_of(q, k)
+    tq, tk = (_tensor(t, name, h, heads.head_dim, n, allow_f32=True) for t, name, h in ((q, "q", heads.n_q_heads), (k, "k", heads.n_kv_heads)))
+    tqo, tko = (_tensor(t, name, h, heads.head_dim, n, allow_f32=True)
+                for t, name, h in ((q_out, "q_out", heads.n_q_heads), (k_out, "k_out", heads.n_kv_heads)))
+    _check(load().ba_norm_rotate(ctypes.byref(heads.c), ctypes.byref(norm.c), _ref(tq), _ref(tk), _ref(tqo), _ref(tko), n,
+                                 _dev_ints(positions, "positions", n), rope_mode, _stream_handle(stream)))
+
+
+def ba_norm_rotate_backward_workspace_bytes(heads: Heads, n_tokens: int) -> int:
+    return int(load().ba_norm_rotate_backward_workspace_bytes(ctypes.byref(heads.c), n_tokens))
+
+
+def ba_norm_rotate_backward(heads: Heads, norm: HeadNorm, q, k, d_q_out, d_k_out, dq, dk, dq_weight=None, dk_weight=None, positions=None,
+                            rope_mode: int = ROPE_APPLY, ws=None, stream=None) -> None:
+    norm._check(heads.head_dim)
+    n, d = _tokens_of(q, k), heads.head_dim
+    of = [_tensor(t, name, heads.n_q_heads if "q" in name else heads.n_kv_heads, d, n, allow_f32=True)
+          for t, name in ((q, "q"), (k, "k"), (d_q_out, "d_q_out"), (d_k_out, "d_k_out"), (dq, "dq"), (dk, "dk"))]
+    wp, wb = _ws(ws)
+    _check(load().ba_norm_rotate_backward(ctypes.byref(heads.c), ctypes.byref(norm.c), *(_ref(t) for t in of),
+                                          _gain_grad(dq_weight, "dq_weight", d), _gain_grad(dk_weight, "dk_weight", d), n,
+                                          _dev_ints(positions, "positions", n), rope_mode, wp, wb, _stream_handle(stream)))
+
+
+def ba_paged_append(heads: Heads, norm: Optional[HeadNorm], cache: PagedCache, q, k, v, q_out, cache_pos, seq_of_token=None, rope_pos=None,
+                    rope_mode: int = ROPE_APPLY, stream=None) -> None:
+    """All tokens of ``k``; cache_pos, seq_of_token, rope_pos: int32 on the GPU."""
+    cache._check(heads)
+    if norm is not None:
+        norm._check(heads.head_dim)
+    n, d = int(k.shape[0]), heads.head_dim
+    tk, tv = _tensor(k, "k", heads.n_kv_heads, d), _tensor(v, "v", heads.n_kv_heads, d, n)
+    tq, tqo = _tensor(q, "q", heads.n_q_heads, d, n), _tensor(q_out, "q_out", heads.n_q_heads, d, n)
+    _check(load().ba_paged_append(ctypes.byref(heads.c), None if norm is None else ctypes.byref(norm.c), ctypes.byref(cache.c), _ref(tq),
+                                  _ref(tk), _ref(tv), _ref(tqo), n, _dev_ints(cache_pos, "cache_pos", n),
+                                  _dev_ints(seq_of_token, "seq_of_token", n), _dev_ints(rope_pos, "rope_pos", n), rope_mode,
+                                  _stream_handle(stream)))
+
+
+def ba_paged_attention_workspace_bytes(heads: Heads, n_seqs: int, q_per_seq: int, max_len: int, cu_group=None, prefix_len=None) -> int:
+    cu, pre = _ints(cu_group), _ints(prefix_len)
+    n = _n_groups(cu, pre)
+    return int(load().ba_paged_attention_workspace_bytes(ctypes.byref(heads.c), n_seqs, q_per_seq, max_len, n, _ip(cu), _ip(pre)))
+
+
+def _n_groups(cu, pre) -> int:
+    if cu is None and pre is None:
+        return 0
+    if cu is None or pre is None or len(cu) != len(pre) + 1:
+        raise ValueError("cu_group: one entry more than prefix_len")
+    return len(pre)
+
+
+def ba_paged_attention(heads: Heads, cache: PagedCache, q, o_out, lse_out, seq_len, max_len: int, cu_group=None, prefix_len=None,
+                       q_per_seq: int = 1, ws=None, stream=None) -> None:
+    """seq_len: int32 on the GPU, at most max_len; cu_group, prefix_len: host arrays (None: nothing is shared)."""
+    cache._check(heads)
+    n = cache.n_seqs * q_per_seq
+    cu, pre = _ints(cu_group), _ints(prefix_len)
+    tq, to = _tensor(q, "q", heads.n_q_heads, heads.head_dim, n), _tensor(o_out, "o_out", heads.n_q_heads, heads.head_dim, n)
+    lse = _lse(lse_out, "lse_out", n, heads.n_q_heads)
+    wp, wb = _ws(ws)
+    _check(load().ba_paged_attention(ctypes.byref(heads.c), ctypes.byref(cache.c), _ref(tq), _ref(to), lse, q_per_seq,
+                                     _dev_ints(seq_len, "seq_len", cache.n_seqs), max_len, _n_groups(cu, pre), _ip(cu), _ip(pre), wp, wb,
+                                     _stream_handle(stream)))
 
 
 def _schedule(fn, *args):

@@ -117,17 +117,17 @@ __device__ __forceinline__ void rotate_fragments(u32x4_t (&raw)[KCH], const f32x
   }
 }
 
-// Sum over each run of N consecutive lanes (8 or 16), in every lane of the run: adds of neighbours
+// Sum over each run of N consecutive lanes (4, 8 or 16), in every lane of the run: adds of neighbours
 // through the vector unit's own lane permutations, no trip through LDS.
 template <int N>
 __device__ __forceinline__ float sum_over_lanes(float x) {
-  static_assert(N == 8 || N == 16, "runs inside one row of sixteen lanes");
+  static_assert(N == 4 || N == 8 || N == 16, "runs inside one row of sixteen lanes");
   auto add = [&](auto ctrl) __attribute__((always_inline)) {
     x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
   };
   add(std::integral_constant<int, 0xb1>{});   // lane ^ 1
   add(std::integral_constant<int, 0x4e>{});   // lane ^ 2
-  add(std::integral_constant<int, 0x141>{});  // the other four of eight (mirrored: they all hold one sum)
+  if constexpr (N > 4) add(std::integral_constant<int, 0x141>{});  // the other four of eight (mirrored: they all hold one sum)
   if constexpr (N == 16) add(std::integral_constant<int, 0x140>{});  // the other eight of sixteen
   return x;
 }

@@ -1,0 +1,90 @@
+// Internal interface between the C boundary (ba_api_paged.hip) and the kernels of head norms (head_norm.hip) and
+// of the paged cache's attention (paged_attention.hip).
+#pragma once
+
+#include "ba_internal.h"
+
+namespace ba {
+
+// ---------------------------------------------------------------- head norms, appending ----------
+enum { kRowsQ = 0, kRowsK = 1, kRowsV = 2 };
+
+// Rows of up to three tensors [tokens][heads][D] on their way through one pass: queries and keys normed (eps >= 0) and
+// rotated, values copied.  A null src leaves a tensor out.
+struct HeadRowsParams {
+  const void *src[3];
+  void *dst[3];
+  int64_t src_st[3], src_sh[3], dst_st[3], dst_sh[3];  // token / head strides, elements
+  int32_t n_heads[3];
+  const void *weight[2];  // gains of the query and key norm, null: ones
+  int32_t weight_f32;
+  float eps;              // negative: no norm
+  int32_t n_tokens, head_dim, dtype, layout, rope;
+  const int32_t *positions;  // device, null: a token's number
+  // keys and values into pages (dst of kRowsK, kRowsV: page 0, row 0)
+  const int32_t *page_table, *seq_of_token, *cache_pos;
+  int64_t stride_table, dst_page[3];
+  int32_t n_seqs, n_pages, max_rows;  // max_rows: rows that a sequence's part of the table spans
+  int32_t page_rows;
+  FastDiv page_div;
+};
+hipError_t launch_norm_rotate(const HeadRowsParams &p, const RopeTable &rt, hipStream_t stream);
+hipError_t launch_paged_append(const HeadRowsParams &p, const RopeTable &rt, hipStream_t stream);
+
+// src, dst, weight and positions as above (queries and keys only); grad: the gradient of dst's forward counterpart
+struct NormBackwardParams {
+  HeadRowsParams rows;
+  const void *grad[2];
+  int64_t grad_st[2], grad_sh[2];
+  float *weight_grad[2];  // device [D], nullable
+  float *partial;         // [workgroups][2][D]
+  int32_t n_wg;
+};
+constexpr int kNormBwdMaxWg = 1024;
+hipError_t launch_norm_rotate_backward(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream);
+
+// ---------------------------------------------------------------- attention over pages ----------
+constexpr int kPagedTileRows = 128, kPagedTileKeys = 32;
+constexpr int kPagedMaxChunk = 2048;  // keys of a work item at most: its part of the page table lies in LDS
+
+struct PagedAttnParams {
+  const uint16_t *q;
+  int64_t q_st, q_sh;
+  uint16_t *o;
+  int64_t o_st, o_sh;
+  float *lse;  // [tokens][query heads], nullable
+  const uint16_t *k, *v;
+  int64_t k_sh, v_sh;          // head strides, elements
+  int64_t k_page_b, v_page_b;  // bytes from page to page
+  uint32_t k_rb, v_rb;         // bytes from row to row
+  const int32_t *page_table;
+  int64_t stride_table;
+  int32_t n_pages, page_rows;
+  FastDiv page_div, group_div, nq_div;
+  const int32_t *seq_len;
+  int32_t cap;  // no sequence is taken to be longer
+  int32_t n_seqs, nq, group, n_kv_heads;
+  float scale_log2e;
+  int32_t chunk;  // keys of a work item
+  int32_t prefix_items;
+  int32_t own_splits, own_row_tiles;
+  float *part_o, *part_ml;  // [part][token][query head][D], [..][2]: (reference in log2 units, sum)
+  int64_t part_rows;        // tokens * query heads
+  int32_t direct;           // one part for every row: the result itself
+};
+// Groups of sequences that share a prefix, in the order of their sequences.
+template <int N>
+struct PagedGroupsT {
+  static constexpr int kGroups = N;
+  int32_t n;
+  int32_t seq0[N], members[N], prefix[N], splits[N], item0[N + 1];
+};
+using PagedGroups = PagedGroupsT<96>;
+using PagedGroupsSmall = PagedGroupsT<8>;
+
+template <typename Groups>
+hipError_t launch_paged_attention(const PagedAttnParams &p, const Groups &g, int head_dim, hipStream_t stream);
+template <typename Groups>
+hipError_t launch_paged_merge(const PagedAttnParams &p, const Groups &g, int head_dim, hipStream_t stream);
+
+}  // namespace ba
