@@ -132,7 +132,7 @@ Extent pool_extent(const ba_tensor *t, int64_t stride_page, const ba_paged_cache
 // Sequences [seq0, seq0 + n_seqs) with at most kMost groups that share something.
 struct PagedPlan {
   int32_t seq0, n_seqs, group_end;  // (group_end: the first group that is left for the next plan)
-  int32_t chunk, own_splits, own_row_tiles, prefix_items;
+  int32_t chunk, own_chunk, own_splits, own_row_tiles, prefix_items;
   int32_t parts;
   PagedGroups groups;
 };
@@ -155,14 +155,14 @@ void plan_paged(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, 
                 const int32_t *prefix_len, int g0, int cus, PagedPlan *pl) {
   memset(pl, 0, sizeof(*pl));
   const int64_t G = h->n_q_heads / h->n_kv_heads, hkv = h->n_kv_heads;
-  auto tiles = [](int64_t keys) { return (keys + kPagedTileKeys - 1) / kPagedTileKeys; };
-  pl->own_row_tiles = (int32_t)((nq * G + kPagedTileRows - 1) / kPagedTileRows);
-  int64_t work = 0;  // key tiles of all items
+  auto row_tiles = [](int64_t rows) { return (rows + paged_tile_rows((int)rows) - 1) / paged_tile_rows((int)rows); };
+  pl->own_row_tiles = (int32_t)row_tiles(nq * G);
+  int64_t prefix_work = 0, own_work = 0;  // keys of all items together
   int32_t least_prefix = max_len;
   if (n_groups == 0) {
     pl->n_seqs = n_seqs;
     least_prefix = 0;
-    work = n_seqs * tiles(max_len) * pl->own_row_tiles * hkv;
+    own_work = (int64_t)n_seqs * max_len * pl->own_row_tiles * hkv;
   } else {
     pl->seq0 = cu_group[g0];
     int g = g0;
@@ -176,25 +176,29 @@ void plan_paged(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, 
         pl->groups.seq0[i] = cu_group[g] - pl->seq0;
         pl->groups.members[i] = members;
         pl->groups.prefix[i] = prefix;
-        work += tiles(prefix) * ((members * nq * G + kPagedTileRows - 1) / kPagedTileRows) * hkv;
+        prefix_work += prefix * row_tiles(members * nq * G) * hkv;
       }
       if (members > 0) least_prefix = std::min(least_prefix, prefix);
-      work += members * tiles(max_len - prefix) * pl->own_row_tiles * hkv;
+      own_work += (int64_t)members * (max_len - prefix) * pl->own_row_tiles * hkv;
     }
     pl->group_end = g;
     pl->n_seqs = cu_group[g] - pl->seq0;
   }
-  int64_t chunk_tiles = std::max<int64_t>(4, (work + 4 * cus - 1) / (4 * cus));
-  pl->chunk = (int32_t)std::min<int64_t>(chunk_tiles * kPagedTileKeys, kPagedMaxChunk);
-  auto splits = [&](int64_t keys) { return (int32_t)((keys + pl->chunk - 1) / pl->chunk); };
-  pl->own_splits = splits(max_len - least_prefix);
+  const int64_t slots = 2 * cus;
+  auto chunk_of = [&](int64_t keys, int64_t least, int64_t most) {
+    return (int32_t)std::min(most, std::max(least, (keys + 63) / 64 * 64));
+  };
+  pl->chunk = chunk_of((prefix_work + own_work / 4) / slots, 128, kPagedMaxChunk);
+  pl->own_chunk = chunk_of((prefix_work + own_work) / (4 * slots), std::max<int64_t>(64, std::min<int64_t>(512, nq * G * 8)), 1024);
+  auto splits = [&](int64_t keys, int64_t chunk) { return (int32_t)((keys + chunk - 1) / chunk); };
+  pl->own_splits = splits(max_len - least_prefix / 16 * 16, pl->own_chunk);
   pl->parts = least_prefix == 0 ? pl->own_splits : 0;
   int32_t items = 0;
   for (int i = 0; i < pl->groups.n; ++i) {
-    pl->groups.splits[i] = splits(pl->groups.prefix[i]);
+    pl->groups.splits[i] = splits(pl->groups.prefix[i], pl->chunk);
     pl->groups.item0[i] = items;
-    items += (int32_t)(pl->groups.splits[i] * ((pl->groups.members[i] * nq * G + kPagedTileRows - 1) / kPagedTileRows) * hkv);
-    pl->parts = std::max(pl->parts, pl->groups.splits[i] + splits(max_len - pl->groups.prefix[i]));
+    items += (int32_t)(pl->groups.splits[i] * row_tiles(pl->groups.members[i] * nq * G) * hkv);
+    pl->parts = std::max(pl->parts, pl->groups.splits[i] + splits(max_len - pl->groups.prefix[i] / 16 * 16, pl->own_chunk));
   }
   pl->groups.item0[pl->groups.n] = items;
   pl->prefix_items = items;
@@ -431,9 +435,10 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
     p.cap = max_len;
     p.n_seqs = pl.n_seqs, p.nq = q_per_seq, p.n_kv_heads = heads->n_kv_heads;
     p.scale_log2e = scale_log2e(heads);
-    p.chunk = pl.chunk, p.prefix_items = pl.prefix_items;
+    p.chunk = pl.chunk, p.own_chunk = pl.own_chunk, p.prefix_items = pl.prefix_items;
     p.own_splits = pl.own_splits, p.own_row_tiles = pl.own_row_tiles;
     p.part_rows = (int64_t)pl.n_seqs * q_per_seq * heads->n_q_heads;
+    p.max_parts = pl.parts;
     p.direct = pl.parts <= 1 && pl.groups.n == 0;
     p.part_o = (float *)ws;
     p.part_ml = (float *)((char *)ws + align256((size_t)p.part_rows * pl.parts * heads->head_dim * 4));

@@ -44,7 +44,9 @@ constexpr int kNormBwdMaxWg = 1024;
 hipError_t launch_norm_rotate_backward(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream);
 
 // ---------------------------------------------------------------- attention over pages ----------
-constexpr int kPagedTileRows = 128, kPagedTileKeys = 32;
+constexpr int kPagedTileRows = 128;    // rows of a work item
+constexpr int kPagedStreamRows = 48;   // ... up to this many in a problem: all of them
+BA_HD int paged_tile_rows(int n_rows) { return n_rows > kPagedStreamRows ? kPagedTileRows : kPagedStreamRows; }
 constexpr int kPagedMaxChunk = 2048;  // keys of a work item at most: its part of the page table lies in LDS
 
 struct PagedAttnParams {
@@ -65,11 +67,12 @@ struct PagedAttnParams {
   int32_t cap;  // no sequence is taken to be longer
   int32_t n_seqs, nq, group, n_kv_heads;
   float scale_log2e;
-  int32_t chunk;  // keys of a work item
+  int32_t chunk, own_chunk;  // keys of a work item of a prefix, of a sequence's own
   int32_t prefix_items;
   int32_t own_splits, own_row_tiles;
   float *part_o, *part_ml;  // [part][token][query head][D], [..][2]: (reference in log2 units, sum)
   int64_t part_rows;        // tokens * query heads
+  int32_t max_parts;        // of a row
   int32_t direct;           // one part for every row: the result itself
 };
 // Groups of sequences that share a prefix, in the order of their sequences.

@@ -2,13 +2,23 @@
 // sequences begin with the same pages (arXiv 2409.15355, Section 2.5's final block, token by token: many questions over one set of
 // passages).  For token t at position pos(t), head h: o = sum_{s <= pos} softmax_s(scale <q, k_s>) v_s.
 //
-// A work item is 128 packed rows (row = token * G + head in group) of one KV head over a range of keys:
+// A work item is a tile of packed rows (row = token * G + head in group) of one KV head over a range of keys:
 //   - of a group's prefix, for the rows of all its sequences: its keys are read once for all of them;
 //   - of what a sequence has behind the prefix, for its own rows.
 // Every item leaves, per row, its output, reference and sum; paged_merge_kernel adds a row's parts up in their order.
-// Keys and values come from the pages straight into LDS, two tiles of 32 keys ahead; the item's part of the page table lies in LDS.
-// Scores are S^T = K Q^T with v_mfma_f32_32x32x16_bf16 (keys along registers, rows along lanes), the exponentials are then the
-// operand of O^T = V^T P^T.  Scores, softmax, sums and parts in 32 bits; P is rounded to bf16 for the second product.
+//
+// Two walks, by the item's rows:
+//   - up to kPagedStreamRows rows, bound by the stream of keys and values: the four waves of a workgroup take tiles of 16 keys in turn,
+//     each through LDS of its own and without a barrier, 16 rows an MFMA (v_mfma_f32_16x16x32_bf16 for S^T = K Q^T, 16x16x16 for
+//     O^T = V^T P^T), and add their sums up at the end;
+//   - beyond, bound by the products: the waves take 32 rows each (v_mfma_f32_32x32x16_bf16) of 128 and share tiles of 32 keys.
+// Two workgroups a compute unit either way.  Keys and values come from the pages straight into LDS; the item's part of the page table lies
+// in LDS.  Tiles begin at multiples of 16 keys, so where a page's rows are a multiple of 16 a load instruction's rows are all of one page and
+// its address is a scalar (kAligned); otherwise every lane looks its own row's page up.
+// The exponentials come out as the operand of the second product.  Scores, softmax, sums and parts in 32 bits; P is rounded to
+// bf16 for the second product.
+#include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "ba_device.h"
@@ -18,30 +28,34 @@
 namespace ba {
 namespace {
 
-constexpr int kPWaves = kPagedTileRows / 32;
+constexpr int kPWaves = 4;
 constexpr int kPThreads = kPWaves * 64;
-constexpr int kPKeys = kPagedTileKeys;
-constexpr int kPBuf = 3;
 constexpr float kRebaseAbove = 1099511627776.0f;  // 2^40: a tile sum beyond this moves the reference
+constexpr int kTilesB = 65536;                    // LDS of the tiles, then the page table's part
 
 template <int D>
 struct PGeo {
-  static constexpr int KCH = D / 16;       // k-steps of the QK contraction
-  static constexpr int DT = D / 32;        // 32-row slabs of O^T
   static constexpr int CPR = D / 8;        // 16-byte chunks per row
   static constexpr int ROWB = D * 2;       // bytes per K/V row in LDS
   static constexpr int LPR = 256 / ROWB;   // rows per 256-byte LDS line
-  static constexpr int GPR = ROWB / 64;    // 64-byte granules per row
-  static constexpr int TILEB = kPKeys * ROWB;
   static constexpr int RPI = 1024 / ROWB;  // rows filled by one LDS-direct wave instruction
-  static constexpr int IPW = kPKeys / RPI / kPWaves;
-  static constexpr int TABLE = 2 * kPBuf * TILEB;  // where the page table's part lies
 };
+typedef __attribute__((address_space(3))) int32_t lds_int;
+typedef __attribute__((address_space(3))) float lds_float;
+typedef __attribute__((address_space(3))) f32x4_t lds_f32x4;
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+typedef const __attribute__((address_space(3))) bf16x8_t lds_bf16x8;
 
 // lds_dma16 with an address per lane: rows of different pages
 __device__ __forceinline__ void lds_dma16_from(const char *from, uint32_t lds_base) {
   lds_base = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_base);
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(lds_base) : "memory");
+}
+// value held by lane ^ 16
+__device__ __forceinline__ float other_sixteen(float x) {
+  const uint32_t u = __float_as_uint(x);
+  auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return (threadIdx.x & 16) ? __uint_as_float(r[0]) : __uint_as_float(r[1]);
 }
 
 // index of the group that sequence `seq` belongs to, or -1
@@ -56,176 +70,400 @@ __device__ __forceinline__ int group_of(const Groups &g, int seq) {
 }
 __device__ __forceinline__ int length_of(const PagedAttnParams &p, int seq) { return max(0, min(p.seq_len[seq], p.cap)); }
 
-template <int D, typename Groups>
-__global__ __launch_bounds__(kPThreads, D == 64 ? 3 : 2) void paged_attn_kernel(PagedAttnParams p, Groups groups) {
+struct PagedItem {
+  int seq0;           // its rows are those of the sequences from this one on; its pages this one's
+  int n_rows, row0;   // rows of the problem, first row of the tile
+  int kvh, part;
+  int k_lo, k0, k1;   // keys [k_lo, k1), tiles from k0 (a multiple of 16) on
+  int page0;          // first entry of the page table in LDS
+  bool holes;         // some pages are not there
+};
+// Row r of an item's problem.
+struct PagedRow {
+  int64_t tok;
+  int head;
+  int limit;  // it sees the item's keys below this
+};
+__device__ __forceinline__ PagedRow paged_row(const PagedAttnParams &p, const PagedItem &it, int r) {
+  PagedRow w;
+  const int tok = (int)fast_div((uint32_t)r, p.group_div), seq = (int)fast_div((uint32_t)tok, p.nq_div);
+  w.tok = (int64_t)it.seq0 * p.nq + tok;
+  w.head = it.kvh * p.group + r - tok * p.group;
+  w.limit = min(it.k1, length_of(p, it.seq0 + seq) - p.nq + (tok - seq * p.nq) + 1);
+  return w;
+}
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) x = min(x, __shfl_xor(x, m));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// Where rows of the item's keys lie, and the loads of a wave instruction's worth of them (RPI rows from `key` on, which do not
+// cross a multiple of 16): lane l fetches chunk `chunk` of row l / CPR.
+template <int D, bool kAligned>
+struct PagedSource {
   using G = PGeo<D>;
-  extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
-  lds_char *smem = (lds_char *)smem_generic;
-  constexpr uint32_t TB = G::TILEB;
-  typedef __attribute__((address_space(3))) int32_t lds_int;
-
-  // ---- which work item ----------------------------------------------------------------------------
-  int seq0, n_rows, row0, kvh, k0, k1, part;
-  if ((int)blockIdx.x < p.prefix_items) {
-    // the row tiles of one range of keys share it: regroup the ids, which go round the 8 XCDs, so that each gets a run of items
-    const uint32_t n = (uint32_t)p.prefix_items, q = n / 8, r = n % 8, x = blockIdx.x % 8;
-    const int id = (int)(x * q + min(x, r) + blockIdx.x / 8);
-    int lo = 0, hi = groups.n;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (groups.item0[mid] <= id) lo = mid; else hi = mid;
+  const PagedAttnParams &p;
+  const PagedItem &it;
+  lds_char *table;
+  const char *k, *v;
+  int lane_row;
+  __device__ __forceinline__ PagedSource(const PagedAttnParams &p_, const PagedItem &it_, lds_char *table_, int lane)
+      : p(p_), it(it_), table(table_), k((const char *)(p_.k + it_.kvh * p_.k_sh)), v((const char *)(p_.v + it_.kvh * p_.v_sh)), lane_row(lane / G::CPR) {}
+  // the page of a key, -1: not there
+  __device__ __forceinline__ int page_of(int key, int &row) const {
+    const int i = (int)fast_div((uint32_t)key, p.page_div);
+    row = key - i * p.page_rows;
+    return ((const lds_int *)table)[i - it.page0];
+  }
+  // chunk offsets (bytes) of this lane in a row of keys and of values
+  __device__ __forceinline__ void fetch(int key, uint32_t kchunk, uint32_t vchunk, uint32_t k_to, uint32_t v_to) const {
+    int row;
+    if constexpr (kAligned) {
+      // (rows behind the item's last lie in the same page, whole blocks of 16 behind it are its last block once more; pages that are
+      // not there: page 0.  All of them are masked)
+      key = __builtin_amdgcn_readfirstlane(key);
+      key = min(key & ~15, (it.k1 - 1) & ~15) | (key & 15);
+      const int page = max(0, __builtin_amdgcn_readfirstlane(page_of(key, row)));
+      lds_dma16(k + page * p.k_page_b + (uint64_t)(uint32_t)row * p.k_rb, (uint32_t)lane_row * p.k_rb + kchunk, k_to);
+      lds_dma16(v + page * p.v_page_b + (uint64_t)(uint32_t)row * p.v_rb, (uint32_t)lane_row * p.v_rb + vchunk, v_to);
+    } else {
+      const int page = max(0, page_of(min(key + lane_row, it.k1 - 1), row));
+      lds_dma16_from(k + page * p.k_page_b + ((uint64_t)(uint32_t)row * p.k_rb + kchunk), k_to);
+      lds_dma16_from(v + page * p.v_page_b + ((uint64_t)(uint32_t)row * p.v_rb + vchunk), v_to);
     }
-    seq0 = groups.seq0[lo];
-    n_rows = groups.members[lo] * p.nq * p.group;
-    const int n_rt = (n_rows + kPagedTileRows - 1) / kPagedTileRows;
-    int rel = id - groups.item0[lo];
-    row0 = rel % n_rt * kPagedTileRows;
-    rel /= n_rt;
-    part = rel % groups.splits[lo];
-    kvh = rel / groups.splits[lo];
-    k0 = part * p.chunk;
-    k1 = min(groups.prefix[lo], k0 + p.chunk);
+  }
+  // bit i: key + i is one of the item's, and its page is there
+  template <int N>
+  __device__ __forceinline__ uint32_t there(int key, int lane) const {
+    const int at = key + (lane & (N - 1));
+    int row;
+    const bool ok = at >= it.k_lo && at < it.k1 && (!it.holes || page_of(max(it.k_lo, min(at, it.k1 - 1)), row) >= 0);
+    return (uint32_t)__builtin_amdgcn_ballot_w64(ok) & (N == 32 ? ~0u : (1u << (N & 31)) - 1u);
+  }
+};
+__device__ __forceinline__ uint32_t below(int lim) { return lim <= 0 ? 0u : lim >= 32 ? ~0u : (1u << lim) - 1u; }
+
+// Four or eight consecutive dimensions of a row's result: the row itself, or its part.
+template <int E>
+__device__ __forceinline__ void write_row(const PagedAttnParams &p, const PagedItem &it, const PagedRow &r, int D, int d, const float *o, float m, float l,
+                                          bool first) {
+  const int64_t row = r.tok * (p.n_kv_heads * p.group) + r.head;
+  if (p.direct) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t *to = p.o + r.tok * p.o_st + r.head * p.o_sh + d;
+#pragma unroll
+    for (int e = 0; e < E; e += 4)
+      *reinterpret_cast<u32x2_t *>(to + e) = u32x2_t{pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv)};
+    if (p.lse && first) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   } else {
-    int rel = (int)blockIdx.x - p.prefix_items;
-    kvh = rel % p.n_kv_heads;
-    rel /= p.n_kv_heads;
-    row0 = rel % p.own_row_tiles * kPagedTileRows;
-    rel /= p.own_row_tiles;
-    seq0 = rel % p.n_seqs;
-    part = rel / p.n_seqs;
-    n_rows = p.nq * p.group;
-    const int g = group_of(groups, seq0), prefix = g < 0 ? 0 : groups.prefix[g];
-    k0 = prefix + part * p.chunk;
-    k1 = min(length_of(p, seq0), k0 + p.chunk);
-    if (g >= 0) part += groups.splits[g];
-    if (k0 >= k1 && !p.direct) return;  // (the merge knows)
-    k1 = max(k0, k1);
-  }
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, hf = lane >> 5;
-  const int n_t = (k1 - k0 + kPKeys - 1) / kPKeys;
-
-  // ---- this lane's row: its token, the keys it sees ---------------------------------------------------
-  const int wave_row0 = row0 + wave * 32;
-  const bool live = wave_row0 < n_rows;
-  const int my_row = min(wave_row0 + col, n_rows - 1);
-  const int tok = (int)fast_div((uint32_t)my_row, p.group_div);
-  const int64_t q_tok = (int64_t)seq0 * p.nq + tok;
-  const int q_head = kvh * p.group + my_row - tok * p.group;
-  const int rel_seq = (int)fast_div((uint32_t)tok, p.nq_div);
-  const int limit = min(k1, length_of(p, seq0 + rel_seq) - p.nq + (tok - rel_seq * p.nq) + 1);  // keys below it
-  int least = limit;  // of the wave's rows
+    const int64_t at = it.part * p.part_rows + row;
 #pragma unroll
-  for (int m = 1; m < 64; m *= 2) least = min(least, __shfl_xor(least, m));
-  least = __builtin_amdgcn_readfirstlane(least);
-
-  bf16x8_t qf[G::KCH];  // Q rows, the B operand of S^T = K Q^T: lane = row, chunk 2 kk + hf
-  {
-    const uint16_t *row = p.q + q_tok * p.q_st + q_head * p.q_sh + hf * 8;
-#pragma unroll
-    for (int kk = 0; kk < G::KCH; ++kk) qf[kk] = *reinterpret_cast<const bf16x8_t *>(row + kk * 16);
+    for (int e = 0; e < E; e += 4) *reinterpret_cast<f32x4_t *>(p.part_o + at * D + d + e) = f32x4_t{o[e], o[e + 1], o[e + 2], o[e + 3]};
+    if (first) *reinterpret_cast<f32x2_t *>(p.part_ml + at * 2) = f32x2_t{l == 0.f ? -INFINITY : m, l};
   }
+}
 
-  // ---- the item's part of the page table --------------------------------------------------------------
-  const int page0 = (int)fast_div((uint32_t)k0, p.page_div);
-  bool holes = false;
-  if (k1 > k0) {
-    const int n_pages = (int)fast_div((uint32_t)(k1 - 1), p.page_div) - page0 + 1;
-    const int32_t *table = p.page_table + seq0 * p.stride_table + page0;
-    int bad = 0;
-    for (int i = threadIdx.x; i < n_pages; i += kPThreads) {
-      const int id = table[i];
-      const bool ok = id >= 0 && id < p.n_pages;
-      ((lds_int *)(smem + G::TABLE))[i] = ok ? id : -1;
-      bad |= !ok;
+// ---- few rows: RG groups of 16 ------------------------------------------------------------------------------------------
+template <int D, bool kAligned, int RG>
+__device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const PagedItem &it, lds_char *smem, int lane, int wave) {
+  using G = PGeo<D>;
+  constexpr int KK = D / 32, DS = D / 16;
+  constexpr uint32_t TB = 16 * G::ROWB;              // a tile of keys, then one of values
+  constexpr int NB = kTilesB / kPWaves / (2 * TB);   // tiles of a wave in LDS
+  constexpr int OPS = 16 / G::RPI;                   // load instructions per tile and kind
+  const PagedSource<D, kAligned> src(p, it, smem + kTilesB, lane);
+  const int col = lane & 15, quad = lane >> 4;
+  const int n_tiles = (it.k1 - it.k0 + 15) / 16;
+  const int n = n_tiles > wave ? (n_tiles - wave + kPWaves - 1) / kPWaves : 0;  // this wave's: wave, wave + 4, ...
+  const uint32_t ring = wave * (NB * 2 * TB);
+
+  auto issue = [&](int i) __attribute__((always_inline)) {
+    const int key = it.k0 + (wave + i * kPWaves) * 16;
+    const uint32_t to = (uint32_t)(uintptr_t)smem + ring + (uint32_t)(i % NB) * (2 * TB);
+    int ln = lane;
+    if (RG > 2) asm volatile("" : "+v"(ln));  // (worked out anew: kept, the offsets take registers that the sums need)
+#pragma unroll
+    for (int u = 0; u < OPS; ++u) {
+      const int r = u * G::RPI + ln / G::CPR, pos = ln % G::CPR;
+      const int line = r / G::LPR;
+      const uint32_t kchunk = (uint32_t)(pos ^ (line & (G::CPR - 1))) << 4;
+      const uint32_t vchunk = (uint32_t)((((pos >> 1) ^ (line & (G::CPR / 2 - 1))) << 1) | (pos & 1)) << 4;
+      src.fetch(key + u * G::RPI, kchunk, vchunk, to + u * 1024, to + TB + u * 1024);
     }
-    holes = __syncthreads_or(bad) != 0;
+  };
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+    if (i < n) issue(i);
+
+  bf16x8_t qf[RG][KK];
+  int limit[RG], least = 0x7fffffff;
+#pragma unroll
+  for (int g = 0; g < RG; ++g) {
+    const PagedRow r = paged_row(p, it, min(it.row0 + g * 16 + col, it.n_rows - 1));
+    limit[g] = r.limit;
+    least = min(least, r.limit);
+    const uint16_t *row = p.q + r.tok * p.q_st + r.head * p.q_sh + quad * 8;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qf[g][kk] = *reinterpret_cast<const bf16x8_t *>(row + kk * 32);
+  }
+  least = wave_min(least);
+#pragma unroll
+  for (int g = 0; g < RG; ++g)
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[g][kk]));
+
+  uint32_t k_rd[KK];
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) k_rd[kk] = ring + col * G::ROWB + (((kk * 4 + quad) ^ ((col / G::LPR) & (G::CPR - 1))) << 4);
+  const int v_row = quad * 4 + (col >> 2), v_swz = (v_row / G::LPR) & (G::CPR / 2 - 1);
+  const uint32_t v_rd = ring + TB + v_row * G::ROWB + (lane & 3) * 8;
+  f32x4_t o[RG][DS];
+  float mb[RG], l[RG];
+#pragma unroll
+  for (int g = 0; g < RG; ++g) {
+    mb[g] = -INFINITY;
+    l[g] = 0.f;
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) o[g][ds] = f32x4_t{0.f, 0.f, 0.f, 0.f};
   }
 
-  // ---- tile fill (swizzled on the global side) and fragment reads, as in the other attention kernels ----
-  uint32_t k_rd[G::KCH];
-  {
-    const int swz = (col / G::LPR) & (G::CPR - 1);
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) {
+    const uint32_t buf = (uint32_t)(i % NB) * (2 * TB);
+    const int newer = min(NB, n - i) - 1;  // tiles on their way behind this one
+    if (newer == 0) dma_wait<0>();
+    else if (NB == 2 || newer == 1) dma_wait<2 * OPS>();
+    else if (newer == 2) dma_wait<4 * OPS>();
+    else dma_wait<6 * OPS>();
+    const int key0 = it.k0 + (wave + i * kPWaves) * 16;
+    bf16x8_t kf[KK];
 #pragma unroll
-    for (int kk = 0; kk < G::KCH; ++kk) k_rd[kk] = col * G::ROWB + (((kk * 2 + hf) ^ swz) << 4);
+    for (int kk = 0; kk < KK; ++kk) kf[kk] = *(lds_bf16x8 *)(smem + (k_rd[kk] + buf));
+    s16x4_t vf[DS];
+    uint32_t swz = v_swz;
+    if (RG > 2) asm volatile("" : "+v"(swz));
+    auto v_frag = [&](int ds) __attribute__((always_inline)) {
+      return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + (v_rd + buf + ((ds ^ swz) << 5))));
+    };
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) vf[ds] = v_frag(ds);
+    const bool masked = it.holes || key0 < it.k_lo || key0 + 16 > least;
+    const uint32_t there = masked ? src.template there<16>(key0, lane) : 0xffffu;
+    // the tile is in registers: its place takes the one that is NB further on
+    lds_wait();
+    if (i + NB < n) issue(i + NB);
+#pragma unroll
+    for (int g = 0; g < RG; ++g) {
+      f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kk], qf[g][kk], s, 0, 0, 0);
+      const int lim = limit[g] - key0;
+      if (masked) {
+        const uint32_t mine = there & below(lim);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (!((mine >> (quad * 4 + e)) & 1)) s[e] = -INFINITY;
+      }
+      // the reference: the row's maximum in the first tile of which it sees a key, raised where an exponential threatens to overflow
+      auto row_max = [&]() __attribute__((always_inline)) {
+        float m = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
+        m = fmaxf(m, other_sixteen(m));
+        return fmaxf(m, other_half(m)) * p.scale_log2e;
+      };
+      if (__builtin_amdgcn_ballot_w64(mb[g] == -INFINITY) != 0) {
+        const float m = row_max();
+        if (mb[g] == -INFINITY) mb[g] = m;
+      }
+      float e4[4], sum;
+      auto exponentials = [&]() __attribute__((always_inline)) {
+        const float ref = mb[g] == -INFINITY ? 0.f : mb[g];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) e4[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], p.scale_log2e, -ref));
+        sum = (e4[0] + e4[1]) + (e4[2] + e4[3]);
+      };
+      exponentials();
+      if (__builtin_amdgcn_ballot_w64(!(sum < kRebaseAbove)) != 0) {
+        // (only the rows concerned: what another row's scores are changes no bit of this one)
+        float all = sum + other_sixteen(sum);
+        all += other_half(all);
+        const float m = !(all < kRebaseAbove) ? fmaxf(row_max(), mb[g]) : mb[g];
+        const float alpha = m == mb[g] ? 1.f : __builtin_amdgcn_exp2f(mb[g] - m);
+        mb[g] = m;
+        l[g] *= alpha;
+#pragma unroll
+        for (int ds = 0; ds < DS; ++ds)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[g][ds][e] *= alpha;
+        exponentials();
+      }
+      l[g] += sum;
+      const u32x2_t w = {pack_bf16(e4[0], e4[1]), pack_bf16(e4[2], e4[3])};
+      const s16x4_t pf = __builtin_bit_cast(s16x4_t, w);
+      if (!masked) {
+#pragma unroll
+        for (int ds = 0; ds < DS; ++ds) o[g][ds] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf[ds], pf, o[g][ds], 0, 0, 0);
+      } else {
+        // A masked probability is zero, but zero times an infinity or a NaN is not: values of keys that a row does not see must
+        // not reach its sums.  The rows that see the same keys go together, with every other key's values at zero.
+        uint64_t left = ~0ull;
+#pragma unroll 1
+        while (left) {
+          const int their_lim = __builtin_amdgcn_readlane(lim, __builtin_ctzll(left));
+          const bool mine = lim == their_lim;
+          left &= ~__builtin_amdgcn_ballot_w64(mine);
+          const uint32_t seen = there & below(their_lim);
+          if (seen == 0) continue;
+#pragma unroll
+          for (int ds = 0; ds < DS; ++ds) {
+            s16x4_t f = vf[ds];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!((seen >> (quad * 4 + e)) & 1)) f[e] = 0;
+            const f32x4_t add = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(f, pf, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[g][ds][e] += mine ? add[e] : 0.f;
+          }
+        }
+      }
+      if (RG > 1) __builtin_amdgcn_sched_barrier(0);  // (one group of rows after the other: together they need more registers than there are)
+    }
   }
-  uint32_t v_rd[G::DT];
+
+  // ---- the waves' sums, 16 rows at a time ----------------------------------------------------------------------
+  constexpr int OST = D + 4;  // (floats from row to row: 16 bytes on, off the last one's banks)
+  static_assert((size_t)kPWaves * 16 * (OST + 2) * 4 <= kTilesB, "the waves' sums fit the tiles' place");
+  lds_float *const os = (lds_float *)smem, *const mls = os + kPWaves * 16 * OST;
+  constexpr int E = D / 16;
+  const int tid = wave * 64 + lane, row = tid / 16, d = tid % 16 * E;
+#pragma unroll
+  for (int g = 0; g < RG; ++g) {
+    if (it.row0 + g * 16 >= it.n_rows) break;
+    __syncthreads();  // (everybody is done with the tiles, or with the rows before)
+    float lt = l[g] + other_sixteen(l[g]);
+    lt += other_half(lt);
+    if (quad == 0) {
+      mls[(wave * 16 + col) * 2] = lt == 0.f ? -INFINITY : mb[g];
+      mls[(wave * 16 + col) * 2 + 1] = lt;
+    }
+#pragma unroll
+    for (int ds = 0; ds < DS; ++ds) *(lds_f32x4 *)(os + (wave * 16 + col) * OST + ds * 16 + quad * 4) = o[g][ds];
+    __syncthreads();
+    float m = -INFINITY, lsum = 0.f, acc[E];
+#pragma unroll
+    for (int w = 0; w < kPWaves; ++w) m = fmaxf(m, mls[(w * 16 + row) * 2]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPWaves; ++w) {
+      const float lw = mls[(w * 16 + row) * 2 + 1];
+      const float f = lw == 0.f ? 0.f : __builtin_amdgcn_exp2f(mls[(w * 16 + row) * 2] - m);
+      lsum += lw * f;
+#pragma unroll
+      for (int e = 0; e < E; e += 4) {
+        const f32x4_t x = *(const lds_f32x4 *)(os + (w * 16 + row) * OST + d + e);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[e + c] += lw == 0.f ? 0.f : x[c] * f;
+      }
+    }
+    const int r = it.row0 + g * 16 + row;
+    if (r < it.n_rows) write_row<E>(p, it, paged_row(p, it, r), D, d, acc, m, lsum, d == 0);
+  }
+}
+
+// ---- many rows: 32 a wave, tiles of 32 keys shared by the four -----------------------------------------------------------
+template <int D, bool kAligned>
+__device__ __forceinline__ void walk_shared(const PagedAttnParams &p, const PagedItem &it, lds_char *smem, int lane, int wave) {
+  using G = PGeo<D>;
+  constexpr int KCH = D / 16, DT = D / 32, GPR = G::ROWB / 64;
+  constexpr uint32_t TB = 32 * G::ROWB;
+  constexpr int NB = 4;  // tiles in LDS
+  static_assert(NB * 2 * TB <= kTilesB, "the tiles fit");
+  constexpr int IPW = 32 / G::RPI / kPWaves;
+  const PagedSource<D, kAligned> src(p, it, smem + kTilesB, lane);
+  const int col = lane & 31, hf = lane >> 5;
+  const int n_t = (it.k1 - it.k0 + 31) / 32;
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    const uint32_t to = (uint32_t)(uintptr_t)smem + (uint32_t)(t % NB) * (2 * TB) + wave * IPW * 1024;
+#pragma unroll
+    for (int u = 0; u < IPW; ++u) {
+      const int r = (wave * IPW + u) * G::RPI + lane / G::CPR, pos = lane % G::CPR;
+      const uint32_t kchunk = (uint32_t)(pos ^ ((r / G::LPR) & (G::CPR - 1))) << 4;
+      const uint32_t vchunk = (uint32_t)((((pos >> 2) ^ ((r / G::LPR) & (GPR - 1))) << 2) | (pos & 3)) << 4;
+      src.fetch(it.k0 + t * 32 + (wave * IPW + u) * G::RPI, kchunk, vchunk, to + u * 1024, to + TB + u * 1024);
+    }
+  };
+  constexpr int OPS = 2 * IPW;  // of a wave and tile
+#pragma unroll
+  for (int t = 0; t < NB - 1; ++t)
+    if (t < n_t) issue(t);
+
+  const int wave_row0 = it.row0 + wave * 32;
+  const bool live = wave_row0 < it.n_rows;
+  const PagedRow me = paged_row(p, it, min(wave_row0 + col, it.n_rows - 1));
+  const int least = wave_min(me.limit);
+  bf16x8_t qf[KCH];  // Q rows, the B operand of S^T = K Q^T: lane = row, chunk 2 kk + hf
+  {
+    const uint16_t *row = p.q + me.tok * p.q_st + me.head * p.q_sh + hf * 8;
+#pragma unroll
+    for (int kk = 0; kk < KCH; ++kk) qf[kk] = *reinterpret_cast<const bf16x8_t *>(row + kk * 16);
+#pragma unroll
+    for (int kk = 0; kk < KCH; ++kk) asm volatile("" : "+v"(qf[kk]));
+  }
+  uint32_t k_rd[KCH], v_rd[DT];
+#pragma unroll
+  for (int kk = 0; kk < KCH; ++kk) k_rd[kk] = col * G::ROWB + (((kk * 2 + hf) ^ ((col / G::LPR) & (G::CPR - 1))) << 4);
   {
     const int vrow = hf * 4 + ((lane & 15) >> 2);
     const int vwithin = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-    const int swz = (vrow / G::LPR) & (G::GPR - 1);
 #pragma unroll
-    for (int dt = 0; dt < G::DT; ++dt) v_rd[dt] = vrow * G::ROWB + ((dt ^ swz) << 6) + vwithin;
+    for (int dt = 0; dt < DT; ++dt) v_rd[dt] = vrow * G::ROWB + ((dt ^ ((vrow / G::LPR) & (GPR - 1))) << 6) + vwithin;
   }
-  const char *k_base = (const char *)(p.k + kvh * p.k_sh), *v_base = (const char *)(p.v + kvh * p.v_sh);
-  const uint32_t lds_copy = (uint32_t)(uintptr_t)smem + wave * G::IPW * 1024;
-  auto page_of = [&](int key, int &row) __attribute__((always_inline)) {
-    const int i = (int)fast_div((uint32_t)key, p.page_div);
-    row = key - i * p.page_rows;
-    return ((const lds_int *)(smem + G::TABLE))[i - page0];
-  };
-  auto issue_copy = [&](int t, int buf) __attribute__((always_inline)) {
+  f32x16_t oacc[DT];
 #pragma unroll
-    for (int u = 0; u < G::IPW; ++u) {
-      const int r = (wave * G::IPW + u) * G::RPI + lane / G::CPR, pos = lane % G::CPR;
-      const uint32_t kchunk = (uint32_t)(pos ^ ((r / G::LPR) & (G::CPR - 1))) << 4;
-      const uint32_t vchunk = (uint32_t)((((pos >> 2) ^ ((r / G::LPR) & (G::GPR - 1))) << 2) | (pos & 3)) << 4;
-      int row;
-      // (rows behind the range take its last one; pages that are not there take page 0: both are masked)
-      const int page = max(0, page_of(min(k0 + t * kPKeys + r, k1 - 1), row));
-      lds_dma16_from(k_base + page * p.k_page_b + ((uint64_t)(uint32_t)row * p.k_rb + kchunk), lds_copy + (uint32_t)buf * (2 * TB) + u * 1024);
-      lds_dma16_from(v_base + page * p.v_page_b + ((uint64_t)(uint32_t)row * p.v_rb + vchunk), lds_copy + (uint32_t)buf * (2 * TB) + TB + u * 1024);
-    }
-  };
-  constexpr int kOpsPerTile = 2 * G::IPW;
-#pragma unroll
-  for (int kk = 0; kk < G::KCH; ++kk) asm volatile("" : "+v"(qf[kk]));  // the rows are waited for here, not inside the loop
-  if (n_t > 0) issue_copy(0, 0);
-  if (n_t > 1) issue_copy(1, 1);
-  __builtin_amdgcn_sched_barrier(0);
-
-  // ---- running state ------------------------------------------------------------------------------------
-  f32x16_t oacc[G::DT];
-#pragma unroll
-  for (int dt = 0; dt < G::DT; ++dt)
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
   float mb = -INFINITY;  // the row's reference, log2 units; not set before the row has seen a key
   float l_run = 0.f;     // this lane's share of the running sum of exponentials
+  constexpr int kWin = KCH < 4 ? KCH : 4;  // fragments on their way from LDS
 
-  int buf = 0;
 #pragma unroll 1
   for (int t = 0; t < n_t; ++t) {
-    if (t + 1 < n_t) dma_wait<kOpsPerTile>(); else dma_wait<0>();
+    const int newer = min(NB - 1, n_t - t) - 1;
+    if (newer == 0) dma_wait<0>();
+    else if (newer == 1) dma_wait<OPS>();
+    else dma_wait<2 * OPS>();
     wg_barrier();  // every wave's share of tile t has landed, and every wave is done with tile t - 1
-    if (t + 2 < n_t) issue_copy(t + 2, buf == 0 ? 2 : buf - 1);
+    if (t + NB - 1 < n_t) issue(t + NB - 1);
     if (live) {
-      const uint32_t kofs = (uint32_t)buf * (2 * TB), vofs = kofs + TB;
-      const int key0 = k0 + t * kPKeys;
+      const uint32_t kofs = (uint32_t)(t % NB) * (2 * TB), vofs = kofs + TB;
+      const int key0 = it.k0 + t * 32;
       f32x16_t s;
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = 0.f;
+      auto k_frag = [&](int kk) __attribute__((always_inline)) { return *(lds_bf16x8 *)(smem + (k_rd[kk] + kofs)); };
+      bf16x8_t fr[kWin];
 #pragma unroll
-      for (int kk = 0; kk < G::KCH; ++kk)
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            *reinterpret_cast<const __attribute__((address_space(3))) bf16x8_t *>(smem + (k_rd[kk] + kofs)), qf[kk], s, 0, 0, 0);
-      // keys that this lane's row does not see at -infinity
-      const bool masked = holes || key0 + kPKeys > least;
-      const int lim = limit - key0;
-      uint32_t there = ~0u;  // keys whose page is there
-      if (masked) {
-        if (holes) {
-          int row;
-          there = (uint32_t)__builtin_amdgcn_ballot_w64(page_of(min(key0 + col, k1 - 1), row) >= 0);
-        }
+      for (int kk = 0; kk < kWin; ++kk) fr[kk] = k_frag(kk);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          const int key = (v >> 2) * 8 + hf * 4 + (v & 3);
-          if (key >= lim || !((there >> key) & 1)) s[v] = -INFINITY;
-        }
+      for (int kk = 0; kk < KCH; ++kk) {
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[kk % kWin], qf[kk], s, 0, 0, 0);
+        if (kk + kWin < KCH) fr[kk % kWin] = k_frag(kk + kWin);
+        __builtin_amdgcn_sched_barrier(0);
       }
-      // the reference: the row's maximum in the first tile of which it sees a key, raised where an exponential threatens to overflow
+      // keys that this lane's row does not see at -infinity
+      const bool masked = it.holes || key0 < it.k_lo || key0 + 32 > least;
+      const int lim = me.limit - key0;
+      uint32_t there = ~0u;
+      if (masked) {
+        there = src.template there<32>(key0, lane);
+        const uint32_t mine = there & below(lim);
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (!((mine >> ((v >> 2) * 8 + hf * 4 + (v & 3))) & 1)) s[v] = -INFINITY;
+      }
       auto row_max = [&]() __attribute__((always_inline)) {
         float m = s[0];
 #pragma unroll
@@ -236,6 +474,17 @@ __global__ __launch_bounds__(kPThreads, D == 64 ? 3 : 2) void paged_attn_kernel(
         const float m = row_max();
         if (mb == -INFINITY) mb = m;
       }
+      auto v_frag = [&](int st) __attribute__((always_inline)) {
+        typedef short s16x8_t __attribute__((ext_vector_type(8)));
+        const int kc = st / DT, dt = st % DT;
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + (v_rd[dt] + vofs) + kc * 16 * G::ROWB));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + (v_rd[dt] + vofs) + (kc * 16 + 8) * G::ROWB));
+        return (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      };
+      bf16x8_t vf[kWin];
+#pragma unroll
+      for (int st = 0; st < 2; ++st) vf[st] = __builtin_bit_cast(bf16x8_t, v_frag(st));
+      __builtin_amdgcn_sched_barrier(0);
       bf16x8_t pf[2];
       float sum;
       auto exponentials = [&]() __attribute__((always_inline)) {
@@ -258,49 +507,44 @@ __global__ __launch_bounds__(kPThreads, D == 64 ? 3 : 2) void paged_attn_kernel(
       };
       exponentials();
       if (__builtin_amdgcn_ballot_w64(!(sum < kRebaseAbove)) != 0) {
-        // (only the rows concerned: what another row's scores are changes no bit of this one)
         const float m = !(sum + other_half(sum) < kRebaseAbove) ? fmaxf(row_max(), mb) : mb;
         const float alpha = m == mb ? 1.f : __builtin_amdgcn_exp2f(mb - m);
         mb = m;
         l_run *= alpha;
 #pragma unroll
-        for (int dt = 0; dt < G::DT; ++dt)
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
           for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
         exponentials();
       }
       l_run += sum;
-      auto v_frag = [&](int kc, int dt) __attribute__((always_inline)) {
-        typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
-        typedef short s16x8_t __attribute__((ext_vector_type(8)));
-        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + (v_rd[dt] + vofs) + kc * 16 * G::ROWB));
-        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + (v_rd[dt] + vofs) + (kc * 16 + 8) * G::ROWB));
-        return (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      };
       if (!masked) {
 #pragma unroll
-        for (int st = 0; st < 2 * G::DT; ++st)
-          oacc[st % G::DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, v_frag(st / G::DT, st % G::DT)), pf[st / G::DT],
-                                                                      oacc[st % G::DT], 0, 0, 0);
+        for (int st = 2; st < kWin; ++st) vf[st] = __builtin_bit_cast(bf16x8_t, v_frag(st));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int st = 0; st < 2 * DT; ++st) {
+          oacc[st % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[st % kWin], pf[st / DT], oacc[st % DT], 0, 0, 0);
+          if (st + kWin < 2 * DT) vf[st % kWin] = __builtin_bit_cast(bf16x8_t, v_frag(st + kWin));
+          __builtin_amdgcn_sched_barrier(0);
+        }
       } else {
-        // A masked probability is zero, but zero times an infinity or a NaN is not: values of keys that a row does not see must
-        // not reach its sums.  The rows that see the same keys go together, with every other key's values at zero.
-        uint64_t left = ~0ull;
+        uint64_t left = ~0ull;  // (as in walk_stream)
 #pragma unroll 1
         while (left) {
           const int their_lim = __builtin_amdgcn_readlane(lim, __builtin_ctzll(left));
           const bool mine = lim == their_lim;
           left &= ~__builtin_amdgcn_ballot_w64(mine);
-          const uint32_t seen = there & (their_lim <= 0 ? 0u : their_lim >= 32 ? ~0u : (1u << their_lim) - 1u);
+          const uint32_t seen = there & below(their_lim);
           if (seen == 0) continue;
 #pragma unroll
-          for (int dt = 0; dt < G::DT; ++dt) {
+          for (int dt = 0; dt < DT; ++dt) {
             f32x16_t add;
 #pragma unroll
             for (int v = 0; v < 16; ++v) add[v] = 0.f;
 #pragma unroll
             for (int kc = 0; kc < 2; ++kc) {
-              auto f = v_frag(kc, dt);
+              auto f = v_frag(kc * DT + dt);
 #pragma unroll
               for (int e = 0; e < 8; ++e)
                 if (!((seen >> (kc * 16 + (e >> 2) * 8 + hf * 4 + (e & 3))) & 1)) f[e] = 0;
@@ -312,67 +556,158 @@ __global__ __launch_bounds__(kPThreads, D == 64 ? 3 : 2) void paged_attn_kernel(
         }
       }
     }
-    buf = buf == kPBuf - 1 ? 0 : buf + 1;
   }
-
-  // ---- out: lane = row, four consecutive dimensions at a time -------------------------------------------
-  if (!live || wave_row0 + col >= n_rows) return;
+  if (!live || wave_row0 + col >= it.n_rows) return;
   const float l = l_run + other_half(l_run);
-  if (p.direct) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint16_t *o = p.o + q_tok * p.o_st + q_head * p.o_sh + hf * 4;
 #pragma unroll
-    for (int dt = 0; dt < G::DT; ++dt)
+  for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4) {
-        const u32x2_t w = {pack_bf16(oacc[dt][q4 * 4] * inv, oacc[dt][q4 * 4 + 1] * inv),
-                           pack_bf16(oacc[dt][q4 * 4 + 2] * inv, oacc[dt][q4 * 4 + 3] * inv)};
-        *reinterpret_cast<u32x2_t *>(o + dt * 32 + q4 * 8) = w;
-      }
-    if (p.lse && hf == 0)
-      p.lse[q_tok * (p.n_kv_heads * p.group) + q_head] = l == 0.f ? -INFINITY : (mb + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-  } else {
-    const int64_t at = part * p.part_rows + q_tok * (p.n_kv_heads * p.group) + q_head;
-    float *o = p.part_o + at * D + hf * 4;
-#pragma unroll
-    for (int dt = 0; dt < G::DT; ++dt)
-#pragma unroll
-      for (int q4 = 0; q4 < 4; ++q4)
-        *reinterpret_cast<f32x4_t *>(o + dt * 32 + q4 * 8) = f32x4_t{oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]};
-    if (hf == 0) *reinterpret_cast<f32x2_t *>(p.part_ml + at * 2) = f32x2_t{l == 0.f ? -INFINITY : mb, l};
-  }
+    for (int q4 = 0; q4 < 4; ++q4) {
+      const float o4[4] = {oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]};
+      write_row<4>(p, it, me, D, dt * 32 + q4 * 8 + hf * 4, o4, mb, l, dt == 0 && q4 == 0 && hf == 0);
+    }
 }
 
-// o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a row's parts, m = max m_i.  32 lanes a row.
+template <int D, bool kAligned, typename Groups>
+__global__ __launch_bounds__(kPThreads, 2) void paged_attn_kernel(PagedAttnParams p, Groups groups) {
+  extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+  lds_char *smem = (lds_char *)smem_generic;
+  PagedItem it;
+  if ((int)blockIdx.x < p.prefix_items) {
+    // the row tiles of one range of keys share it: regroup the ids, which go round the 8 XCDs, so that each gets a run of items
+    const uint32_t n = (uint32_t)p.prefix_items, q = n / 8, r = n % 8, x = blockIdx.x % 8;
+    const int id = (int)(x * q + min(x, r) + blockIdx.x / 8);
+    int lo = 0, hi = groups.n;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (groups.item0[mid] <= id) lo = mid; else hi = mid;
+    }
+    it.seq0 = groups.seq0[lo];
+    it.n_rows = groups.members[lo] * p.nq * p.group;
+    const int tile = paged_tile_rows(it.n_rows), n_rt = (it.n_rows + tile - 1) / tile;
+    int rel = id - groups.item0[lo];
+    it.row0 = rel % n_rt * tile;
+    rel /= n_rt;
+    it.part = rel % groups.splits[lo];
+    it.kvh = rel / groups.splits[lo];
+    it.k_lo = it.k0 = it.part * p.chunk;
+    it.k1 = min(groups.prefix[lo], it.k0 + p.chunk);
+  } else {
+    int rel = (int)blockIdx.x - p.prefix_items;
+    it.kvh = rel % p.n_kv_heads;
+    rel /= p.n_kv_heads;
+    it.n_rows = p.nq * p.group;
+    it.row0 = rel % p.own_row_tiles * paged_tile_rows(it.n_rows);
+    rel /= p.own_row_tiles;
+    it.seq0 = rel % p.n_seqs;
+    it.part = rel / p.n_seqs;
+    const int g = group_of(groups, it.seq0), prefix = g < 0 ? 0 : groups.prefix[g];
+    // (cut at multiples of the chunk behind the multiple of 16 that the prefix ends above)
+    it.k0 = prefix / 16 * 16 + it.part * p.own_chunk;
+    it.k1 = min(length_of(p, it.seq0), it.k0 + p.own_chunk);
+    it.k_lo = max(prefix, it.k0);
+    if (g >= 0) it.part += groups.splits[g];
+    if (it.k_lo >= it.k1) {
+      if (!p.direct) return;  // (the merge knows)
+      it.k0 = it.k_lo = it.k1 = 0;
+    }
+  }
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // ---- the item's part of the page table --------------------------------------------------------------------------
+  it.page0 = (int)fast_div((uint32_t)it.k0, p.page_div);
+  it.holes = false;
+  if (it.k1 > it.k0) {
+    const int n_pages = (int)fast_div((uint32_t)(it.k1 - 1), p.page_div) - it.page0 + 1;
+    const int32_t *table = p.page_table + it.seq0 * p.stride_table + it.page0;
+    int bad = 0;
+    for (int i = threadIdx.x; i < n_pages; i += kPThreads) {
+      const int id = table[i];
+      const bool ok = id >= 0 && id < p.n_pages;
+      ((lds_int *)(smem + kTilesB))[i] = ok ? id : -1;
+      bad |= !ok;
+    }
+    it.holes = __syncthreads_or(bad) != 0;
+  }
+  const int rows = it.n_rows - it.row0;
+  if (it.n_rows > kPagedStreamRows) walk_shared<D, kAligned>(p, it, smem, lane, wave);
+  else if (rows > 32) walk_stream<D, kAligned, 3>(p, it, smem, lane, wave);
+  else if (rows > 16) walk_stream<D, kAligned, 2>(p, it, smem, lane, wave);
+  else walk_stream<D, kAligned, 1>(p, it, smem, lane, wave);
+}
+
+// o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a row's parts, m = max m_i: 32 lanes a row, kWays times over (every
+// kWays-th part each).  Their references and sums arrive together, a lane per part, ahead of the outputs.
 constexpr int kMergeThreads = 256;
-template <int D, typename Groups>
+template <int D, int kWays, typename Groups>
 __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnParams p, Groups groups) {
-  constexpr int E = D / 32;
+  constexpr int E = D / 32, kRows = kMergeThreads / 32 / kWays;
   typedef float vec_t __attribute__((ext_vector_type(E)));
-  const int64_t row = (int64_t)blockIdx.x * (kMergeThreads / 32) + threadIdx.x / 32;
-  if (row >= p.part_rows) return;
-  const int lane = threadIdx.x & 31, hq = p.n_kv_heads * p.group;
+  __shared__ float all_ml[kWays][2];
+  __shared__ vec_t all_o[kWays][32];
+  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / 32 / kWays;
+  if (row >= p.part_rows) return;  // (kWays > 1: a workgroup's one row)
+  const int lane = threadIdx.x & 31, way = threadIdx.x / 32 % kWays, hq = p.n_kv_heads * p.group;
   const int tok = (int)(row / hq), head = (int)(row - (int64_t)tok * hq);
   const int seq = (int)fast_div((uint32_t)tok, p.nq_div);
   const int g = group_of(groups, seq);
   const int prefix = g < 0 ? 0 : groups.prefix[g];
-  const int parts = (g < 0 ? 0 : groups.splits[g]) + (max(0, length_of(p, seq) - prefix) + p.chunk - 1) / p.chunk;
+  // (a sequence that ends in its prefix has no part of its own)
+  const int len = length_of(p, seq), own = len > prefix ? (len - prefix / 16 * 16 + p.own_chunk - 1) / p.own_chunk : 0;
+  const int parts = (g < 0 ? 0 : groups.splits[g]) + own;
   float m = -INFINITY, l = 0.f;
   vec_t o;
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < parts; ++i) {
-    const int64_t at = i * p.part_rows + row;
-    const f32x2_t ml = *reinterpret_cast<const f32x2_t *>(p.part_ml + at * 2);
-    const vec_t x = *reinterpret_cast<const vec_t *>(p.part_o + at * D + lane * E);
-    if (ml[1] == 0.f) continue;  // saw nothing
-    const float to = fmaxf(m, ml[0]);
-    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - to), add = __builtin_amdgcn_exp2f(ml[0] - to);
-    m = to;
-    l = l * keep + ml[1] * add;
+  for (int i0 = way; i0 < parts; i0 += 32 * kWays) {
+    const int n = min(32, (parts - i0 + kWays - 1) / kWays);  // parts i0, i0 + kWays, ...
+    f32x2_t ml = {-INFINITY, 0.f};
+    if (lane < n) ml = *reinterpret_cast<const f32x2_t *>(p.part_ml + ((i0 + lane * kWays) * p.part_rows + row) * 2);
+    float top = ml[0];
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = o[e] * keep + x[e] * add;
+    for (int x = 1; x < 32; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
+    const float to = fmaxf(m, top);
+    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - to);
+    const float w = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - to);  // (a part that saw nothing)
+    float add = ml[1] * w;
+#pragma unroll
+    for (int x = 1; x < 32; x *= 2) add += __shfl_xor(add, x);
+    m = to;
+    l = l * keep + add;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= keep;
+    const float *from = p.part_o + (i0 * p.part_rows + row) * D + lane * E;
+    constexpr int kAhead = 8;
+    for (int i = 0; i < n; i += kAhead) {
+      vec_t x[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) x[u] = *reinterpret_cast<const vec_t *>(from + min(i + u, n - 1) * (kWays * p.part_rows * D));
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const float wi = __shfl(w, i + u, 32);  // (lanes without a part: zero)
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += wi == 0.f ? 0.f : x[u][e] * wi;
+      }
+    }
+  }
+  if constexpr (kWays > 1) {
+    all_o[way][lane] = o;
+    if (lane == 0) all_ml[way][0] = m, all_ml[way][1] = l;
+    __syncthreads();
+    if (way) return;
+#pragma unroll
+    for (int w = 1; w < kWays; ++w) m = fmaxf(m, all_ml[w][0]);
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWays; ++w) {
+      const float f = all_ml[w][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(all_ml[w][0] - m);
+      l += all_ml[w][1] * f;
+      const vec_t x = all_o[w][lane];
+#pragma unroll
+      for (int e = 0; e < E; ++e) o[e] += x[e] * f;
+    }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   uint32_t w[E / 2];
@@ -384,22 +719,42 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnPar
   if (p.lse && lane == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
+template <int D, bool kAligned, typename Groups>
+hipError_t launch_attn_a(const PagedAttnParams &p, const Groups &g, unsigned items, size_t lds, hipStream_t stream) {
+  // (a launch of more than 64 KB of LDS has to be allowed first, on every device)
+  static std::atomic<bool> told[16];
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev >= 16 || !told[dev].load(std::memory_order_acquire)) {
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attn_kernel<D, kAligned, Groups>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            kTilesB + (kPagedMaxChunk + 2) * 4);
+    if (e != hipSuccess) return e;
+    if (dev < 16) told[dev].store(true, std::memory_order_release);
+  }
+  paged_attn_kernel<D, kAligned, Groups><<<items, kPThreads, lds, stream>>>(p, g);
+  return hipGetLastError();
+}
 template <int D, typename Groups>
 hipError_t launch_attn_d(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
   const int64_t items = p.prefix_items + (int64_t)p.n_seqs * p.n_kv_heads * p.own_row_tiles * p.own_splits;
-  if (items < 1 || items > 0x7fffffff || p.chunk > kPagedMaxChunk) return hipErrorInvalidValue;
-  const size_t lds = PGeo<D>::TABLE + (size_t)(p.chunk / p.page_rows + 2) * 4;  // (a range may begin and end inside a page)
-  static_assert(PGeo<D>::TABLE + (kPagedMaxChunk + 2) * 4 <= 65536, "as much as a launch may ask for without further ado");
-  paged_attn_kernel<D, Groups><<<(unsigned)items, kPThreads, lds, stream>>>(p, g);
+  const int32_t chunk = std::max(p.chunk, p.own_chunk);
+  if (items < 1 || items > 0x7fffffff || chunk > kPagedMaxChunk) return hipErrorInvalidValue;
+  const size_t lds = kTilesB + (size_t)(chunk / p.page_rows + 2) * 4;  // (a range may begin and end inside a page)
+  static_assert(2 * (kTilesB + (kPagedMaxChunk + 2) * 4) <= 160 * 1024, "two workgroups a compute unit");
+  return p.page_rows % 16 == 0 ? launch_attn_a<D, true>(p, g, (unsigned)items, lds, stream) : launch_attn_a<D, false>(p, g, (unsigned)items, lds, stream);
+}
+template <int D, int kWays, typename Groups>
+hipError_t launch_merge_w(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
+  constexpr int kRows = kMergeThreads / 32 / kWays;
+  const int64_t wgs = (p.part_rows + kRows - 1) / kRows;
+  if (wgs < 1 || wgs > 0x7fffffff) return hipErrorInvalidValue;
+  paged_merge_kernel<D, kWays, Groups><<<(unsigned)wgs, kMergeThreads, 0, stream>>>(p, g);
   return hipGetLastError();
 }
 template <int D, typename Groups>
 hipError_t launch_merge_d(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
-  constexpr int kRows = kMergeThreads / 32;
-  const int64_t wgs = (p.part_rows + kRows - 1) / kRows;
-  if (wgs < 1 || wgs > 0x7fffffff) return hipErrorInvalidValue;
-  paged_merge_kernel<D, Groups><<<(unsigned)wgs, kMergeThreads, 0, stream>>>(p, g);
-  return hipGetLastError();
+  return p.max_parts > 8 ? launch_merge_w<D, 8>(p, g, stream) : launch_merge_w<D, 1>(p, g, stream);
 }
 
 }  // namespace
