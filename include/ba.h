@@ -392,8 +392,8 @@ size_t ba_block_attention_prompts_backward_workspace_bytes(const ba_heads *heads
  * positions: DEVICE, n_tokens ints, null -> a token's number.
  */
 typedef struct ba_head_norm {
-  const void *q_weight; /* device, [head_dim], nullable -> ones */
-  const void *k_weight; /* device, [head_dim], nullable -> ones */
+  const void *q_weight; /* device, [head_dim], 16-byte aligned, nullable -> ones */
+  const void *k_weight; /* the same                              */
   int32_t dtype;        /* BA_DTYPE_* of the gains               */
   float eps;            /* > 0                                   */
 } ba_head_norm;

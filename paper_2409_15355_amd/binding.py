@@ -68,6 +68,14 @@ class BaPagedCache(ctypes.Structure):
                 ("stride_table", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
 
 
+class _KnownNorm(ctypes.Structure):  # (as the native half of this face reads them)
+    _fields_ = [("norm", BaHeadNorm), ("head_dim", ctypes.c_int32)]
+
+
+class _KnownCache(ctypes.Structure):
+    _fields_ = [("cache", BaPagedCache), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
 class BaError(RuntimeError):
     def __init__(self, status: int, name: str, detail: str):
         super().__init__(f"{name} ({status}): {detail}")
@@ -205,6 +213,8 @@ def _load_native(lib):
                             tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in
                                   ("ba_encode_blocks", "ba_reencode_positions", "ba_final_block_attention", "ba_final_block_attention_static",
                                    "ba_final_block_attention_cached", "ba_block_attention_prompts", "ba_block_attention_prompts_backward")))
+                _face.setup_paged(HeadNorm, PagedCache, tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in
+                                                              ("ba_norm_rotate", "ba_norm_rotate_backward", "ba_paged_append", "ba_paged_attention")))
                 return _face
             why = f"it was built for torch {built_for}, this is {torch.__version__}"
     import warnings
@@ -268,13 +278,17 @@ class HeadNorm:
                 raise ValueError("q_weight and k_weight: one dtype for both")
             dtype = w.dtype
         self.q_weight, self.k_weight, self.eps = q_weight, k_weight, float(eps)
-        self.c = BaHeadNorm(None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
-                            DTYPE_F32 if dtype is None or dtype == torch.float32 else DTYPE_BF16, self.eps)
+        sizes = {int(w.shape[0]) for w in (q_weight, k_weight) if w is not None}
+        if len(sizes) > 1:
+            raise ValueError("q_weight and k_weight: one head_dim for both")
+        self.known = _KnownNorm(BaHeadNorm(None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
+                                           DTYPE_F32 if dtype is None or dtype == torch.float32 else DTYPE_BF16, self.eps),
+                                sizes.pop() if sizes else 0)
+        self.c = self.known.norm
 
     def _check(self, head_dim: int) -> None:
-        for name, w in (("q_weight", self.q_weight), ("k_weight", self.k_weight)):
-            if w is not None and w.shape[0] != head_dim:
-                raise ValueError(f"{name}: {w.shape[0]} gains, the call's head description says {head_dim}")
+        if self.known.head_dim not in (0, head_dim):
+            raise ValueError(f"norm: {self.known.head_dim} gains, the call's head description says {head_dim}")
 
 
 class PagedCache:
@@ -297,8 +311,9 @@ class PagedCache:
         self.n_seqs, max_pages = page_table.shape
         k, v = (_tensor(t, name, layers=True) for name, t in (("k_pages", k_pages), ("v_pages", v_pages)))
         self.max_rows = max_pages * rows
-        self.c = BaPagedCache(k, v, k_pages.stride(0), v_pages.stride(0), n_pages, rows, page_table.data_ptr(), page_table.stride(0),
-                              self.n_seqs, max_pages)
+        self.known = _KnownCache(BaPagedCache(k, v, k_pages.stride(0), v_pages.stride(0), n_pages, rows, page_table.data_ptr(),
+                                              page_table.stride(0), self.n_seqs, max_pages), self.n_kv_heads, self.head_dim)
+        self.c = self.known.cache
 
     def _check(self, heads: "Heads") -> None:
         if (self.n_kv_heads, self.head_dim) != (heads.n_kv_heads, heads.head_dim):
@@ -642,6 +657,8 @@ def _tokens_of(*tensors) -> int:
 
 def ba_norm_rotate(heads: Heads, norm: HeadNorm, q, k, q_out, k_out, positions=None, rope_mode: int = ROPE_APPLY, stream=None) -> None:
     """All tokens of ``q`` and ``k`` (either may be None); positions: int32 on the GPU."""
+    if _done(_face().norm_rotate(heads, q, k, q_out, k_out, positions, norm, rope_mode, stream)):
+        return
     norm._check(heads.head_dim)
     n = _tokens_of(q, k)
     tq, tk = (_tensor(t, name, h, heads.head_dim, n, allow_f32=True) for t, name, h in ((q, "q", heads.n_q_heads), (k, "k", heads.n_kv_heads)))
@@ -657,6 +674,8 @@ def ba_norm_rotate_backward_workspace_bytes(heads: Heads, n_tokens: int) -> int:
 
 def ba_norm_rotate_backward(heads: Heads, norm: HeadNorm, q, k, d_q_out, d_k_out, dq, dk, dq_weight=None, dk_weight=None, positions=None,
                             rope_mode: int = ROPE_APPLY, ws=None, stream=None) -> None:
+    if _done(_face().norm_rotate_backward(heads, q, k, d_q_out, d_k_out, dq, dk, dq_weight, dk_weight, positions, norm, rope_mode, ws, stream)):
+        return
     norm._check(heads.head_dim)
     n, d = _tokens_of(q, k), heads.head_dim
     of = [_tensor(t, name, heads.n_q_heads if "q" in name else heads.n_kv_heads, d, n, allow_f32=True)
@@ -670,6 +689,8 @@ def ba_norm_rotate_backward(heads: Heads, norm: HeadNorm, q, k, d_q_out, d_k_out
 def ba_paged_append(heads: Heads, norm: Optional[HeadNorm], cache: PagedCache, q, k, v, q_out, cache_pos, seq_of_token=None, rope_pos=None,
                     rope_mode: int = ROPE_APPLY, stream=None) -> None:
     """All tokens of ``k``; cache_pos, seq_of_token, rope_pos: int32 on the GPU."""
+    if _done(_face().paged_append(heads, q, k, v, q_out, cache_pos, seq_of_token, rope_pos, norm, cache, rope_mode, stream)):
+        return
     cache._check(heads)
     if norm is not None:
         norm._check(heads.head_dim)
@@ -699,6 +720,8 @@ def _n_groups(cu, pre) -> int:
 def ba_paged_attention(heads: Heads, cache: PagedCache, q, o_out, lse_out, seq_len, max_len: int, cu_group=None, prefix_len=None,
                        q_per_seq: int = 1, ws=None, stream=None) -> None:
     """seq_len: int32 on the GPU, at most max_len; cu_group, prefix_len: host arrays (None: nothing is shared)."""
+    if _done(_face().paged_attention(heads, q, o_out, lse_out, seq_len, cu_group, prefix_len, cache, max_len, q_per_seq, ws, stream)):
+        return
     cache._check(heads)
     n = cache.n_seqs * q_per_seq
     cu, pre = _ints(cu_group), _ints(prefix_len)

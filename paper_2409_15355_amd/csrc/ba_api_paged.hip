@@ -45,8 +45,7 @@ bool same_place(const ba_tensor *a, const ba_tensor *b) {
 int32_t check_norm(const ba_head_norm *n) {
   if (n->dtype != BA_DTYPE_BF16 && n->dtype != BA_DTYPE_F32) return fail(BA_ERR_UNSUPPORTED, "norm: dtype %d of the gains not supported", n->dtype);
   if (!(n->eps > 0.f) || !std::isfinite(n->eps)) return fail(BA_ERR_INVALID_ARG, "norm: eps must be positive");
-  const uintptr_t mask = elt_size(n->dtype) - 1;
-  if (((uintptr_t)n->q_weight & mask) || ((uintptr_t)n->k_weight & mask)) return fail(BA_ERR_ALIGNMENT, "norm: gains not aligned to their type");
+  if (((uintptr_t)n->q_weight | (uintptr_t)n->k_weight) & 15) return fail(BA_ERR_ALIGNMENT, "norm: gains must be 16-byte aligned");
   return BA_OK;
 }
 int32_t check_rope_mode(int32_t rope_mode) {
@@ -111,6 +110,8 @@ int32_t check_cache(const ba_paged_cache *c, const ba_heads *h) {
   if (c->n_seqs < 0 || c->max_pages < 0) return fail(BA_ERR_INVALID_ARG, "cache: negative sequence or page count");
   if (((c->k_stride_page | c->v_stride_page) * 2) & 15) return fail(BA_ERR_ALIGNMENT, "cache: page strides must be 16-byte aligned");
   if (c->k_stride_page < 0 || c->v_stride_page < 0) return fail(BA_ERR_INVALID_ARG, "cache: negative page stride");
+  if (std::max(c->k_stride_page, c->v_stride_page) >= (int64_t)1 << 35)  // (counted in 32-bit units of 16 bytes)
+    return fail(BA_ERR_UNSUPPORTED, "cache: pages of 64 GB and more");
   if (c->n_seqs > 0 && c->max_pages > 0) {
     if (!c->page_table) return fail(BA_ERR_INVALID_ARG, "page_table: null");
     if (c->stride_table < 0 || (c->n_seqs > 1 && c->stride_table < c->max_pages))
@@ -422,7 +423,7 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
     p.lse = lse_out ? lse_out + tok0 * heads->n_q_heads : nullptr;
     p.k = (const uint16_t *)cache->k.ptr, p.v = (const uint16_t *)cache->v.ptr;
     p.k_sh = cache->k.stride_head, p.v_sh = cache->v.stride_head;
-    p.k_page_b = cache->k_stride_page * 2, p.v_page_b = cache->v_stride_page * 2;
+    p.k_page_b16 = (uint32_t)(cache->k_stride_page / 8), p.v_page_b16 = (uint32_t)(cache->v_stride_page / 8);
     p.k_rb = (uint32_t)cache->k.stride_tok * 2, p.v_rb = (uint32_t)cache->v.stride_tok * 2;
     p.page_table = cache->page_table + (int64_t)pl.seq0 * cache->stride_table;
     p.stride_table = cache->stride_table;

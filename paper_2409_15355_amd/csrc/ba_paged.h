@@ -57,7 +57,7 @@ struct PagedAttnParams {
   float *lse;  // [tokens][query heads], nullable
   const uint16_t *k, *v;
   int64_t k_sh, v_sh;          // head strides, elements
-  int64_t k_page_b, v_page_b;  // bytes from page to page
+  uint32_t k_page_b16, v_page_b16;  // from page to page, in units of 16 bytes
   uint32_t k_rb, v_rb;         // bytes from row to row
   const int32_t *page_table;
   int64_t stride_table;

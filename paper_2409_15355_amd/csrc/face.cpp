@@ -36,8 +36,14 @@ struct {
   decltype(&ba_block_attention_prompts) prompts;
   decltype(&ba_block_attention_prompts_backward) prompts_backward;
 } lib;
-PyTypeObject *heads_type;
-PyObject *name_c, *name_cuda_stream, *get_device, *get_raw_stream;
+struct {
+  decltype(&ba_norm_rotate) norm_rotate;
+  decltype(&ba_norm_rotate_backward) norm_rotate_backward;
+  decltype(&ba_paged_append) paged_append;
+  decltype(&ba_paged_attention) paged_attention;
+} paged;
+PyTypeObject *heads_type, *norm_type, *cache_type;
+PyObject *name_c, *name_known, *name_cuda_stream, *get_device, *get_raw_stream;
 
 // Arguments that are not the plain case.
 struct Declined {};
@@ -45,25 +51,45 @@ void need(bool ok) {
   if (!ok) throw Declined();
 }
 
-// The ba_heads inside a Heads object, held for the call.
-struct HeadsArg {
+// The structure that an object of a known type keeps in an attribute, held for the call.
+template <typename T>
+struct Held {
   Py_buffer view{};
-  const ba_heads *h = nullptr;
-  explicit HeadsArg(PyObject *o) {
-    need(Py_TYPE(o) == heads_type);
-    PyObject *c = PyObject_GetAttr(o, name_c);
+  const T *h = nullptr;
+  Held(PyObject *o, PyTypeObject *type, PyObject *attribute) {
+    need(Py_TYPE(o) == type);
+    PyObject *c = PyObject_GetAttr(o, attribute);
     need(c != nullptr);
     const int rc = PyObject_GetBuffer(c, &view, PyBUF_SIMPLE);  // (the view holds a reference of its own)
     Py_DECREF(c);
     need(rc == 0);
-    if (view.len != (Py_ssize_t)sizeof(ba_heads)) {
+    if (view.len != (Py_ssize_t)sizeof(T)) {
       PyBuffer_Release(&view);
       throw Declined();
     }
-    h = (const ba_heads *)view.buf;
+    h = (const T *)view.buf;
   }
-  ~HeadsArg() { PyBuffer_Release(&view); }
-  HeadsArg(const HeadsArg &) = delete;
+  ~Held() { PyBuffer_Release(&view); }
+  Held(const Held &) = delete;
+};
+// The ba_heads inside a Heads object.
+struct HeadsArg : Held<ba_heads> {
+  explicit HeadsArg(PyObject *o) : Held(o, heads_type, name_c) {}
+};
+// What a HeadNorm and a PagedCache know, the sizes that the library's structures do not have among them.
+struct KnownNorm {
+  ba_head_norm norm;
+  int32_t head_dim;  // 0: no gains
+};
+struct KnownCache {
+  ba_paged_cache cache;
+  int32_t n_kv_heads, head_dim;
+};
+struct NormArg : Held<KnownNorm> {
+  NormArg(PyObject *o, int64_t d) : Held(o, norm_type, name_known) { need(!h->head_dim || h->head_dim == d); }
+};
+struct CacheArg : Held<KnownCache> {
+  CacheArg(PyObject *o, const ba_heads *heads) : Held(o, cache_type, name_known) { need(h->n_kv_heads == heads->n_kv_heads && h->head_dim == heads->head_dim); }
 };
 
 bool is_int32_array(PyObject *o) {
@@ -143,6 +169,24 @@ float *lse_of(PyObject *o, int64_t tokens, int64_t n_q_heads) {
   const at::Tensor &x = plain_tensor(o);
   need(x.scalar_type() == at::kFloat && x.dim() == 2 && x.is_contiguous() && x.size(1) == n_q_heads && x.size(0) >= tokens);
   return (float *)x.data_ptr();
+}
+// at least n integers, or floats, in GPU memory
+template <typename T>
+T *device_array(PyObject *o, at::ScalarType type, int64_t n) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor &x = plain_tensor(o);
+  need(x.scalar_type() == type && x.dim() == 1 && x.is_contiguous() && x.size(0) >= n);
+  return (T *)x.data_ptr();
+}
+float *gain_grad(PyObject *o, int64_t d) {
+  need(o == Py_None || plain_tensor(o).numel() == d);
+  return device_array<float>(o, at::kFloat, d);
+}
+int64_t tokens_of(PyObject *q, PyObject *k) {
+  need(q != Py_None || k != Py_None);
+  const at::Tensor &x = plain_tensor(q != Py_None ? q : k);
+  need(x.dim() == 3 && x.size(0) <= INT32_MAX);
+  return x.size(0);
 }
 struct Workspace {
   void *p = nullptr;
@@ -336,6 +380,76 @@ PyObject *prompts_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// (arguments in another order than the Python functions': tensors, integer arrays, the rest)
+PyObject *norm_rotate(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 9, 5, 5, [&] {
+    const HeadsArg h(a[0]);
+    const int64_t T = tokens_of(a[1], a[2]), hq = h.h->n_q_heads, hkv = h.h->n_kv_heads, d = h.h->head_dim;
+    const TensorArg q(a[1], hq, d, T, true), k(a[2], hkv, d, T, true), qo(a[3], hq, d, T, true), ko(a[4], hkv, d, T, true);
+    const int32_t *const at = device_array<int32_t>(a[5], at::kInt, T);
+    const NormArg norm(a[6], d);
+    const int32_t mode = int_of(a[7]);
+    void *const stream = stream_of(a[8]);
+    return unlocked([&] { return paged.norm_rotate(h.h, &norm.h->norm, q.p, k.p, qo.p, ko.p, (int32_t)T, at, mode, stream); });
+  });
+}
+
+PyObject *norm_rotate_backward(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 14, 9, 9, [&] {
+    const HeadsArg h(a[0]);
+    const int64_t T = tokens_of(a[1], a[2]), hq = h.h->n_q_heads, hkv = h.h->n_kv_heads, d = h.h->head_dim;
+    const TensorArg q(a[1], hq, d, T, true), k(a[2], hkv, d, T, true), gq(a[3], hq, d, T, true), gk(a[4], hkv, d, T, true),
+        dq(a[5], hq, d, T, true), dk(a[6], hkv, d, T, true);
+    float *const dwq = gain_grad(a[7], d), *const dwk = gain_grad(a[8], d);
+    const int32_t *const at = device_array<int32_t>(a[9], at::kInt, T);
+    const NormArg norm(a[10], d);
+    const int32_t mode = int_of(a[11]);
+    const Workspace ws(a[12]);
+    void *const stream = stream_of(a[13]);
+    return unlocked([&] {
+      return paged.norm_rotate_backward(h.h, &norm.h->norm, q.p, k.p, gq.p, gk.p, dq.p, dk.p, dwq, dwk, (int32_t)T, at, mode, ws.p, ws.bytes, stream);
+    });
+  });
+}
+
+PyObject *paged_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 12, 7, 7, [&] {
+    const HeadsArg h(a[0]);
+    const int64_t T = tokens_of(a[2], a[2]), hq = h.h->n_q_heads, hkv = h.h->n_kv_heads, d = h.h->head_dim;
+    const TensorArg q(a[1], hq, d, T), k(a[2], hkv, d, T), v(a[3], hkv, d, T), qo(a[4], hq, d, T);
+    const int32_t *const at = device_array<int32_t>(a[5], at::kInt, T), *const seq = device_array<int32_t>(a[6], at::kInt, T),
+                         *const pos = device_array<int32_t>(a[7], at::kInt, T);
+    const CacheArg cache(a[9], h.h);
+    const int32_t mode = int_of(a[10]);
+    void *const stream = stream_of(a[11]);
+    auto call = [&](const ba_head_norm *norm) {
+      return unlocked([&] { return paged.paged_append(h.h, norm, &cache.h->cache, q.p, k.p, v.p, qo.p, (int32_t)T, at, seq, pos, mode, stream); });
+    };
+    if (a[8] == Py_None) return call(nullptr);
+    const NormArg norm(a[8], d);
+    return call(&norm.h->norm);
+  });
+}
+
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 12, 4, 6, [&] {
+    const HeadsArg h(a[0]);
+    const CacheArg cache(a[7], h.h);
+    const Ints cu(a[5]), prefix(a[6]);
+    need(!cu.p == !prefix.p && (!cu.p || cu.n == prefix.n + 1));
+    const int32_t max_len = int_of(a[8]), nq = int_of(a[9]);
+    const int64_t seqs = cache.h->cache.n_seqs, T = seqs * std::max(nq, 0), hq = h.h->n_q_heads, d = h.h->head_dim;
+    const TensorArg q(a[1], hq, d, T), o(a[2], hq, d, T);
+    float *const lse = lse_of(a[3], T, hq);
+    const int32_t *const len = device_array<int32_t>(a[4], at::kInt, seqs);
+    const Workspace ws(a[10]);
+    void *const stream = stream_of(a[11]);
+    return unlocked([&] {
+      return paged.paged_attention(h.h, &cache.h->cache, q.p, o.p, lse, nq, len, max_len, (int32_t)prefix.n, cu.p, prefix.p, ws.p, ws.bytes, stream);
+    });
+  });
+}
+
 // setup(Heads class, current_device(), raw_stream(device) or None, addresses of the entry points in the order of `lib`)
 PyObject *setup(PyObject *, PyObject *args) {
   PyObject *type, *dev, *raw;
@@ -352,8 +466,24 @@ PyObject *setup(PyObject *, PyObject *args) {
   Py_RETURN_NONE;
 }
 
+// setup_paged(HeadNorm class, PagedCache class, addresses of the entry points in the order of `paged`)
+PyObject *setup_paged(PyObject *, PyObject *args) {
+  PyObject *norm, *cache;
+  unsigned long long at[4];
+  if (!PyArg_ParseTuple(args, "O!O!(KKKK)", &PyType_Type, &norm, &PyType_Type, &cache, at, at + 1, at + 2, at + 3)) return nullptr;
+  Py_INCREF(norm), Py_INCREF(cache);
+  norm_type = (PyTypeObject *)norm;
+  cache_type = (PyTypeObject *)cache;
+  static_assert(sizeof(paged) == 4 * sizeof(void *), "an address each");
+  void *p[4];
+  for (int i = 0; i < 4; ++i) p[i] = (void *)(uintptr_t)at[i];
+  memcpy(&paged, p, sizeof(paged));
+  Py_RETURN_NONE;
+}
+
 #define FAST(name, fn) {name, (PyCFunction)(void (*)(void))(fn), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, nullptr},
+                         {"setup_paged", setup_paged, METH_VARARGS, nullptr},
                          FAST("encode_blocks", encode_blocks),
                          FAST("reencode_positions", reencode_positions),
                          FAST("final_block", final_block<false>),
@@ -361,6 +491,10 @@ PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, nullptr},
                          FAST("final_block_cached", final_block_cached),
                          FAST("prompts", prompts),
                          FAST("prompts_backward", prompts_backward),
+                         FAST("norm_rotate", norm_rotate),
+                         FAST("norm_rotate_backward", norm_rotate_backward),
+                         FAST("paged_append", paged_append),
+                         FAST("paged_attention", paged_attention),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_face", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -369,8 +503,9 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_face", nullptr, -1, methods, null
 PyMODINIT_FUNC PyInit__face() {
   import_array();
   name_c = PyUnicode_InternFromString("c");
+  name_known = PyUnicode_InternFromString("known");
   name_cuda_stream = PyUnicode_InternFromString("cuda_stream");
-  if (!name_c || !name_cuda_stream) return nullptr;
+  if (!name_c || !name_known || !name_cuda_stream) return nullptr;
   PyObject *m = PyModule_Create(&module);
   if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) Py_CLEAR(m);
   return m;

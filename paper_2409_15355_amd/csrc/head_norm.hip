@@ -8,6 +8,7 @@
 // back in small ones.  The 16-byte pieces c and c + CH / 2 of a vector belong to one lane, so that either pairing of the rotation
 // stays inside a lane, and the sum of squares is three or four adds of neighbouring lanes.  A lane meets the heads of one token
 // one after the other, so cos and sin (some 40 operations a pair) are worked out once for all of them.
+#include <algorithm>
 #include <type_traits>
 
 #include "ba_lds.h"
@@ -17,6 +18,7 @@
 namespace ba {
 namespace {
 
+constexpr int kManySlots = 4, kFewSlots = 16;
 // kSlots: heads of a token that a workgroup takes at a time
 template <typename T, int D, int kSlots>
 struct RowGeo {
@@ -28,14 +30,15 @@ struct RowGeo {
   static_assert(TOK >= 1, "a token's lanes fit a workgroup");
 };
 
-// cos and sin of a lane's VEC pairs: in its two pieces one after the other (interleaved), or of its first with its second (half)
+// a lane's VEC pairs: in its two pieces one after the other (interleaved), or of its first with its second (half)
+template <int VEC, int CH, int LAYOUT>
+__device__ __forceinline__ int lane_pair(int c, int e) {
+  return LAYOUT == 0 ? (e < VEC / 2 ? c * (VEC / 2) + e : (c + CH / 2) * (VEC / 2) + (e - VEC / 2)) : c * VEC + e;
+}
 template <int VEC, int CH, int LAYOUT>
 __device__ __forceinline__ void lane_turns(const RopeTable &rt, int c, int pos, float (&cs)[VEC], float (&sn)[VEC]) {
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    const int j = LAYOUT == 0 ? (e < VEC / 2 ? c * (VEC / 2) + e : (c + CH / 2) * (VEC / 2) + (e - VEC / 2)) : c * VEC + e;
-    sincos_phase(rope_phase(pos, rt.turns[j]), cs[e], sn[e]);
-  }
+  for (int e = 0; e < VEC; ++e) sincos_phase(rope_phase(pos, rt.turns[lane_pair<VEC, CH, LAYOUT>(c, e)]), cs[e], sn[e]);
 }
 template <int VEC, int LAYOUT>
 __device__ __forceinline__ void turn_pieces(float (&x)[VEC], float (&y)[VEC], const float (&cs)[VEC], const float (&sn)[VEC]) {
@@ -50,91 +53,171 @@ __device__ __forceinline__ void turn_pieces(float (&x)[VEC], float (&y)[VEC], co
     for (int e = 0; e < VEC; ++e) rotate(x[e], y[e], cs[e], sn[e]);
   }
 }
+// a lane's gains
 template <int VEC, int CH>
 __device__ __forceinline__ void lane_gains(const void *w, bool f32, int c, float (&wx)[VEC], float (&wy)[VEC]) {
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    const int a = c * VEC + e, b = (c + CH / 2) * VEC + e;
+  auto piece = [&](int at, float (&to)[VEC]) __attribute__((always_inline)) {
     if (!w) {
-      wx[e] = wy[e] = 1.f;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) to[e] = 1.f;
     } else if (f32) {
-      wx[e] = ((const float *)w)[a];
-      wy[e] = ((const float *)w)[b];
+#pragma unroll
+      for (int e = 0; e < VEC; e += 4) {
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>((const float *)w + at + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[e + i] = x[i];
+      }
     } else {
-      wx[e] = bf16_lo(((const uint16_t *)w)[a]);
-      wy[e] = bf16_lo(((const uint16_t *)w)[b]);
+#pragma unroll
+      for (int e = 0; e < VEC; e += 4) {
+        const u32x2_t x = *reinterpret_cast<const u32x2_t *>((const uint16_t *)w + at + e);
+        to[e] = bf16_lo(x[0]), to[e + 1] = bf16_hi(x[0]), to[e + 2] = bf16_lo(x[1]), to[e + 3] = bf16_hi(x[1]);
+      }
+    }
+  };
+  piece(c * VEC, wx);
+  piece((c + CH / 2) * VEC, wy);
+}
+
+// The row of the paged cache that a token's keys and values go to.
+struct CacheRow {
+  bool kept;  // there is one
+  int64_t page;
+  int row;
+};
+__device__ __forceinline__ CacheRow cache_row(const HeadRowsParams &p, int t) {
+  CacheRow r = {false, 0, 0};
+  const int seq = p.seq_of_token ? p.seq_of_token[t] : t, at = p.cache_pos[t];
+  if (seq >= 0 && seq < p.n_seqs && at >= 0 && at < p.max_rows) {
+    const uint32_t i = fast_div((uint32_t)at, p.page_div);
+    r.row = at - (int)i * p.page_rows;
+    r.page = p.page_table[seq * p.stride_table + i];
+    r.kept = r.page >= 0 && r.page < p.n_pages;
+  }
+  return r;
+}
+
+// A few heads of one tensor and token on their way: kBatch of them in flight per lane.
+template <typename T, int D, int LAYOUT, bool kPaged>
+struct HeadRows {
+  static constexpr int kBatch = 4;
+  typedef Chunk<T, false, false> Ch;
+  static constexpr int VEC = Ch::VEC, CH = D / VEC, TPV = CH / 2;
+  const HeadRowsParams &p;
+  int kind, c, n;
+  const T *src;
+  bool norm, turn;
+  float wx[VEC], wy[VEC];
+  Ch x[kBatch], y[kBatch];
+  __device__ __forceinline__ HeadRows(const HeadRowsParams &p_, int kind_, int c_, int t)
+      : p(p_), kind(kind_), c(c_), n(p_.n_heads[kind_]), src((const T *)p_.src[kind_] + t * p_.src_st[kind_] + c_ * VEC),
+        norm(kind_ != kRowsV && p_.eps >= 0.f), turn(kind_ != kRowsV && p_.rope) {}
+  __device__ __forceinline__ void gains() {
+    if (norm) lane_gains<VEC, CH>(p.weight[kind], p.weight_f32, c, wx, wy);
+  }
+  __device__ __forceinline__ void load(int h0, int step) {
+    const int64_t sh = p.src_sh[kind];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int h = min(h0 + u * step, n - 1);
+      x[u].load(src + h * sh);
+      y[u].load(src + h * sh + (CH / 2) * VEC);
+    }
+  }
+  __device__ __forceinline__ T *target(int t, const CacheRow &to) const {
+    T *dst = (T *)p.dst[kind] + c * VEC;
+    return dst + (kPaged && kind != kRowsQ ? to.page * p.dst_page[kind] + to.row * p.dst_st[kind] : t * p.dst_st[kind]);
+  }
+  __device__ __forceinline__ void store(T *dst, int h0, int step, const float (&cs)[VEC], const float (&sn)[VEC]) {
+    const int64_t sh = p.dst_sh[kind];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int h = h0 + u * step;
+      if (h >= n) break;
+      if (norm) {
+        float ss = 0.f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) ss += x[u].f[e] * x[u].f[e] + y[u].f[e] * y[u].f[e];
+        const float r = rsqrtf(sum_over_lanes<TPV>(ss) * (1.0f / D) + p.eps);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          x[u].f[e] *= r * wx[e];
+          y[u].f[e] *= r * wy[e];
+        }
+      }
+      if (turn) turn_pieces<VEC, LAYOUT>(x[u].f, y[u].f, cs, sn);
+      x[u].store(dst + h * sh);
+      y[u].store(dst + h * sh + (CH / 2) * VEC);
+    }
+  }
+};
+
+// Calls that fill the chip: a lane takes every fourth head of a token's tensors, one tensor after the other.
+// kPaged: keys and values go to their rows of a paged cache.
+template <typename T, int D, int LAYOUT, bool kPaged>
+__global__ __launch_bounds__(kRotThreads) void head_rows_kernel(HeadRowsParams p, RopeTable rt) {
+  using G = RowGeo<T, D, kManySlots>;
+  using Rows = HeadRows<T, D, LAYOUT, kPaged>;
+  const int c = threadIdx.x % G::TPV, slot = threadIdx.x / G::TPV % kManySlots;
+  const int t = blockIdx.x * G::TOK + threadIdx.x / G::TPT;
+  if (t >= p.n_tokens) return;
+  float cs[G::VEC], sn[G::VEC];
+  if (p.rope) lane_turns<G::VEC, G::CH, LAYOUT>(rt, c, p.positions ? p.positions[t] : t, cs, sn);
+  CacheRow to = {};
+  if constexpr (kPaged) to = cache_row(p, t);
+#pragma unroll 1
+  for (int kind = 0; kind < (kPaged ? 3 : 2); ++kind) {
+    if (!p.src[kind] || (kPaged && kind != kRowsQ && !to.kept)) continue;
+    Rows rows(p, kind, c, t);
+    rows.gains();
+    T *dst = rows.target(t, to);
+#pragma unroll 1
+    for (int h0 = slot; h0 < rows.n; h0 += kManySlots * Rows::kBatch) {
+      rows.load(h0, kManySlots);
+      rows.store(dst, h0, kManySlots, cs, sn);
     }
   }
 }
 
-// kPaged: keys and values go to their rows of a paged cache.  gridDim.y: one workgroup for all of a token's tensors, or one each.
-template <typename T, int D, int LAYOUT, int kSlots, bool kPaged>
-__global__ __launch_bounds__(kRotThreads) void head_rows_kernel(HeadRowsParams p, RopeTable rt) {
-  using G = RowGeo<T, D, kSlots>;
-  typedef Chunk<T, false, false> Ch;
-  constexpr int VEC = G::VEC, CH = G::CH;
-  constexpr int kBatch = 4;  // heads in flight per lane
-  const int c = threadIdx.x % G::TPV, slot = threadIdx.x / G::TPV % kSlots;
-  const int t = blockIdx.x * G::TOK + threadIdx.x / G::TPT;
-  if (t >= p.n_tokens) return;
-
+// Calls bound by the way to memory and back: a workgroup per tensor (blockIdx.y) and token or two, all of its loads ahead of
+// everything else; cos and sin are worked out once for the token's heads, a pair or less to a lane.
+template <typename T, int D, int LAYOUT, bool kPaged>
+__global__ __launch_bounds__(kRotThreads) void head_rows_few_kernel(HeadRowsParams p, RopeTable rt) {
+  using G = RowGeo<T, D, kFewSlots>;
+  using Rows = HeadRows<T, D, LAYOUT, kPaged>;
+  constexpr int VEC = G::VEC;
+  static_assert(G::TPT >= D / 2, "a lane for every pair");
+  __shared__ float2 turns[G::TOK][D / 2];
+  const int kind = blockIdx.y;
+  const int c = threadIdx.x % G::TPV, slot = threadIdx.x / G::TPV % kFewSlots, tl = threadIdx.x / G::TPT, j = threadIdx.x % G::TPT;
+  const int t = min((int)blockIdx.x * G::TOK + tl, p.n_tokens - 1);
+  const bool mine = (int)blockIdx.x * G::TOK + tl < p.n_tokens;
+  if (!p.src[kind]) return;
+  Rows rows(p, kind, c, t);
+  rows.load(slot, kFewSlots);
+  rows.gains();
+  CacheRow to = {};
+  if (kPaged && kind != kRowsQ) to = cache_row(p, t);
   float cs[VEC], sn[VEC];
-  if (p.rope) lane_turns<VEC, CH, LAYOUT>(rt, c, p.positions ? p.positions[t] : t, cs, sn);
-  // the token's row of the cache; none: nothing is kept of it
-  bool kept = true;
-  int64_t page = 0;
-  int row = 0;
-  if constexpr (kPaged) {
-    const int seq = p.seq_of_token ? p.seq_of_token[t] : t, at = p.cache_pos[t];
-    kept = seq >= 0 && seq < p.n_seqs && at >= 0 && at < p.max_rows;
-    if (kept) {
-      const uint32_t i = fast_div((uint32_t)at, p.page_div);
-      row = at - (int)i * p.page_rows;
-      page = p.page_table[seq * p.stride_table + i];
-      kept = page >= 0 && page < p.n_pages;
+  if (rows.turn) {
+    if (j < D / 2) {
+      float cj, sj;
+      sincos_phase(rope_phase(p.positions ? p.positions[t] : t, rt.turns[j]), cj, sj);
+      turns[tl][j] = make_float2(cj, sj);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) {
+      const float2 f = turns[tl][lane_pair<VEC, G::CH, LAYOUT>(c, e)];
+      cs[e] = f.x, sn[e] = f.y;
     }
   }
-  const int first = gridDim.y == 1 ? 0 : blockIdx.y, last = gridDim.y == 1 ? 2 : blockIdx.y;
+  if (!mine || (kPaged && kind != kRowsQ && !to.kept)) return;
+  T *dst = rows.target(t, to);
 #pragma unroll 1
-  for (int kind = first; kind <= last; ++kind) {
-    if (!p.src[kind] || (kPaged && kind != kRowsQ && !kept)) continue;
-    const T *src = (const T *)p.src[kind] + t * p.src_st[kind] + c * VEC;
-    T *dst = (T *)p.dst[kind] + c * VEC;
-    dst += kPaged && kind != kRowsQ ? page * p.dst_page[kind] + row * p.dst_st[kind] : t * p.dst_st[kind];
-    const int64_t src_sh = p.src_sh[kind], dst_sh = p.dst_sh[kind];
-    const int n = p.n_heads[kind];
-    const bool norm = kind != kRowsV && p.eps >= 0.f, turn = kind != kRowsV && p.rope;
-    float wx[VEC], wy[VEC];
-    if (norm) lane_gains<VEC, CH>(p.weight[kind], p.weight_f32, c, wx, wy);
-#pragma unroll 1
-    for (int h0 = slot; h0 < n; h0 += kSlots * kBatch) {
-      Ch x[kBatch], y[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int h = min(h0 + u * kSlots, n - 1);
-        x[u].load(src + h * src_sh);
-        y[u].load(src + h * src_sh + (CH / 2) * VEC);
-      }
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int h = h0 + u * kSlots;
-        if (h >= n) break;
-        if (norm) {
-          float ss = 0.f;
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) ss += x[u].f[e] * x[u].f[e] + y[u].f[e] * y[u].f[e];
-          const float r = rsqrtf(sum_over_lanes<G::TPV>(ss) * (1.0f / D) + p.eps);
-#pragma unroll
-          for (int e = 0; e < VEC; ++e) {
-            x[u].f[e] *= r * wx[e];
-            y[u].f[e] *= r * wy[e];
-          }
-        }
-        if (turn) turn_pieces<VEC, LAYOUT>(x[u].f, y[u].f, cs, sn);
-        x[u].store(dst + h * dst_sh);
-        y[u].store(dst + h * dst_sh + (CH / 2) * VEC);
-      }
-    }
+  for (int h0 = slot; h0 < rows.n; h0 += kFewSlots * Rows::kBatch) {
+    if (h0 != slot) rows.load(h0, kFewSlots);
+    rows.store(dst, h0, kFewSlots, cs, sn);
   }
 }
 
@@ -213,37 +296,53 @@ __global__ __launch_bounds__(kRotThreads) void norm_backward_kernel(NormBackward
 }
 
 // partial [n_wg][2][D] -> the gradients of the gains, in the order of the workgroups (64-bit sums: they are few)
+constexpr int kGainThreads = 1024, kGainCols = 16;
 template <int D>
-__global__ __launch_bounds__(kRotThreads) void gain_sums_kernel(NormBackwardParams p) {
-  constexpr int kCols = 32, kWays = kRotThreads / kCols;
+__global__ __launch_bounds__(kGainThreads) void gain_sums_kernel(NormBackwardParams p) {
+  constexpr int kCols = kGainCols, kWays = kGainThreads / kCols;
   __shared__ double red[kWays][kCols];
   const int kind = blockIdx.x / (D / kCols), col = blockIdx.x % (D / kCols) * kCols + threadIdx.x % kCols, way = threadIdx.x / kCols;
   if (!p.weight_grad[kind]) return;
+  static_assert(kNormBwdMaxWg % kWays == 0, "as many rounds as fit the registers");
+  float x[kNormBwdMaxWg / kWays];  // (all of a thread's loads go out together)
+#pragma unroll
+  for (int r = 0; r < kNormBwdMaxWg / kWays; ++r) {
+    const int i = r * kWays + way;
+    x[r] = i < p.n_wg ? p.partial[((int64_t)i * 2 + kind) * D + col] : 0.f;
+  }
   double sum = 0.0;
-#pragma unroll 8
-  for (int i = way; i < p.n_wg; i += kWays) sum += (double)p.partial[((int64_t)i * 2 + kind) * D + col];
+#pragma unroll
+  for (int r = 0; r < kNormBwdMaxWg / kWays; ++r) sum += (double)x[r];
   red[way][threadIdx.x % kCols] = sum;
   __syncthreads();
-  if (way == 0) {
-#pragma unroll
-    for (int w = 1; w < kWays; ++w) sum += red[w][threadIdx.x];
-    p.weight_grad[kind][col] = (float)sum;
+  for (int half = kWays / 2; half > 0; half /= 2) {
+    if (way < half) red[way][threadIdx.x % kCols] += red[way + half][threadIdx.x % kCols];
+    __syncthreads();
   }
+  if (way == 0) p.weight_grad[kind][col] = (float)red[0][threadIdx.x];
 }
 
-template <typename T, int D, int kSlots, bool kPaged>
-hipError_t launch_rows(const HeadRowsParams &p, const RopeTable &rt, bool split, hipStream_t stream) {
-  const dim3 grid((unsigned)((p.n_tokens + RowGeo<T, D, kSlots>::TOK - 1) / RowGeo<T, D, kSlots>::TOK), split ? (kPaged ? 3 : 2) : 1);
-  if (p.layout == 0)
-    head_rows_kernel<T, D, 0, kSlots, kPaged><<<grid, kRotThreads, 0, stream>>>(p, rt);
-  else
-    head_rows_kernel<T, D, 1, kSlots, kPaged><<<grid, kRotThreads, 0, stream>>>(p, rt);
+// Which of the two, us a call, many / few (Python face and all, which takes 4.7 of them).  32 over 8 heads of 128, bf16, norm and rotation: 64
+// tokens 7.6 / 5.2, 512 8.8 / 5.7, 1,024 9.7 / 7.8, 2,048 11.7 / 11.6, 4,096 17.0 / 19.5.  8 over 2 of 64, fp32: 1,024 5.6 / 5.2, 2,077 6.1 / 7.0.
+// Keys and values of 8 heads into pages: 512 5.3 / 5.3, 2,048 6.5 / 7.8.  The first one's lanes wait for memory once for every sixteen heads.
+inline bool few_tokens(const HeadRowsParams &p) {
+  const int heads = std::max(p.src[kRowsQ] ? p.n_heads[kRowsQ] : 0, p.n_heads[kRowsK]);
+  return p.n_tokens <= (heads > kManySlots * 4 ? 2048 : 1024);
+}
+template <typename T, int D, int LAYOUT, bool kPaged>
+hipError_t launch_rows(const HeadRowsParams &p, const RopeTable &rt, hipStream_t stream) {
+  if (few_tokens(p)) {
+    constexpr int TOK = RowGeo<T, D, kFewSlots>::TOK;
+    head_rows_few_kernel<T, D, LAYOUT, kPaged><<<dim3((unsigned)(p.n_tokens + TOK - 1) / TOK, kPaged ? 3 : 2), kRotThreads, 0, stream>>>(p, rt);
+  } else {
+    constexpr int TOK = RowGeo<T, D, kManySlots>::TOK;
+    head_rows_kernel<T, D, LAYOUT, kPaged><<<(unsigned)((p.n_tokens + (int64_t)TOK - 1) / TOK), kRotThreads, 0, stream>>>(p, rt);
+  }
   return hipGetLastError();
 }
 template <typename T, int D, bool kPaged>
 hipError_t launch_rows_d(const HeadRowsParams &p, const RopeTable &rt, hipStream_t stream) {
-  if (p.n_tokens <= 2048) return launch_rows<T, D, 16, kPaged>(p, rt, true, stream);
-  return launch_rows<T, D, 4, kPaged>(p, rt, false, stream);
+  return p.layout == 0 ? launch_rows<T, D, 0, kPaged>(p, rt, stream) : launch_rows<T, D, 1, kPaged>(p, rt, stream);
 }
 template <typename T, int D>
 hipError_t launch_back(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream) {
@@ -255,7 +354,7 @@ hipError_t launch_back(const NormBackwardParams &p, const RopeTable &rt, hipStre
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  gain_sums_kernel<D><<<2 * D / 32, kRotThreads, 0, stream>>>(p);
+  gain_sums_kernel<D><<<2 * D / kGainCols, kGainThreads, 0, stream>>>(p);
   return hipGetLastError();
 }
 

@@ -98,8 +98,8 @@ __device__ __forceinline__ int wave_min(int x) {
   return __builtin_amdgcn_readfirstlane(x);
 }
 
-// Where rows of the item's keys lie, and the loads of a wave instruction's worth of them (RPI rows from `key` on, which do not
-// cross a multiple of 16): lane l fetches chunk `chunk` of row l / CPR.
+// Where rows of the item's keys lie, and the loads of a run of them that does not cross a multiple of 16: wave instructions of RPI rows
+// each, lane l fetching one chunk of row l / CPR.
 template <int D, bool kAligned>
 struct PagedSource {
   using G = PGeo<D>;
@@ -107,30 +107,46 @@ struct PagedSource {
   const PagedItem &it;
   lds_char *table;
   const char *k, *v;
-  int lane_row;
-  __device__ __forceinline__ PagedSource(const PagedAttnParams &p_, const PagedItem &it_, lds_char *table_, int lane)
-      : p(p_), it(it_), table(table_), k((const char *)(p_.k + it_.kvh * p_.k_sh)), v((const char *)(p_.v + it_.kvh * p_.v_sh)), lane_row(lane / G::CPR) {}
+  __device__ __forceinline__ PagedSource(const PagedAttnParams &p_, const PagedItem &it_, lds_char *table_)
+      : p(p_), it(it_), table(table_), k((const char *)(p_.k + it_.kvh * p_.k_sh)), v((const char *)(p_.v + it_.kvh * p_.v_sh)) {}
   // the page of a key, -1: not there
   __device__ __forceinline__ int page_of(int key, int &row) const {
     const int i = (int)fast_div((uint32_t)key, p.page_div);
     row = key - i * p.page_rows;
     return ((const lds_int *)table)[i - it.page0];
   }
-  // chunk offsets (bytes) of this lane in a row of keys and of values
-  __device__ __forceinline__ void fetch(int key, uint32_t kchunk, uint32_t vchunk, uint32_t k_to, uint32_t v_to) const {
-    int row;
+  // where a row of page `page` lies behind page 0's
+  static __device__ __forceinline__ uint64_t behind(int page, uint32_t page_b16, int row, uint32_t rb) {
+    return ((uint64_t)(uint32_t)page * page_b16 << 4) + (uint64_t)(uint32_t)row * rb;
+  }
+  // N wave instructions of keys and of values, rows `key` on; chunks(u, &kchunk, &vchunk): what this lane fetches of its row in the u-th
+  template <int N, typename Chunks>
+  __device__ __forceinline__ void fetch(int key, int lane_row, uint32_t k_to, uint32_t v_to, Chunks &&chunks) const {
     if constexpr (kAligned) {
       // (rows behind the item's last lie in the same page, whole blocks of 16 behind it are its last block once more; pages that are
       // not there: page 0.  All of them are masked)
       key = __builtin_amdgcn_readfirstlane(key);
       key = min(key & ~15, (it.k1 - 1) & ~15) | (key & 15);
+      int row;
       const int page = max(0, __builtin_amdgcn_readfirstlane(page_of(key, row)));
-      lds_dma16(k + page * p.k_page_b + (uint64_t)(uint32_t)row * p.k_rb, (uint32_t)lane_row * p.k_rb + kchunk, k_to);
-      lds_dma16(v + page * p.v_page_b + (uint64_t)(uint32_t)row * p.v_rb, (uint32_t)lane_row * p.v_rb + vchunk, v_to);
+      const char *k0 = k + behind(page, p.k_page_b16, row, p.k_rb), *v0 = v + behind(page, p.v_page_b16, row, p.v_rb);
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        uint32_t kc, vc;
+        chunks(u, kc, vc);
+        lds_dma16(k0, (uint32_t)(u * G::RPI + lane_row) * p.k_rb + kc, k_to + u * 1024);
+        lds_dma16(v0, (uint32_t)(u * G::RPI + lane_row) * p.v_rb + vc, v_to + u * 1024);
+      }
     } else {
-      const int page = max(0, page_of(min(key + lane_row, it.k1 - 1), row));
-      lds_dma16_from(k + page * p.k_page_b + ((uint64_t)(uint32_t)row * p.k_rb + kchunk), k_to);
-      lds_dma16_from(v + page * p.v_page_b + ((uint64_t)(uint32_t)row * p.v_rb + vchunk), v_to);
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        uint32_t kc, vc;
+        chunks(u, kc, vc);
+        int row;
+        const int page = max(0, page_of(min(key + u * G::RPI + lane_row, it.k1 - 1), row));
+        lds_dma16_from(k + behind(page, p.k_page_b16, row, p.k_rb) + kc, k_to + u * 1024);
+        lds_dma16_from(v + behind(page, p.v_page_b16, row, p.v_rb) + vc, v_to + u * 1024);
+      }
     }
   }
   // bit i: key + i is one of the item's, and its page is there
@@ -172,7 +188,7 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const Page
   constexpr uint32_t TB = 16 * G::ROWB;              // a tile of keys, then one of values
   constexpr int NB = kTilesB / kPWaves / (2 * TB);   // tiles of a wave in LDS
   constexpr int OPS = 16 / G::RPI;                   // load instructions per tile and kind
-  const PagedSource<D, kAligned> src(p, it, smem + kTilesB, lane);
+  const PagedSource<D, kAligned> src(p, it, smem + kTilesB);
   const int col = lane & 15, quad = lane >> 4;
   const int n_tiles = (it.k1 - it.k0 + 15) / 16;
   const int n = n_tiles > wave ? (n_tiles - wave + kPWaves - 1) / kPWaves : 0;  // this wave's: wave, wave + 4, ...
@@ -183,14 +199,11 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const Page
     const uint32_t to = (uint32_t)(uintptr_t)smem + ring + (uint32_t)(i % NB) * (2 * TB);
     int ln = lane;
     if (RG > 2) asm volatile("" : "+v"(ln));  // (worked out anew: kept, the offsets take registers that the sums need)
-#pragma unroll
-    for (int u = 0; u < OPS; ++u) {
-      const int r = u * G::RPI + ln / G::CPR, pos = ln % G::CPR;
-      const int line = r / G::LPR;
-      const uint32_t kchunk = (uint32_t)(pos ^ (line & (G::CPR - 1))) << 4;
-      const uint32_t vchunk = (uint32_t)((((pos >> 1) ^ (line & (G::CPR / 2 - 1))) << 1) | (pos & 1)) << 4;
-      src.fetch(key + u * G::RPI, kchunk, vchunk, to + u * 1024, to + TB + u * 1024);
-    }
+    src.template fetch<OPS>(key, ln / G::CPR, to, to + TB, [&](int u, uint32_t &kchunk, uint32_t &vchunk) __attribute__((always_inline)) {
+      const int line = (u * G::RPI + ln / G::CPR) / G::LPR, pos = ln % G::CPR;
+      kchunk = (uint32_t)(pos ^ (line & (G::CPR - 1))) << 4;
+      vchunk = (uint32_t)((((pos >> 1) ^ (line & (G::CPR / 2 - 1))) << 1) | (pos & 1)) << 4;
+    });
   };
 #pragma unroll
   for (int i = 0; i < NB; ++i)
@@ -380,18 +393,17 @@ __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, const Page
   constexpr int NB = 4;  // tiles in LDS
   static_assert(NB * 2 * TB <= kTilesB, "the tiles fit");
   constexpr int IPW = 32 / G::RPI / kPWaves;
-  const PagedSource<D, kAligned> src(p, it, smem + kTilesB, lane);
+  const PagedSource<D, kAligned> src(p, it, smem + kTilesB);
   const int col = lane & 31, hf = lane >> 5;
   const int n_t = (it.k1 - it.k0 + 31) / 32;
   auto issue = [&](int t) __attribute__((always_inline)) {
     const uint32_t to = (uint32_t)(uintptr_t)smem + (uint32_t)(t % NB) * (2 * TB) + wave * IPW * 1024;
-#pragma unroll
-    for (int u = 0; u < IPW; ++u) {
-      const int r = (wave * IPW + u) * G::RPI + lane / G::CPR, pos = lane % G::CPR;
-      const uint32_t kchunk = (uint32_t)(pos ^ ((r / G::LPR) & (G::CPR - 1))) << 4;
-      const uint32_t vchunk = (uint32_t)((((pos >> 2) ^ ((r / G::LPR) & (GPR - 1))) << 2) | (pos & 3)) << 4;
-      src.fetch(it.k0 + t * 32 + (wave * IPW + u) * G::RPI, kchunk, vchunk, to + u * 1024, to + TB + u * 1024);
-    }
+    static_assert(IPW * G::RPI == 8, "a wave's rows do not cross a multiple of 16");
+    src.template fetch<IPW>(it.k0 + t * 32 + wave * 8, lane / G::CPR, to, to + TB, [&](int u, uint32_t &kchunk, uint32_t &vchunk) __attribute__((always_inline)) {
+      const int line = (wave * 8 + u * G::RPI + lane / G::CPR) / G::LPR, pos = lane % G::CPR;
+      kchunk = (uint32_t)(pos ^ (line & (G::CPR - 1))) << 4;
+      vchunk = (uint32_t)((((pos >> 2) ^ (line & (GPR - 1))) << 2) | (pos & 3)) << 4;
+    });
   };
   constexpr int OPS = 2 * IPW;  // of a wave and tile
 #pragma unroll
