@@ -407,7 +407,7 @@ int32_t ba_norm_rotate(const ba_heads *heads, const ba_head_norm *norm, const ba
  * q, k: the inputs of the forward call; d_q_out, d_k_out: the gradients of its outputs; dq, dk like q and k, which
  * may be exactly d_q_out or q (d_k_out or k).  dq_weight, dk_weight: device, [head_dim] floats, nullable; zeros
  * without tokens.  Deterministic: every sum is added up in a fixed order.
- * ws: 256-byte aligned, at least ba_norm_rotate_backward_workspace_bytes() bytes (1 MB at most).
+ * ws: 256-byte aligned, at least ba_norm_rotate_backward_workspace_bytes() bytes (512 KB at most).
  */
 int32_t ba_norm_rotate_backward(const ba_heads *heads, const ba_head_norm *norm, const ba_tensor *q,
                                 const ba_tensor *k, const ba_tensor *d_q_out,

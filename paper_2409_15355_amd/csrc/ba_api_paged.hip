@@ -98,7 +98,13 @@ int32_t check_apart(const ba_tensor *a, const char *a_name, int a_heads, const b
   return fail(BA_ERR_INVALID_ARG, "%s overlaps %s", a_name, b_name);
 }
 
-int backward_wgs(int64_t tokens) { return (int)std::min<int64_t>(tokens, kNormBwdMaxWg); }
+// Workgroups of the backward pass: as many as the chip holds at a time, shared out by heads (each tensor's share is the same without the
+// other: so are the bits of its gain's gradient).
+void backward_wgs(int64_t tokens, const ba_heads *h, bool q, bool k, NormBackwardParams *p) {
+  const int64_t hq = h->n_q_heads, all = hq + h->n_kv_heads;
+  p->wg_q = q ? (int32_t)std::min<int64_t>(tokens, kNormBwdMaxWg * hq / all) : 0;
+  p->n_wg = p->wg_q + (k ? (int32_t)std::min<int64_t>(tokens, std::max<int64_t>(1, kNormBwdMaxWg * (all - hq) / all)) : 0);
+}
 
 // ---- the paged cache -----------------------------------------------------------------------------------
 int32_t check_cache(const ba_paged_cache *c, const ba_heads *h) {
@@ -265,7 +271,7 @@ int32_t ba_norm_rotate(const ba_heads *heads, const ba_head_norm *norm, const ba
 
 size_t ba_norm_rotate_backward_workspace_bytes(const ba_heads *heads, int32_t n_tokens) {
   if (check_heads(heads, true) != BA_OK || n_tokens <= 0) return 0;
-  return align256((size_t)backward_wgs(n_tokens) * 2 * heads->head_dim * 4);
+  return align256((size_t)std::min<int64_t>(2 * (int64_t)n_tokens, kNormBwdMaxWg) * heads->head_dim * 4);
 }
 
 int32_t ba_norm_rotate_backward(const ba_heads *heads, const ba_head_norm *norm, const ba_tensor *q, const ba_tensor *k,
@@ -321,7 +327,7 @@ int32_t ba_norm_rotate_backward(const ba_heads *heads, const ba_head_norm *norm,
   }
   set_pass(&r, heads, norm, n_tokens, q ? q->dtype : k->dtype, positions, rope_mode);
   p.partial = (float *)ws;
-  p.n_wg = backward_wgs(n_tokens);
+  backward_wgs(n_tokens, heads, q != nullptr, k != nullptr, &p);
   return launch();
 }
 

@@ -37,8 +37,8 @@ struct NormBackwardParams {
   const void *grad[2];
   int64_t grad_st[2], grad_sh[2];
   float *weight_grad[2];  // device [D], nullable
-  float *partial;         // [workgroups][2][D]
-  int32_t n_wg;
+  float *partial;         // [workgroups][D]
+  int32_t wg_q, n_wg;     // workgroups for the queries, and all of them
 };
 constexpr int kNormBwdMaxWg = 1024;
 hipError_t launch_norm_rotate_backward(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream);

@@ -17,8 +17,8 @@ struct Chunk {
   typedef T_ T;
   static constexpr int VEC = 16 / sizeof(T);
   float f[VEC];
-  __device__ __forceinline__ void load(const T *p) {
-    const u32x4_t w = load_row_piece<kLoadPast>((const char *)p);
+  __device__ __forceinline__ void load(const T *p) { expand(load_row_piece<kLoadPast>((const char *)p)); }
+  __device__ __forceinline__ void expand(const u32x4_t &w) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if constexpr (VEC == 8) {

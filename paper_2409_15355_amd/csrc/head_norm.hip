@@ -221,81 +221,107 @@ __global__ __launch_bounds__(kRotThreads) void head_rows_few_kernel(HeadRowsPara
   }
 }
 
-// A workgroup takes token chunks blockIdx.x, + gridDim.x, ... and leaves its sums of the gains' gradients.
+// The first wg_q workgroups take queries, the others keys, a chunk of tokens each and every wg_q-th (n_wg - wg_q-th) after it, and leave
+// their sums of the gain's gradient.  A lane takes every kSlots-th head of its token, the next one's pieces on their way meanwhile.
 template <typename T, int D, int LAYOUT, int kSlots>
-__global__ __launch_bounds__(kRotThreads) void norm_backward_kernel(NormBackwardParams p, RopeTable rt) {
+__global__ __launch_bounds__(kRotThreads, 4) void norm_backward_kernel(NormBackwardParams p, RopeTable rt) {
   using G = RowGeo<T, D, kSlots>;
   typedef Chunk<T, false, false> Ch;
   constexpr int VEC = G::VEC, CH = G::CH, kVecs = kRotThreads / G::TPV;
   __shared__ float red[kVecs][D];
   const HeadRowsParams &r = p.rows;
-  const int c = threadIdx.x % G::TPV, slot = threadIdx.x / G::TPV % kSlots;
-  float dw[2][2 * VEC];
+  const int kind = (int)blockIdx.x >= p.wg_q, first = blockIdx.x - (kind ? p.wg_q : 0), step = kind ? p.n_wg - p.wg_q : p.wg_q;
+  const int c = threadIdx.x % G::TPV, slot = threadIdx.x / G::TPV % kSlots, n = r.n_heads[kind];
+  const T *src = (const T *)r.src[kind] + c * VEC, *grad = (const T *)p.grad[kind] + c * VEC;
+  T *dst = (T *)r.dst[kind] + c * VEC;
+  struct Pieces {
+    u32x4_t x, y, gx, gy;  // as they lie in memory: half the registers that they take as floats
+    int pos;
+  };
+  auto load = [&](Pieces &w, int64_t t, int h) __attribute__((always_inline)) {
+    const T *s = src + t * r.src_st[kind] + h * r.src_sh[kind], *g = grad + t * p.grad_st[kind] + h * p.grad_sh[kind];
+    w.x = *reinterpret_cast<const u32x4_t *>(s);
+    w.y = *reinterpret_cast<const u32x4_t *>(s + (CH / 2) * VEC);
+    w.gx = *reinterpret_cast<const u32x4_t *>(g);
+    w.gy = *reinterpret_cast<const u32x4_t *>(g + (CH / 2) * VEC);
+    w.pos = r.positions ? r.positions[t] : (int)t;
+  };
+  int64_t t = (int64_t)first * G::TOK + threadIdx.x / G::TPT;
+  int h = slot;
+  bool live = t < r.n_tokens && h < n;
+  Pieces next;
+  if (live) load(next, t, h);
+  // (the gains wait in LDS: with them, too, a lane would hold more than the 128 registers that let four workgroups share a compute unit)
+  __shared__ __attribute__((aligned(16))) float gains[D];
+  if ((int)threadIdx.x < G::TPV) {
+    float wx[VEC], wy[VEC];
+    lane_gains<VEC, CH>(r.weight[kind], r.weight_f32, c, wx, wy);
 #pragma unroll
-  for (int e = 0; e < 2 * VEC; ++e) dw[0][e] = dw[1][e] = 0.f;
-#pragma unroll 1
-  for (int64_t t = (int64_t)blockIdx.x * G::TOK + threadIdx.x / G::TPT; t < r.n_tokens; t += (int64_t)gridDim.x * G::TOK) {
-    float cs[VEC], sn[VEC];
-    if (r.rope) {
-      lane_turns<VEC, CH, LAYOUT>(rt, c, r.positions ? r.positions[t] : (int)t, cs, sn);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) sn[e] = -sn[e];  // the gradient turns back
-    }
-#pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-      if (!r.src[kind]) continue;
-      float wx[VEC], wy[VEC];
-      lane_gains<VEC, CH>(r.weight[kind], r.weight_f32, c, wx, wy);
-      const T *src = (const T *)r.src[kind] + t * r.src_st[kind] + c * VEC;
-      const T *grad = (const T *)p.grad[kind] + t * p.grad_st[kind] + c * VEC;
-      T *dst = (T *)r.dst[kind] + t * r.dst_st[kind] + c * VEC;
-#pragma unroll 1
-      for (int h = slot; h < r.n_heads[kind]; h += kSlots) {
-        Ch x, y, gx, gy;
-        x.load(src + h * r.src_sh[kind]);
-        y.load(src + h * r.src_sh[kind] + (CH / 2) * VEC);
-        gx.load(grad + h * p.grad_sh[kind]);
-        gy.load(grad + h * p.grad_sh[kind] + (CH / 2) * VEC);
-        if (r.rope) turn_pieces<VEC, LAYOUT>(gx.f, gy.f, cs, sn);
-        float ss = 0.f, dot = 0.f;
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          ss += x.f[e] * x.f[e] + y.f[e] * y.f[e];
-          dot += x.f[e] * (gx.f[e] * wx[e]) + y.f[e] * (gy.f[e] * wy[e]);
-        }
-        const float rs = rsqrtf(sum_over_lanes<G::TPV>(ss) * (1.0f / D) + r.eps);
-        const float m = sum_over_lanes<G::TPV>(dot) * (1.0f / D) * rs * rs;  // mean(b o x r) r
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          dw[kind][e] += gx.f[e] * (x.f[e] * rs);
-          dw[kind][VEC + e] += gy.f[e] * (y.f[e] * rs);
-          x.f[e] = rs * (gx.f[e] * wx[e] - x.f[e] * m);
-          y.f[e] = rs * (gy.f[e] * wy[e] - y.f[e] * m);
-        }
-        x.store(dst + h * r.dst_sh[kind]);
-        y.store(dst + h * r.dst_sh[kind] + (CH / 2) * VEC);
-      }
-    }
+    for (int e = 0; e < VEC; ++e) gains[c * VEC + e] = wx[e], gains[(c + CH / 2) * VEC + e] = wy[e];
   }
+  __syncthreads();
+  float dw[2 * VEC], cs[VEC], sn[VEC];
 #pragma unroll
-  for (int kind = 0; kind < 2; ++kind) {
-    __syncthreads();
+  for (int e = 0; e < 2 * VEC; ++e) dw[e] = 0.f;
+#pragma unroll 1
+  while (live) {
+    int64_t t2 = t;
+    int h2 = h + kSlots;
+    if (h2 >= n) h2 = slot, t2 += (int64_t)step * G::TOK;
+    live = t2 < r.n_tokens;
+    struct {
+      Ch x, y, gx, gy;
+      int pos;
+    } cur;
+    cur.x.expand(next.x), cur.y.expand(next.y), cur.gx.expand(next.gx), cur.gy.expand(next.gy);
+    cur.pos = next.pos;
+    if (live) load(next, t2, h2);
+    if (r.rope) {
+      if (h == slot) {
+        lane_turns<VEC, CH, LAYOUT>(rt, c, cur.pos, cs, sn);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sn[e] = -sn[e];  // the gradient turns back
+      }
+      turn_pieces<VEC, LAYOUT>(cur.gx.f, cur.gy.f, cs, sn);
+    }
+    int cw = c;
+    asm volatile("" : "+v"(cw));  // (read anew each time)
+    float ss = 0.f, dot = 0.f, wx[VEC], wy[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
-      red[threadIdx.x / G::TPV][c * VEC + e] = dw[kind][e];
-      red[threadIdx.x / G::TPV][(c + CH / 2) * VEC + e] = dw[kind][VEC + e];
+      wx[e] = gains[cw * VEC + e], wy[e] = gains[(cw + CH / 2) * VEC + e];
+      ss += cur.x.f[e] * cur.x.f[e] + cur.y.f[e] * cur.y.f[e];
+      dot += cur.x.f[e] * (cur.gx.f[e] * wx[e]) + cur.y.f[e] * (cur.gy.f[e] * wy[e]);
     }
-    __syncthreads();
-    if (threadIdx.x < D) {
-      float sum = 0.f;
+    const float rs = rsqrtf(sum_over_lanes<G::TPV>(ss) * (1.0f / D) + r.eps);
+    const float m = sum_over_lanes<G::TPV>(dot) * (1.0f / D) * rs * rs;  // mean(b o x r) r
 #pragma unroll
-      for (int v = 0; v < kVecs; ++v) sum += red[v][threadIdx.x];
-      p.partial[((int64_t)blockIdx.x * 2 + kind) * D + threadIdx.x] = sum;
+    for (int e = 0; e < VEC; ++e) {
+      dw[e] += cur.gx.f[e] * (cur.x.f[e] * rs);
+      dw[VEC + e] += cur.gy.f[e] * (cur.y.f[e] * rs);
+      cur.x.f[e] = rs * (cur.gx.f[e] * wx[e] - cur.x.f[e] * m);
+      cur.y.f[e] = rs * (cur.gy.f[e] * wy[e] - cur.y.f[e] * m);
     }
+    T *to = dst + t * r.dst_st[kind] + h * r.dst_sh[kind];
+    cur.x.store(to);
+    cur.y.store(to + (CH / 2) * VEC);
+    t = t2, h = h2;
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) {
+    red[threadIdx.x / G::TPV][c * VEC + e] = dw[e];
+    red[threadIdx.x / G::TPV][(c + CH / 2) * VEC + e] = dw[VEC + e];
+  }
+  __syncthreads();
+  if (threadIdx.x < D) {
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) sum += red[v][threadIdx.x];
+    p.partial[(int64_t)blockIdx.x * D + threadIdx.x] = sum;
   }
 }
 
-// partial [n_wg][2][D] -> the gradients of the gains, in the order of the workgroups (64-bit sums: they are few)
+// partial [n_wg][D] -> the gradients of the gains, in a fixed order (64-bit sums: they are few)
 constexpr int kGainThreads = 1024, kGainCols = 16;
 template <int D>
 __global__ __launch_bounds__(kGainThreads) void gain_sums_kernel(NormBackwardParams p) {
@@ -303,12 +329,13 @@ __global__ __launch_bounds__(kGainThreads) void gain_sums_kernel(NormBackwardPar
   __shared__ double red[kWays][kCols];
   const int kind = blockIdx.x / (D / kCols), col = blockIdx.x % (D / kCols) * kCols + threadIdx.x % kCols, way = threadIdx.x / kCols;
   if (!p.weight_grad[kind]) return;
+  const int first = kind ? p.wg_q : 0, n = kind ? p.n_wg - p.wg_q : p.wg_q;
   static_assert(kNormBwdMaxWg % kWays == 0, "as many rounds as fit the registers");
   float x[kNormBwdMaxWg / kWays];  // (all of a thread's loads go out together)
 #pragma unroll
   for (int r = 0; r < kNormBwdMaxWg / kWays; ++r) {
     const int i = r * kWays + way;
-    x[r] = i < p.n_wg ? p.partial[((int64_t)i * 2 + kind) * D + col] : 0.f;
+    x[r] = i < n ? p.partial[(int64_t)(first + i) * D + col] : 0.f;
   }
   double sum = 0.0;
 #pragma unroll
@@ -344,13 +371,21 @@ template <typename T, int D, bool kPaged>
 hipError_t launch_rows_d(const HeadRowsParams &p, const RopeTable &rt, hipStream_t stream) {
   return p.layout == 0 ? launch_rows<T, D, 0, kPaged>(p, rt, stream) : launch_rows<T, D, 1, kPaged>(p, rt, stream);
 }
+template <typename T, int D, int LAYOUT>
+void launch_back_rows(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream) {
+  // us a call, every fourth head / every sixteenth: 32 over 8 heads of 128, bf16, one token 13.1 / 9.6, 256 14.5 / 11.1, 512 15.7 / 13.4, 1,024
+  // 18.4 / 18.4, 2,048 21.1 / 24.5; 16 over 8, fp32, 256 10.8 / 9.8, 1,024 15.2 / 16.6; 8 over 2 of 64, fp32, 64 9.0 / 9.0, 512 11.0 / 11.6.
+  const int heads = std::max(p.rows.n_heads[kRowsQ], p.rows.n_heads[kRowsK]);
+  if (p.rows.n_tokens <= (heads > kManySlots * 4 ? 512 : 256))
+    norm_backward_kernel<T, D, LAYOUT, kFewSlots><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
+  else
+    norm_backward_kernel<T, D, LAYOUT, kManySlots><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
+}
 template <typename T, int D>
 hipError_t launch_back(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream) {
   if (p.n_wg > 0) {
-    if (p.rows.layout == 0)
-      norm_backward_kernel<T, D, 0, 4><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
-    else
-      norm_backward_kernel<T, D, 1, 4><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
+    if (p.rows.layout == 0) launch_back_rows<T, D, 0>(p, rt, stream);
+    else launch_back_rows<T, D, 1>(p, rt, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
