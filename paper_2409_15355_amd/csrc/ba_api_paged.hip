@@ -215,7 +215,7 @@ void plan_paged(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, 
 size_t plan_bytes(const PagedPlan &pl, const ba_heads *h, int32_t nq) {
   if (pl.parts <= 1 && pl.groups.n == 0) return 0;
   const size_t rows = (size_t)pl.n_seqs * nq * h->n_q_heads;
-  return align256(rows * pl.parts * h->head_dim * 4) + align256(rows * pl.parts * 8);
+  return align256(rows * pl.parts * h->head_dim * 2) + align256(rows * pl.parts * 16);
 }
 
 int32_t check_paged_sizes(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len) {
@@ -447,8 +447,8 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
     p.part_rows = (int64_t)pl.n_seqs * q_per_seq * heads->n_q_heads;
     p.max_parts = pl.parts;
     p.direct = pl.parts <= 1 && pl.groups.n == 0;
-    p.part_o = (float *)ws;
-    p.part_ml = (float *)((char *)ws + align256((size_t)p.part_rows * pl.parts * heads->head_dim * 4));
+    p.part_o = (uint16_t *)ws;
+    p.part_ml = (float *)((char *)ws + align256((size_t)p.part_rows * pl.parts * heads->head_dim * 2));
     auto run = [&](const auto &groups) {
       hipError_t e;
       {

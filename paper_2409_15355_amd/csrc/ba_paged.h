@@ -70,7 +70,8 @@ struct PagedAttnParams {
   int32_t chunk, own_chunk;  // keys of a work item of a prefix, of a sequence's own
   int32_t prefix_items;
   int32_t own_splits, own_row_tiles;
-  float *part_o, *part_ml;  // [part][token][query head][D], [..][2]: (reference in log2 units, sum)
+  uint16_t *part_o;         // [part][token][query head][D], fp16
+  float *part_ml;           // [part][token][query head][4]: reference in log2 units, sum, what part_o is to be multiplied by
   int64_t part_rows;        // tokens * query heads
   int32_t max_parts;        // of a row
   int32_t direct;           // one part for every row: the result itself

@@ -160,24 +160,52 @@ struct PagedSource {
 };
 __device__ __forceinline__ uint32_t below(int lim) { return lim <= 0 ? 0u : lim >= 32 ? ~0u : (1u << lim) - 1u; }
 
-// Four or eight consecutive dimensions of a row's result: the row itself, or its part.
-template <int E>
-__device__ __forceinline__ void write_row(const PagedAttnParams &p, const PagedItem &it, const PagedRow &r, int D, int d, const float *o, float m, float l,
+// A row's result: E consecutive dimensions of it at a time, of D.  top: the largest size among all D of o.
+// Parts are kept as fp16, divided by their sum and by a power of two that brings the largest into [2^13, 2^14): 2^-11 of an element at
+// most, an eighth of what the result's own rounding to bf16 may take, and half the memory traffic of 32 bits (64 sequences over
+// 31,744 shared keys, 32 over 8 heads of 128: 33 MB out and in again, of 130 MB of keys and values).
+struct RowEnd {
+  float m, l, inv, mult, scale;
+};
+__device__ __forceinline__ RowEnd row_end(const PagedAttnParams &p, float m, float l, float top) {
+  RowEnd e = {m, l, l == 0.f ? 0.f : 1.f / l, 1.f, 1.f};
+  if (!p.direct) {
+    const int exp = max(-100, __builtin_amdgcn_frexp_expf(top * e.inv));  // (0 of an infinity or a NaN, which stay what they are)
+    e.mult = e.inv * __builtin_ldexpf(1.f, 14 - exp);
+    e.scale = __builtin_ldexpf(1.f, exp - 14);
+  }
+  return e;
+}
+template <int D, int E>
+__device__ __forceinline__ void write_row(const PagedAttnParams &p, const PagedItem &it, const PagedRow &r, const RowEnd &end, int d, const float *o,
                                           bool first) {
   const int64_t row = r.tok * (p.n_kv_heads * p.group) + r.head;
   if (p.direct) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
     uint16_t *to = p.o + r.tok * p.o_st + r.head * p.o_sh + d;
 #pragma unroll
     for (int e = 0; e < E; e += 4)
-      *reinterpret_cast<u32x2_t *>(to + e) = u32x2_t{pack_bf16(o[e] * inv, o[e + 1] * inv), pack_bf16(o[e + 2] * inv, o[e + 3] * inv)};
-    if (p.lse && first) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+      *reinterpret_cast<u32x2_t *>(to + e) =
+          u32x2_t{pack_bf16(o[e] * end.inv, o[e + 1] * end.inv), pack_bf16(o[e + 2] * end.inv, o[e + 3] * end.inv)};
+    if (p.lse && first) p.lse[row] = end.l == 0.f ? -INFINITY : (end.m + __builtin_amdgcn_logf(end.l)) * 0.6931471805599453f;
   } else {
     const int64_t at = it.part * p.part_rows + row;
 #pragma unroll
-    for (int e = 0; e < E; e += 4) *reinterpret_cast<f32x4_t *>(p.part_o + at * D + d + e) = f32x4_t{o[e], o[e + 1], o[e + 2], o[e + 3]};
-    if (first) *reinterpret_cast<f32x2_t *>(p.part_ml + at * 2) = f32x2_t{l == 0.f ? -INFINITY : m, l};
+    for (int e = 0; e < E; e += 4)
+      *reinterpret_cast<u32x2_t *>(p.part_o + at * D + d + e) =
+          u32x2_t{pack_f16(o[e] * end.mult, o[e + 1] * end.mult), pack_f16(o[e + 2] * end.mult, o[e + 3] * end.mult)};
+    if (first) *reinterpret_cast<f32x4_t *>(p.part_ml + at * 4) = f32x4_t{end.l == 0.f ? -INFINITY : end.m, end.l, end.scale, 0.f};
   }
+}
+// the largest of each run of 16 lanes, in every lane of the run
+__device__ __forceinline__ float max_over_sixteen(float x) {
+  auto with = [&](auto ctrl) __attribute__((always_inline)) {
+    x = fmaxf(x, __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true)));
+  };
+  with(std::integral_constant<int, 0xb1>{});   // (as sum_over_lanes)
+  with(std::integral_constant<int, 0x4e>{});
+  with(std::integral_constant<int, 0x141>{});
+  with(std::integral_constant<int, 0x140>{});
+  return x;
 }
 
 // ---- few rows: RG groups of 16 ------------------------------------------------------------------------------------------
@@ -379,8 +407,12 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const Page
         for (int c = 0; c < 4; ++c) acc[e + c] += lw == 0.f ? 0.f : x[c] * f;
       }
     }
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(acc[e]));
+    const RowEnd end = row_end(p, m, lsum, max_over_sixteen(top));
     const int r = it.row0 + g * 16 + row;
-    if (r < it.n_rows) write_row<E>(p, it, paged_row(p, it, r), D, d, acc, m, lsum, d == 0);
+    if (r < it.n_rows) write_row<D, E>(p, it, paged_row(p, it, r), end, d, acc, d == 0);
   }
 }
 
@@ -569,14 +601,20 @@ __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, const Page
       }
     }
   }
-  if (!live || wave_row0 + col >= it.n_rows) return;
-  const float l = l_run + other_half(l_run);
+  if (!live) return;
+  float top = 0.f;
+#pragma unroll
+  for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) top = fmaxf(top, fabsf(oacc[dt][v]));
+  const RowEnd end = row_end(p, mb, l_run + other_half(l_run), fmaxf(top, other_half(top)));
+  if (wave_row0 + col >= it.n_rows) return;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int q4 = 0; q4 < 4; ++q4) {
       const float o4[4] = {oacc[dt][q4 * 4], oacc[dt][q4 * 4 + 1], oacc[dt][q4 * 4 + 2], oacc[dt][q4 * 4 + 3]};
-      write_row<4>(p, it, me, D, dt * 32 + q4 * 8 + hf * 4, o4, mb, l, dt == 0 && q4 == 0 && hf == 0);
+      write_row<D, 4>(p, it, me, end, dt * 32 + q4 * 8 + hf * 4, o4, dt == 0 && q4 == 0 && hf == 0);
     }
 }
 
@@ -648,18 +686,14 @@ __global__ __launch_bounds__(kPThreads, 2) void paged_attn_kernel(PagedAttnParam
   else walk_stream<D, kAligned, 1>(p, it, smem, lane, wave);
 }
 
-// o = sum_i 2^(m_i - m) o_i / sum_i 2^(m_i - m) l_i over a row's parts, m = max m_i: 32 lanes a row, kWays times over (every
-// kWays-th part each).  Their references and sums arrive together, a lane per part, ahead of the outputs.
-constexpr int kMergeThreads = 256;
+// o = sum_i w_i o_i / sum_i w_i over a row's parts, w_i = 2^(m_i - m) l_i, m = max m_i: sixteen lanes a row, kWays times over (every
+// kWays-th part each).  References and sums arrive together, a lane per part, ahead of the outputs.
+constexpr int kMergeThreads = 256, kMergeLanes = 16;
 template <int D, int kWays, typename Groups>
 __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnParams p, Groups groups) {
-  constexpr int E = D / 32, kRows = kMergeThreads / 32 / kWays;
-  typedef float vec_t __attribute__((ext_vector_type(E)));
-  __shared__ float all_ml[kWays][2];
-  __shared__ vec_t all_o[kWays][32];
-  const int64_t row = (int64_t)blockIdx.x * kRows + threadIdx.x / 32 / kWays;
-  if (row >= p.part_rows) return;  // (kWays > 1: a workgroup's one row)
-  const int lane = threadIdx.x & 31, way = threadIdx.x / 32 % kWays, hq = p.n_kv_heads * p.group;
+  constexpr int L = kMergeLanes, E = D / L, kRows = kMergeThreads / L / kWays;
+  const int lane = threadIdx.x % L, way = threadIdx.x / L % kWays, slot = threadIdx.x / L / kWays, hq = p.n_kv_heads * p.group;
+  const int64_t my_row = (int64_t)blockIdx.x * kRows + slot, row = min(my_row, p.part_rows - 1);
   const int tok = (int)(row / hq), head = (int)(row - (int64_t)tok * hq);
   const int seq = (int)fast_div((uint32_t)tok, p.nq_div);
   const int g = group_of(groups, seq);
@@ -667,68 +701,89 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnPar
   // (a sequence that ends in its prefix has no part of its own)
   const int len = length_of(p, seq), own = len > prefix ? (len - prefix / 16 * 16 + p.own_chunk - 1) / p.own_chunk : 0;
   const int parts = (g < 0 ? 0 : groups.splits[g]) + own;
-  float m = -INFINITY, l = 0.f;
-  vec_t o;
+  const int n = parts > way ? (parts - way + kWays - 1) / kWays : 0;  // this way's: way, way + kWays, ...
+  auto end_of = [&](int i) __attribute__((always_inline)) {
+    return i < n ? *reinterpret_cast<const f32x4_t *>(p.part_ml + ((way + (int64_t)i * kWays) * p.part_rows + row) * 4) : f32x4_t{-INFINITY, 0.f, 0.f, 0.f};
+  };
+  const f32x4_t first = end_of(lane);
+  float m = first[0], l = first[1];
+  for (int i = lane + L; i < n; i += L) {
+    const f32x4_t e = end_of(i);
+    const float to = fmaxf(m, e[0]);
+    l = (l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - to)) + (e[1] == 0.f ? 0.f : e[1] * __builtin_amdgcn_exp2f(e[0] - to));
+    m = to;
+  }
+  const float top = max_over_sixteen(m);
+  l = sum_over_lanes<L>(l == 0.f ? 0.f : l * __builtin_amdgcn_exp2f(m - top));
+  m = top;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  float o[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) o[e] = 0.f;
-  for (int i0 = way; i0 < parts; i0 += 32 * kWays) {
-    const int n = min(32, (parts - i0 + kWays - 1) / kWays);  // parts i0, i0 + kWays, ...
-    f32x2_t ml = {-INFINITY, 0.f};
-    if (lane < n) ml = *reinterpret_cast<const f32x2_t *>(p.part_ml + ((i0 + lane * kWays) * p.part_rows + row) * 2);
-    float top = ml[0];
-#pragma unroll
-    for (int x = 1; x < 32; x *= 2) top = fmaxf(top, __shfl_xor(top, x));
-    const float to = fmaxf(m, top);
-    const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - to);
-    const float w = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - to);  // (a part that saw nothing)
-    float add = ml[1] * w;
-#pragma unroll
-    for (int x = 1; x < 32; x *= 2) add += __shfl_xor(add, x);
-    m = to;
-    l = l * keep + add;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] *= keep;
-    const float *from = p.part_o + (i0 * p.part_rows + row) * D + lane * E;
-    constexpr int kAhead = 8;
-    for (int i = 0; i < n; i += kAhead) {
-      vec_t x[kAhead];
-#pragma unroll
-      for (int u = 0; u < kAhead; ++u) x[u] = *reinterpret_cast<const vec_t *>(from + min(i + u, n - 1) * (kWays * p.part_rows * D));
+  for (int i0 = 0; i0 < n; i0 += L) {
+    const f32x4_t e = i0 ? end_of(i0 + lane) : first;
+    const float w = e[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(e[0] - m) * (e[1] * inv) * e[2];
+    const int here = min(L, n - i0);
+    const uint16_t *from = p.part_o + ((way + (int64_t)i0 * kWays) * p.part_rows + row) * D + lane * E;
+    constexpr int kAhead = kWays > 1 ? 4 : 8;
+#pragma unroll 1
+    for (int i = 0; i < here; i += kAhead) {
+      uint32_t x[kAhead][E / 2];
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const float wi = __shfl(w, i + u, 32);  // (lanes without a part: zero)
+        const uint16_t *at = from + min(i + u, here - 1) * (kWays * p.part_rows * D);
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += wi == 0.f ? 0.f : x[u][e] * wi;
+        for (int c = 0; c < E / 2; c += 2) {
+          const u32x2_t h = *reinterpret_cast<const u32x2_t *>(at + 2 * c);
+          x[u][c] = h[0], x[u][c + 1] = h[1];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        const float wi = __shfl(w, i + u, L);  // (lanes without a part, and parts that saw nothing: zero)
+#pragma unroll
+        for (int c = 0; c < E / 2; ++c) {
+          o[2 * c] += wi == 0.f ? 0.f : f16_lo(x[u][c]) * wi;
+          o[2 * c + 1] += wi == 0.f ? 0.f : f16_hi(x[u][c]) * wi;
+        }
       }
     }
   }
   if constexpr (kWays > 1) {
-    all_o[way][lane] = o;
-    if (lane == 0) all_ml[way][0] = m, all_ml[way][1] = l;
+    // two dimensions of a row to a thread
+    typedef float pair_t __attribute__((ext_vector_type(2)));
+    __shared__ __attribute__((aligned(16))) float all_o[kRows][kWays][D];
+    __shared__ pair_t all_ml[kRows][kWays];
+#pragma unroll
+    for (int e = 0; e < E; e += 4) *reinterpret_cast<f32x4_t *>(&all_o[slot][way][lane * E + e]) = f32x4_t{o[e], o[e + 1], o[e + 2], o[e + 3]};
+    if (lane == 0) all_ml[slot][way] = pair_t{m, l};
     __syncthreads();
-    if (way) return;
+    const int mine = threadIdx.x / (D / 2), d = threadIdx.x % (D / 2) * 2;
+    const int64_t to_row = (int64_t)blockIdx.x * kRows + mine;
+    if (mine >= kRows || to_row >= p.part_rows) return;
+    float a = 0.f, b = 0.f;
+    m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int w = 1; w < kWays; ++w) m = fmaxf(m, all_ml[w][0]);
-    l = 0.f;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int w = 0; w < kWays; ++w) m = fmaxf(m, all_ml[mine][w][0]);
 #pragma unroll
     for (int w = 0; w < kWays; ++w) {
-      const float f = all_ml[w][1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(all_ml[w][0] - m);
-      l += all_ml[w][1] * f;
-      const vec_t x = all_o[w][lane];
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[e] += x[e] * f;
+      const pair_t ml = all_ml[mine][w], x = *reinterpret_cast<const pair_t *>(&all_o[mine][w][d]);
+      const float f = ml[1] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ml[0] - m) * ml[1];
+      l += f;
+      a += f == 0.f ? 0.f : x[0] * f;
+      b += f == 0.f ? 0.f : x[1] * f;
     }
+    const float all = l == 0.f ? 0.f : 1.f / l;
+    const int64_t to_tok = to_row / hq;
+    *reinterpret_cast<uint32_t *>(p.o + to_tok * p.o_st + (to_row - to_tok * hq) * p.o_sh + d) = pack_bf16(a * all, b * all);
+    if (p.lse && d == 0) p.lse[to_row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+  } else {
+    if (my_row >= p.part_rows) return;
+    uint16_t *to = p.o + tok * p.o_st + head * p.o_sh + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; e += 4) *reinterpret_cast<u32x2_t *>(to + e) = u32x2_t{pack_bf16(o[e], o[e + 1]), pack_bf16(o[e + 2], o[e + 3])};
+    if (p.lse && lane == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint32_t w[E / 2];
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e) w[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
-  uint32_t *to = reinterpret_cast<uint32_t *>(p.o + tok * p.o_st + head * p.o_sh + lane * E);
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e) to[e] = w[e];
-  if (p.lse && lane == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 template <int D, bool kAligned, typename Groups>
@@ -758,15 +813,18 @@ hipError_t launch_attn_d(const PagedAttnParams &p, const Groups &g, hipStream_t 
 }
 template <int D, int kWays, typename Groups>
 hipError_t launch_merge_w(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
-  constexpr int kRows = kMergeThreads / 32 / kWays;
+  constexpr int kRows = kMergeThreads / kMergeLanes / kWays;
   const int64_t wgs = (p.part_rows + kRows - 1) / kRows;
   if (wgs < 1 || wgs > 0x7fffffff) return hipErrorInvalidValue;
   paged_merge_kernel<D, kWays, Groups><<<(unsigned)wgs, kMergeThreads, 0, stream>>>(p, g);
   return hipGetLastError();
 }
+// As many ways as leave each two parts, in launches that the chip holds at a time.
 template <int D, typename Groups>
 hipError_t launch_merge_d(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
-  return p.max_parts > 8 ? launch_merge_w<D, 8>(p, g, stream) : launch_merge_w<D, 1>(p, g, stream);
+  if (p.max_parts >= 32 && p.part_rows <= 1024) return launch_merge_w<D, 16>(p, g, stream);
+  if (p.max_parts >= 8 && p.part_rows <= 4096) return launch_merge_w<D, 4>(p, g, stream);
+  return launch_merge_w<D, 1>(p, g, stream);
 }
 
 }  // namespace
