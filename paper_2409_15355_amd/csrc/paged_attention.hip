@@ -119,17 +119,26 @@ struct PagedSource {
   static __device__ __forceinline__ uint64_t behind(int page, uint32_t page_b16, int row, uint32_t rb) {
     return ((uint64_t)(uint32_t)page * page_b16 << 4) + (uint64_t)(uint32_t)row * rb;
   }
-  // N wave instructions of keys and of values, rows `key` on; chunks(u, &kchunk, &vchunk): what this lane fetches of its row in the u-th
-  template <int N, typename Chunks>
-  __device__ __forceinline__ void fetch(int key, int lane_row, uint32_t k_to, uint32_t v_to, Chunks &&chunks) const {
+  // Where the rows from a key on lie: asked for ahead of the loads, which would wait for LDS otherwise.
+  struct Run {
+    int key, page, row;
+  };
+  __device__ __forceinline__ Run run_at(int key) const {
+    Run r = {key, 0, 0};
     if constexpr (kAligned) {
       // (rows behind the item's last lie in the same page, whole blocks of 16 behind it are its last block once more; pages that are
       // not there: page 0.  All of them are masked)
       key = __builtin_amdgcn_readfirstlane(key);
-      key = min(key & ~15, (it.k1 - 1) & ~15) | (key & 15);
-      int row;
-      const int page = max(0, __builtin_amdgcn_readfirstlane(page_of(key, row)));
-      const char *k0 = k + behind(page, p.k_page_b16, row, p.k_rb), *v0 = v + behind(page, p.v_page_b16, row, p.v_rb);
+      r.page = page_of(min(key & ~15, (it.k1 - 1) & ~15) | (key & 15), r.row);
+    }
+    return r;
+  }
+  // N wave instructions of keys and of values, a run's rows; chunks(u, &kchunk, &vchunk): what this lane fetches of its row in the u-th
+  template <int N, typename Chunks>
+  __device__ __forceinline__ void fetch(const Run &run, int lane_row, uint32_t k_to, uint32_t v_to, Chunks &&chunks) const {
+    if constexpr (kAligned) {
+      const int page = max(0, __builtin_amdgcn_readfirstlane(run.page));
+      const char *k0 = k + behind(page, p.k_page_b16, run.row, p.k_rb), *v0 = v + behind(page, p.v_page_b16, run.row, p.v_rb);
 #pragma unroll
       for (int u = 0; u < N; ++u) {
         uint32_t kc, vc;
@@ -143,7 +152,7 @@ struct PagedSource {
         uint32_t kc, vc;
         chunks(u, kc, vc);
         int row;
-        const int page = max(0, page_of(min(key + u * G::RPI + lane_row, it.k1 - 1), row));
+        const int page = max(0, page_of(min(run.key + u * G::RPI + lane_row, it.k1 - 1), row));
         lds_dma16_from(k + behind(page, p.k_page_b16, row, p.k_rb) + kc, k_to + u * 1024);
         lds_dma16_from(v + behind(page, p.v_page_b16, row, p.v_rb) + vc, v_to + u * 1024);
       }
@@ -209,8 +218,9 @@ __device__ __forceinline__ float max_over_sixteen(float x) {
 }
 
 // ---- few rows: RG groups of 16 ------------------------------------------------------------------------------------------
-template <int D, bool kAligned, int RG>
-__device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const PagedItem &it, lds_char *smem, int lane, int wave) {
+// stage(): puts the item's part of the page table into LDS (the rows are asked for first, and arrive meanwhile)
+template <int D, bool kAligned, int RG, typename Stage>
+__device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem &it, lds_char *smem, int lane, int wave, Stage &&stage) {
   using G = PGeo<D>;
   constexpr int KK = D / 32, DS = D / 16;
   constexpr uint32_t TB = 16 * G::ROWB;              // a tile of keys, then one of values
@@ -222,21 +232,17 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const Page
   const int n = n_tiles > wave ? (n_tiles - wave + kPWaves - 1) / kPWaves : 0;  // this wave's: wave, wave + 4, ...
   const uint32_t ring = wave * (NB * 2 * TB);
 
-  auto issue = [&](int i) __attribute__((always_inline)) {
-    const int key = it.k0 + (wave + i * kPWaves) * 16;
+  auto run_of = [&](int i) __attribute__((always_inline)) { return src.run_at(it.k0 + (wave + i * kPWaves) * 16); };
+  auto issue = [&](int i, const auto &run) __attribute__((always_inline)) {
     const uint32_t to = (uint32_t)(uintptr_t)smem + ring + (uint32_t)(i % NB) * (2 * TB);
     int ln = lane;
     if (RG > 2) asm volatile("" : "+v"(ln));  // (worked out anew: kept, the offsets take registers that the sums need)
-    src.template fetch<OPS>(key, ln / G::CPR, to, to + TB, [&](int u, uint32_t &kchunk, uint32_t &vchunk) __attribute__((always_inline)) {
+    src.template fetch<OPS>(run, ln / G::CPR, to, to + TB, [&](int u, uint32_t &kchunk, uint32_t &vchunk) __attribute__((always_inline)) {
       const int line = (u * G::RPI + ln / G::CPR) / G::LPR, pos = ln % G::CPR;
       kchunk = (uint32_t)(pos ^ (line & (G::CPR - 1))) << 4;
       vchunk = (uint32_t)((((pos >> 1) ^ (line & (G::CPR / 2 - 1))) << 1) | (pos & 1)) << 4;
     });
   };
-#pragma unroll
-  for (int i = 0; i < NB; ++i)
-    if (i < n) issue(i);
-
   bf16x8_t qf[RG][KK];
   int limit[RG], least = 0x7fffffff;
 #pragma unroll
@@ -248,11 +254,14 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const Page
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) qf[g][kk] = *reinterpret_cast<const bf16x8_t *>(row + kk * 32);
   }
-  least = wave_min(least);
+  stage();
 #pragma unroll
   for (int g = 0; g < RG; ++g)
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[g][kk]));
+    for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(qf[g][kk]));  // (waited for here, not inside the loop)
+#pragma unroll 1
+  for (int i = 0; i < min(n, NB); ++i) issue(i, run_of(i));
+  least = wave_min(least);
 
   uint32_t k_rd[KK];
 #pragma unroll
@@ -278,6 +287,7 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const Page
     else if (newer == 2) dma_wait<4 * OPS>();
     else dma_wait<6 * OPS>();
     const int key0 = it.k0 + (wave + i * kPWaves) * 16;
+    const auto ahead = run_of(i + NB);
     bf16x8_t kf[KK];
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) kf[kk] = *(lds_bf16x8 *)(smem + (k_rd[kk] + buf));
@@ -293,7 +303,19 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const Page
     const uint32_t there = masked ? src.template there<16>(key0, lane) : 0xffffu;
     // the tile is in registers: its place takes the one that is NB further on
     lds_wait();
-    if (i + NB < n) issue(i + NB);
+    if (i + NB < n) issue(i + NB, ahead);
+    // A masked probability is zero, but zero times an infinity or a NaN is not: values of keys that a row does not see must
+    // not reach its sums, and are set to zero.
+    bool apart = false;  // the rows see different keys of the tile
+    if (masked) {
+      const int lim0 = __builtin_amdgcn_readfirstlane(limit[0] - key0);
+#pragma unroll
+      for (int g = 0; g < RG; ++g) apart |= __builtin_amdgcn_ballot_w64(below(limit[g] - key0) != below(lim0)) != 0;
+      const uint32_t seen = (apart ? there : there & below(lim0)) >> (quad * 4);
+      const u32x2_t keep = {(seen & 1 ? 0xffffu : 0u) | (seen & 2 ? 0xffff0000u : 0u), (seen & 4 ? 0xffffu : 0u) | (seen & 8 ? 0xffff0000u : 0u)};
+#pragma unroll
+      for (int ds = 0; ds < DS; ++ds) vf[ds] = __builtin_bit_cast(s16x4_t, __builtin_bit_cast(u32x2_t, vf[ds]) & keep);
+    }
 #pragma unroll
     for (int g = 0; g < RG; ++g) {
       f32x4_t s = {0.f, 0.f, 0.f, 0.f};
@@ -341,26 +363,23 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const Page
       l[g] += sum;
       const u32x2_t w = {pack_bf16(e4[0], e4[1]), pack_bf16(e4[2], e4[3])};
       const s16x4_t pf = __builtin_bit_cast(s16x4_t, w);
-      if (!masked) {
+      if (!apart) {
 #pragma unroll
         for (int ds = 0; ds < DS; ++ds) o[g][ds] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vf[ds], pf, o[g][ds], 0, 0, 0);
       } else {
-        // A masked probability is zero, but zero times an infinity or a NaN is not: values of keys that a row does not see must
-        // not reach its sums.  The rows that see the same keys go together, with every other key's values at zero.
+        // the rows that see the same keys go together
         uint64_t left = ~0ull;
 #pragma unroll 1
         while (left) {
           const int their_lim = __builtin_amdgcn_readlane(lim, __builtin_ctzll(left));
           const bool mine = lim == their_lim;
           left &= ~__builtin_amdgcn_ballot_w64(mine);
-          const uint32_t seen = there & below(their_lim);
-          if (seen == 0) continue;
+          const uint32_t seen = below(their_lim) >> (quad * 4);
+          if (their_lim <= 0) continue;
+          const u32x2_t keep = {(seen & 1 ? 0xffffu : 0u) | (seen & 2 ? 0xffff0000u : 0u), (seen & 4 ? 0xffffu : 0u) | (seen & 8 ? 0xffff0000u : 0u)};
 #pragma unroll
           for (int ds = 0; ds < DS; ++ds) {
-            s16x4_t f = vf[ds];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (!((seen >> (quad * 4 + e)) & 1)) f[e] = 0;
+            const s16x4_t f = __builtin_bit_cast(s16x4_t, __builtin_bit_cast(u32x2_t, vf[ds]) & keep);
             const f32x4_t add = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(f, pf, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[g][ds][e] += mine ? add[e] : 0.f;
@@ -417,8 +436,8 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, const Page
 }
 
 // ---- many rows: 32 a wave, tiles of 32 keys shared by the four -----------------------------------------------------------
-template <int D, bool kAligned>
-__device__ __forceinline__ void walk_shared(const PagedAttnParams &p, const PagedItem &it, lds_char *smem, int lane, int wave) {
+template <int D, bool kAligned, typename Stage>
+__device__ __forceinline__ void walk_shared(const PagedAttnParams &p, PagedItem &it, lds_char *smem, int lane, int wave, Stage &&stage) {
   using G = PGeo<D>;
   constexpr int KCH = D / 16, DT = D / 32, GPR = G::ROWB / 64;
   constexpr uint32_t TB = 32 * G::ROWB;
@@ -428,20 +447,17 @@ __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, const Page
   const PagedSource<D, kAligned> src(p, it, smem + kTilesB);
   const int col = lane & 31, hf = lane >> 5;
   const int n_t = (it.k1 - it.k0 + 31) / 32;
-  auto issue = [&](int t) __attribute__((always_inline)) {
+  auto run_of = [&](int t) __attribute__((always_inline)) { return src.run_at(it.k0 + t * 32 + wave * 8); };
+  auto issue = [&](int t, const auto &run) __attribute__((always_inline)) {
     const uint32_t to = (uint32_t)(uintptr_t)smem + (uint32_t)(t % NB) * (2 * TB) + wave * IPW * 1024;
     static_assert(IPW * G::RPI == 8, "a wave's rows do not cross a multiple of 16");
-    src.template fetch<IPW>(it.k0 + t * 32 + wave * 8, lane / G::CPR, to, to + TB, [&](int u, uint32_t &kchunk, uint32_t &vchunk) __attribute__((always_inline)) {
+    src.template fetch<IPW>(run, lane / G::CPR, to, to + TB, [&](int u, uint32_t &kchunk, uint32_t &vchunk) __attribute__((always_inline)) {
       const int line = (wave * 8 + u * G::RPI + lane / G::CPR) / G::LPR, pos = lane % G::CPR;
       kchunk = (uint32_t)(pos ^ (line & (G::CPR - 1))) << 4;
       vchunk = (uint32_t)((((pos >> 2) ^ (line & (GPR - 1))) << 2) | (pos & 3)) << 4;
     });
   };
   constexpr int OPS = 2 * IPW;  // of a wave and tile
-#pragma unroll
-  for (int t = 0; t < NB - 1; ++t)
-    if (t < n_t) issue(t);
-
   const int wave_row0 = it.row0 + wave * 32;
   const bool live = wave_row0 < it.n_rows;
   const PagedRow me = paged_row(p, it, min(wave_row0 + col, it.n_rows - 1));
@@ -451,9 +467,12 @@ __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, const Page
     const uint16_t *row = p.q + me.tok * p.q_st + me.head * p.q_sh + hf * 8;
 #pragma unroll
     for (int kk = 0; kk < KCH; ++kk) qf[kk] = *reinterpret_cast<const bf16x8_t *>(row + kk * 16);
+    stage();
 #pragma unroll
     for (int kk = 0; kk < KCH; ++kk) asm volatile("" : "+v"(qf[kk]));
   }
+#pragma unroll 1
+  for (int t = 0; t < min(n_t, NB - 1); ++t) issue(t, run_of(t));
   uint32_t k_rd[KCH], v_rd[DT];
 #pragma unroll
   for (int kk = 0; kk < KCH; ++kk) k_rd[kk] = col * G::ROWB + (((kk * 2 + hf) ^ ((col / G::LPR) & (G::CPR - 1))) << 4);
@@ -479,7 +498,8 @@ __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, const Page
     else if (newer == 1) dma_wait<OPS>();
     else dma_wait<2 * OPS>();
     wg_barrier();  // every wave's share of tile t has landed, and every wave is done with tile t - 1
-    if (t + NB - 1 < n_t) issue(t + NB - 1);
+    const auto ahead = run_of(t + NB - 1);
+    if (!live && t + NB - 1 < n_t) issue(t + NB - 1, ahead);
     if (live) {
       const uint32_t kofs = (uint32_t)(t % NB) * (2 * TB), vofs = kofs + TB;
       const int key0 = it.k0 + t * 32;
@@ -497,6 +517,7 @@ __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, const Page
         if (kk + kWin < KCH) fr[kk % kWin] = k_frag(kk + kWin);
         __builtin_amdgcn_sched_barrier(0);
       }
+      if (t + NB - 1 < n_t) issue(t + NB - 1, ahead);  // (in the shadow of the products)
       // keys that this lane's row does not see at -infinity
       const bool masked = it.holes || key0 < it.k_lo || key0 + 32 > least;
       const int lim = me.limit - key0;
@@ -654,36 +675,42 @@ __global__ __launch_bounds__(kPThreads, 2) void paged_attn_kernel(PagedAttnParam
     const int g = group_of(groups, it.seq0), prefix = g < 0 ? 0 : groups.prefix[g];
     // (cut at multiples of the chunk behind the multiple of 16 that the prefix ends above)
     it.k0 = prefix / 16 * 16 + it.part * p.own_chunk;
-    it.k1 = min(length_of(p, it.seq0), it.k0 + p.own_chunk);
+    it.k1 = min(p.cap, it.k0 + p.own_chunk);  // (as far as the sequence may reach: see below)
     it.k_lo = max(prefix, it.k0);
     if (g >= 0) it.part += groups.splits[g];
+  }
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // ---- the item's part of the page table; the entries are asked for together with the sequence's length -----------------------
+  it.page0 = (int)fast_div((uint32_t)it.k0, p.page_div);
+  const int32_t *const table = p.page_table + it.seq0 * p.stride_table + it.page0;
+  auto n_pages = [&]() __attribute__((always_inline)) { return it.k1 > it.k0 ? (int)fast_div((uint32_t)(it.k1 - 1), p.page_div) - it.page0 + 1 : 0; };
+  int id = -1;
+  if ((int)threadIdx.x < n_pages()) id = table[threadIdx.x];
+  if ((int)blockIdx.x >= p.prefix_items) {
+    it.k1 = min(it.k1, length_of(p, it.seq0));
     if (it.k_lo >= it.k1) {
       if (!p.direct) return;  // (the merge knows)
       it.k0 = it.k_lo = it.k1 = 0;
     }
   }
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // ---- the item's part of the page table --------------------------------------------------------------------------
-  it.page0 = (int)fast_div((uint32_t)it.k0, p.page_div);
-  it.holes = false;
-  if (it.k1 > it.k0) {
-    const int n_pages = (int)fast_div((uint32_t)(it.k1 - 1), p.page_div) - it.page0 + 1;
-    const int32_t *table = p.page_table + it.seq0 * p.stride_table + it.page0;
+  auto stage = [&]() __attribute__((always_inline)) {
+    const int n = n_pages();
     int bad = 0;
-    for (int i = threadIdx.x; i < n_pages; i += kPThreads) {
-      const int id = table[i];
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kPThreads) {
+      if (i >= kPThreads) id = table[i];
       const bool ok = id >= 0 && id < p.n_pages;
       ((lds_int *)(smem + kTilesB))[i] = ok ? id : -1;
       bad |= !ok;
     }
     it.holes = __syncthreads_or(bad) != 0;
-  }
+  };
   const int rows = it.n_rows - it.row0;
-  if (it.n_rows > kPagedStreamRows) walk_shared<D, kAligned>(p, it, smem, lane, wave);
-  else if (rows > 32) walk_stream<D, kAligned, 3>(p, it, smem, lane, wave);
-  else if (rows > 16) walk_stream<D, kAligned, 2>(p, it, smem, lane, wave);
-  else walk_stream<D, kAligned, 1>(p, it, smem, lane, wave);
+  if (it.n_rows > kPagedStreamRows) walk_shared<D, kAligned>(p, it, smem, lane, wave, stage);
+  else if (rows > 32) walk_stream<D, kAligned, 3>(p, it, smem, lane, wave, stage);
+  else if (rows > 16) walk_stream<D, kAligned, 2>(p, it, smem, lane, wave, stage);
+  else walk_stream<D, kAligned, 1>(p, it, smem, lane, wave, stage);
 }
 
 // o = sum_i w_i o_i / sum_i w_i over a row's parts, w_i = 2^(m_i - m) l_i, m = max m_i: sixteen lanes a row, kWays times over (every
