@@ -323,10 +323,10 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem 
       for (int kk = 0; kk < KK; ++kk) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[kk], qf[g][kk], s, 0, 0, 0);
       const int lim = limit[g] - key0;
       if (masked) {
-        const uint32_t mine = there & below(lim);
+        const uint32_t mine = (there & below(lim)) >> (quad * 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (!((mine >> (quad * 4 + e)) & 1)) s[e] = -INFINITY;
+          if (!((mine >> e) & 1)) s[e] = -INFINITY;
       }
       // the reference: the row's maximum in the first tile of which it sees a key, raised where an exponential threatens to overflow
       auto row_max = [&]() __attribute__((always_inline)) {
@@ -473,152 +473,163 @@ __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, PagedItem 
   }
 #pragma unroll 1
   for (int t = 0; t < min(n_t, NB - 1); ++t) issue(t, run_of(t));
-  uint32_t k_rd[KCH], v_rd[DT];
-#pragma unroll
-  for (int kk = 0; kk < KCH; ++kk) k_rd[kk] = col * G::ROWB + (((kk * 2 + hf) ^ ((col / G::LPR) & (G::CPR - 1))) << 4);
-  {
-    const int vrow = hf * 4 + ((lane & 15) >> 2);
-    const int vwithin = ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) v_rd[dt] = vrow * G::ROWB + ((dt ^ ((vrow / G::LPR) & (GPR - 1))) << 6) + vwithin;
-  }
-  f32x16_t oacc[DT];
+  // where this lane's fragments begin; chunk pairs kk and slabs dt on are an exclusive or away (the swizzle is one, too)
+  const uint32_t k_rd = col * G::ROWB + ((hf ^ ((col / G::LPR) & (G::CPR - 1))) << 4);
+  const int v_row = hf * 4 + ((lane & 15) >> 2);
+  const uint32_t v_rd = v_row * G::ROWB + (((v_row / G::LPR) & (GPR - 1)) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+  f32x16_t oacc[DT], s;
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
     for (int v = 0; v < 16; ++v) oacc[dt][v] = 0.f;
+  bf16x8_t pf[2];
   float mb = -INFINITY;  // the row's reference, log2 units; not set before the row has seen a key
   float l_run = 0.f;     // this lane's share of the running sum of exponentials
-  constexpr int kWin = KCH < 4 ? KCH : 4;  // fragments on their way from LDS
-
-#pragma unroll 1
-  for (int t = 0; t < n_t; ++t) {
+  constexpr int kWin = 4;  // fragments on their way from LDS
+  auto place = [&](int t) __attribute__((always_inline)) { return (uint32_t)(t % NB) * (2 * TB); };
+  auto v_frag = [&](uint32_t vofs, int st) __attribute__((always_inline)) {
+    typedef short s16x8_t __attribute__((ext_vector_type(8)));
+    const int kc = st / DT, dt = st % DT;
+    const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + ((v_rd + vofs) ^ (dt << 6)) + kc * 16 * G::ROWB));
+    const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + ((v_rd + vofs) ^ (dt << 6)) + (kc * 16 + 8) * G::ROWB));
+    return __builtin_bit_cast(bf16x8_t, (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  auto scores = [&](int t) __attribute__((always_inline)) {
+    const uint32_t kofs = place(t);
+    auto k_frag = [&](int kk) __attribute__((always_inline)) { return *(lds_bf16x8 *)(smem + ((k_rd + kofs) ^ (kk << 5))); };
+    bf16x8_t fr[kWin];
+#pragma unroll
+    for (int kk = 0; kk < kWin; ++kk) fr[kk] = k_frag(kk);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int kk = 0; kk < KCH; ++kk) {
+      const f32x16_t zero = {};
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[kk % kWin], qf[kk], kk ? s : zero, 0, 0, 0);
+      if (kk + kWin < KCH) fr[kk % kWin] = k_frag(kk + kWin);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  auto exponentials = [&]() __attribute__((always_inline)) {
+    auto row_max = [&]() __attribute__((always_inline)) {
+      float m = s[0];
+#pragma unroll
+      for (int v = 1; v < 16; ++v) m = fmaxf(m, s[v]);
+      return fmaxf(m, other_half(m)) * p.scale_log2e;
+    };
+    // the reference: the row's maximum in the first tile of which it sees a key, raised where an exponential threatens to overflow
+    if (__builtin_amdgcn_ballot_w64(mb == -INFINITY) != 0) {
+      const float m = row_max();
+      if (mb == -INFINITY) mb = m;
+    }
+    float sum;
+    auto powers = [&]() __attribute__((always_inline)) {
+      const float ref = mb == -INFINITY ? 0.f : mb;
+      float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        u32x4_t w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e * 8 + 2 * i], p.scale_log2e, -ref));
+          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e * 8 + 2 * i + 1], p.scale_log2e, -ref));
+          s0 += p0;
+          s1 += p1;
+          w[i] = pack_bf16(p0, p1);
+        }
+        pf[e] = __builtin_bit_cast(bf16x8_t, w);
+      }
+      sum = s0 + s1;
+    };
+    powers();
+    if (__builtin_amdgcn_ballot_w64(!(sum < kRebaseAbove)) != 0) {
+      // (only the rows concerned: what another row's scores are changes no bit of this one)
+      const float m = !(sum + other_half(sum) < kRebaseAbove) ? fmaxf(row_max(), mb) : mb;
+      const float alpha = m == mb ? 1.f : __builtin_amdgcn_exp2f(mb - m);
+      mb = m;
+      l_run *= alpha;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
+      powers();
+    }
+    l_run += sum;
+  };
+  // tile t has landed (every wave's share), nobody needs tile t - 1
+  auto next_tile = [&](int t) __attribute__((always_inline)) {
     const int newer = min(NB - 1, n_t - t) - 1;
     if (newer == 0) dma_wait<0>();
     else if (newer == 1) dma_wait<OPS>();
     else dma_wait<2 * OPS>();
-    wg_barrier();  // every wave's share of tile t has landed, and every wave is done with tile t - 1
-    const auto ahead = run_of(t + NB - 1);
-    if (!live && t + NB - 1 < n_t) issue(t + NB - 1, ahead);
-    if (live) {
-      const uint32_t kofs = (uint32_t)(t % NB) * (2 * TB), vofs = kofs + TB;
-      const int key0 = it.k0 + t * 32;
-      f32x16_t s;
-#pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = 0.f;
-      auto k_frag = [&](int kk) __attribute__((always_inline)) { return *(lds_bf16x8 *)(smem + (k_rd[kk] + kofs)); };
-      bf16x8_t fr[kWin];
-#pragma unroll
-      for (int kk = 0; kk < kWin; ++kk) fr[kk] = k_frag(kk);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int kk = 0; kk < KCH; ++kk) {
-        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fr[kk % kWin], qf[kk], s, 0, 0, 0);
-        if (kk + kWin < KCH) fr[kk % kWin] = k_frag(kk + kWin);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-      if (t + NB - 1 < n_t) issue(t + NB - 1, ahead);  // (in the shadow of the products)
-      // keys that this lane's row does not see at -infinity
-      const bool masked = it.holes || key0 < it.k_lo || key0 + 32 > least;
-      const int lim = me.limit - key0;
-      uint32_t there = ~0u;
-      if (masked) {
-        there = src.template there<32>(key0, lane);
-        const uint32_t mine = there & below(lim);
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (!((mine >> ((v >> 2) * 8 + hf * 4 + (v & 3))) & 1)) s[v] = -INFINITY;
-      }
-      auto row_max = [&]() __attribute__((always_inline)) {
-        float m = s[0];
-#pragma unroll
-        for (int v = 1; v < 16; ++v) m = fmaxf(m, s[v]);
-        return fmaxf(m, other_half(m)) * p.scale_log2e;
-      };
-      if (__builtin_amdgcn_ballot_w64(mb == -INFINITY) != 0) {
-        const float m = row_max();
-        if (mb == -INFINITY) mb = m;
-      }
-      auto v_frag = [&](int st) __attribute__((always_inline)) {
-        typedef short s16x8_t __attribute__((ext_vector_type(8)));
-        const int kc = st / DT, dt = st % DT;
-        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + (v_rd[dt] + vofs) + kc * 16 * G::ROWB));
-        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + (v_rd[dt] + vofs) + (kc * 16 + 8) * G::ROWB));
-        return (s16x8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-      };
-      bf16x8_t vf[kWin];
-#pragma unroll
-      for (int st = 0; st < 2; ++st) vf[st] = __builtin_bit_cast(bf16x8_t, v_frag(st));
-      __builtin_amdgcn_sched_barrier(0);
-      bf16x8_t pf[2];
-      float sum;
-      auto exponentials = [&]() __attribute__((always_inline)) {
-        const float ref = mb == -INFINITY ? 0.f : mb;
-        float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          u32x4_t w;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e * 8 + 2 * i], p.scale_log2e, -ref));
-            const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e * 8 + 2 * i + 1], p.scale_log2e, -ref));
-            s0 += p0;
-            s1 += p1;
-            w[i] = pack_bf16(p0, p1);
-          }
-          pf[e] = __builtin_bit_cast(bf16x8_t, w);
-        }
-        sum = s0 + s1;
-      };
-      exponentials();
-      if (__builtin_amdgcn_ballot_w64(!(sum < kRebaseAbove)) != 0) {
-        const float m = !(sum + other_half(sum) < kRebaseAbove) ? fmaxf(row_max(), mb) : mb;
-        const float alpha = m == mb ? 1.f : __builtin_amdgcn_exp2f(mb - m);
-        mb = m;
-        l_run *= alpha;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
-        exponentials();
-      }
-      l_run += sum;
-      if (!masked) {
-#pragma unroll
-        for (int st = 2; st < kWin; ++st) vf[st] = __builtin_bit_cast(bf16x8_t, v_frag(st));
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int st = 0; st < 2 * DT; ++st) {
-          oacc[st % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[st % kWin], pf[st / DT], oacc[st % DT], 0, 0, 0);
-          if (st + kWin < 2 * DT) vf[st % kWin] = __builtin_bit_cast(bf16x8_t, v_frag(st + kWin));
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      } else {
-        uint64_t left = ~0ull;  // (as in walk_stream)
+    wg_barrier();
+  };
+  // Tiles before t_part: all of the wave's rows see all of their keys.  (Apart from the others: one loop for both would keep a second set
+  // of sums, and move 64 registers a tile.)
+  const int t_part = !live || it.holes || it.k_lo > it.k0 ? 0 : max(0, min(n_t, (least - it.k0) / 32));
 #pragma unroll 1
-        while (left) {
-          const int their_lim = __builtin_amdgcn_readlane(lim, __builtin_ctzll(left));
-          const bool mine = lim == their_lim;
-          left &= ~__builtin_amdgcn_ballot_w64(mine);
-          const uint32_t seen = there & below(their_lim);
-          if (seen == 0) continue;
+  for (int t = 0; t < t_part; ++t) {
+    next_tile(t);
+    const auto ahead = run_of(t + NB - 1);
+    scores(t);
+    if (t + NB - 1 < n_t) issue(t + NB - 1, ahead);  // (in the shadow of the products)
+    const uint32_t vofs = place(t) + TB;
+    bf16x8_t vf[kWin];
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            f32x16_t add;
+    for (int st = 0; st < 2; ++st) vf[st] = v_frag(vofs, st);
+    __builtin_amdgcn_sched_barrier(0);
+    exponentials();
 #pragma unroll
-            for (int v = 0; v < 16; ++v) add[v] = 0.f;
+    for (int st = 2; st < kWin; ++st) vf[st] = v_frag(vofs, st);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int kc = 0; kc < 2; ++kc) {
-              auto f = v_frag(kc * DT + dt);
+    for (int st = 0; st < 2 * DT; ++st) {
+      oacc[st % DT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[st % kWin], pf[st / DT], oacc[st % DT], 0, 0, 0);
+      if (st + kWin < 2 * DT) vf[st % kWin] = v_frag(vofs, st + kWin);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+#pragma unroll 1
+  for (int t = t_part; t < n_t; ++t) {
+    next_tile(t);
+    if (t + NB - 1 < n_t) issue(t + NB - 1, run_of(t + NB - 1));
+    if (!live) continue;
+    const int key0 = it.k0 + t * 32, lim = max(0, min(32, me.limit - key0));
+    const uint32_t there = src.template there<32>(key0, lane);
+    scores(t);
+    {  // keys that this lane's row does not see at -infinity
+      const uint32_t seen = (there & below(lim)) >> (hf * 4);
 #pragma unroll
-              for (int e = 0; e < 8; ++e)
-                if (!((seen >> (kc * 16 + (e >> 2) * 8 + hf * 4 + (e & 3))) & 1)) f[e] = 0;
-              add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f), pf[kc], add, 0, 0, 0);
-            }
+      for (int v = 0; v < 16; ++v)
+        if (!((seen >> ((v >> 2) * 8 + (v & 3))) & 1)) s[v] = -INFINITY;
+    }
+    exponentials();
+    // A masked probability is zero, but zero times an infinity or a NaN is not: values of keys that a row does not see must not
+    // reach its sums.  The rows that see the same keys go together, with every other key's values at zero.
+    uint64_t left = ~0ull;
+#pragma unroll 1
+    while (left) {
+      const int their_lim = __builtin_amdgcn_readlane(lim, __builtin_ctzll(left));
+      const bool same = lim == their_lim;
+      left &= ~__builtin_amdgcn_ballot_w64(same);
+      const uint32_t seen = there & below(their_lim);
+      if (seen == 0) continue;
 #pragma unroll
-            for (int v = 0; v < 16; ++v) oacc[dt][v] += mine ? add[v] : 0.f;
+      for (int dt = 0; dt < DT; ++dt) {
+        f32x16_t add = {};
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc) {
+          const uint32_t mask = seen >> (kc * 16 + hf * 4);
+          u32x4_t f = __builtin_bit_cast(u32x4_t, v_frag(place(t) + TB, kc * DT + dt));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {  // keys (e / 2) * 8 + (e % 2) * 2 and the next
+            const uint32_t two = mask >> (e / 2 * 8 + e % 2 * 2);
+            f[e] &= (two & 1 ? 0xffffu : 0u) | (two & 2 ? 0xffff0000u : 0u);
           }
+          add = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, f), pf[kc], add, 0, 0, 0);
         }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) oacc[dt][v] += same ? add[v] : 0.f;
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
   }
