@@ -456,7 +456,7 @@ int32_t ba_paged_append(const ba_heads *heads, const ba_head_norm *norm, const b
 
 /*
  * Attention of the newest tokens of every sequence over its pages: an answer's next token, or a few drafted ones.
- * Sequence s has seq_len[s] tokens in the cache (device; taken as at most max_len, which is the host's bound), the last
+ * Sequence s has seq_len[s] tokens in the cache (device; taken as at most max_len, which is the host's bound, 2^30 at most), the last
  * q_per_seq of them are rows [s * q_per_seq, (s + 1) * q_per_seq) of q and o_out ([n_seqs * q_per_seq, n_q_heads, D], bf16,
  * rotated).  Token i of them is the sequence's token p = seq_len[s] - q_per_seq + i and sees tokens 0 .. p:
  *   o[i, h] = sum_{t <= p} softmax_t(scale * <q[i, h], k_t>) v_t.

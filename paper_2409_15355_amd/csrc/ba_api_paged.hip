@@ -141,6 +141,7 @@ struct PagedPlan {
   int32_t seq0, n_seqs, group_end;  // (group_end: the first group that is left for the next plan)
   int32_t chunk, own_chunk, own_splits, own_row_tiles, prefix_items;
   int32_t parts;
+  int64_t items;  // of the launch, all of them
   PagedGroups groups;
 };
 
@@ -200,17 +201,18 @@ void plan_paged(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, 
   auto splits = [&](int64_t keys, int64_t chunk) { return (int32_t)((keys + chunk - 1) / chunk); };
   pl->own_splits = splits(max_len - least_prefix / 16 * 16, pl->own_chunk);
   pl->parts = least_prefix == 0 ? pl->own_splits : 0;
-  int32_t items = 0;
+  int64_t items = 0;
   for (int i = 0; i < pl->groups.n; ++i) {
     pl->groups.splits[i] = splits(pl->groups.prefix[i], pl->chunk);
-    pl->groups.item0[i] = items;
-    items += (int32_t)(pl->groups.splits[i] * row_tiles(pl->groups.members[i] * nq * G) * hkv);
+    pl->groups.item0[i] = (int32_t)std::min<int64_t>(items, INT32_MAX);
+    items += (int64_t)(pl->groups.splits[i] * row_tiles(pl->groups.members[i] * nq * G) * hkv);
     pl->parts = std::max(pl->parts, pl->groups.splits[i] + splits(max_len - pl->groups.prefix[i] / 16 * 16, pl->own_chunk));
   }
-  pl->groups.item0[pl->groups.n] = items;
-  pl->prefix_items = items;
+  pl->groups.item0[pl->groups.n] = (int32_t)std::min<int64_t>(items, INT32_MAX);
+  pl->prefix_items = (int32_t)std::min<int64_t>(items, INT32_MAX);
   // (somebody has to write the rows of sequences that see nothing)
   if (pl->parts <= 1 && items == 0) pl->own_splits = 1;
+  pl->items = items + (int64_t)pl->n_seqs * hkv * pl->own_row_tiles * pl->own_splits;
 }
 size_t plan_bytes(const PagedPlan &pl, const ba_heads *h, int32_t nq) {
   if (pl.parts <= 1 && pl.groups.n == 0) return 0;
@@ -223,8 +225,9 @@ int32_t check_paged_sizes(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t
   if ((rc = check_heads(h, true))) return rc;
   if (n_seqs < 0) return fail(BA_ERR_INVALID_ARG, "negative sequence count");
   if (nq < 1) return fail(BA_ERR_INVALID_ARG, "q_per_seq must be positive");
-  if (max_len < 0 || max_len > 0x7fffffff - 1024) return fail(BA_ERR_INVALID_ARG, "max_len out of range");
-  // (row and item numbers are 32-bit)
+  if (max_len < 0) return fail(BA_ERR_INVALID_ARG, "negative max_len");
+  // (row, key and item numbers are 32-bit)
+  if (max_len > (1 << 30)) return fail(BA_ERR_UNSUPPORTED, "max_len beyond 2^30");
   if ((int64_t)n_seqs * nq > (1 << 28) || (int64_t)n_seqs * nq * h->n_q_heads > (1 << 28))
     return fail(BA_ERR_UNSUPPORTED, "more than 2^28 query rows in one call");
   return BA_OK;
@@ -419,6 +422,7 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
     plan_paged(heads, n_seqs, q_per_seq, max_len, n_groups, cu_group, prefix_len, g, num_cus(), &pl);
     g = pl.group_end;
     if (pl.n_seqs == 0) continue;
+    if (pl.items > INT32_MAX) return fail(BA_ERR_UNSUPPORTED, "more than 2^31 work items in one launch");
     const int64_t tok0 = (int64_t)pl.seq0 * q_per_seq;
     PagedAttnParams p;
     memset(&p, 0, sizeof(p));
