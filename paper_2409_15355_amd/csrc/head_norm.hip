@@ -97,11 +97,11 @@ __device__ __forceinline__ CacheRow cache_row(const HeadRowsParams &p, int t) {
   return r;
 }
 
-// A few heads of one tensor and token on their way: kBatch of them in flight per lane.
-template <typename T, int D, int LAYOUT, bool kPaged>
+// A few heads of one tensor and token on their way: kBatch of them in flight per lane.  kPast: see past_caches.
+template <typename T, int D, int LAYOUT, bool kPaged, int kPast>
 struct HeadRows {
   static constexpr int kBatch = 4;
-  typedef Chunk<T, false, false> Ch;
+  typedef Chunk<T, (kPast > 1), (kPast > 0)> Ch;
   static constexpr int VEC = Ch::VEC, CH = D / VEC, TPV = CH / 2;
   const HeadRowsParams &p;
   int kind, c, n;
@@ -154,10 +154,10 @@ struct HeadRows {
 
 // Calls that fill the chip: a lane takes every fourth head of a token's tensors, one tensor after the other.
 // kPaged: keys and values go to their rows of a paged cache.
-template <typename T, int D, int LAYOUT, bool kPaged>
+template <typename T, int D, int LAYOUT, bool kPaged, int kPast>
 __global__ __launch_bounds__(kRotThreads) void head_rows_kernel(HeadRowsParams p, RopeTable rt) {
   using G = RowGeo<T, D, kManySlots>;
-  using Rows = HeadRows<T, D, LAYOUT, kPaged>;
+  using Rows = HeadRows<T, D, LAYOUT, kPaged, kPast>;
   const int c = threadIdx.x % G::TPV, slot = threadIdx.x / G::TPV % kManySlots;
   const int t = blockIdx.x * G::TOK + threadIdx.x / G::TPT;
   if (t >= p.n_tokens) return;
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kRotThreads) void head_rows_kernel(HeadRowsParams p
 template <typename T, int D, int LAYOUT, bool kPaged>
 __global__ __launch_bounds__(kRotThreads) void head_rows_few_kernel(HeadRowsParams p, RopeTable rt) {
   using G = RowGeo<T, D, kFewSlots>;
-  using Rows = HeadRows<T, D, LAYOUT, kPaged>;
+  using Rows = HeadRows<T, D, LAYOUT, kPaged, 0>;
   constexpr int VEC = G::VEC;
   static_assert(G::TPT >= D / 2, "a lane for every pair");
   __shared__ float2 turns[G::TOK][D / 2];
@@ -223,10 +223,10 @@ __global__ __launch_bounds__(kRotThreads) void head_rows_few_kernel(HeadRowsPara
 
 // The first wg_q workgroups take queries, the others keys, a chunk of tokens each and every wg_q-th (n_wg - wg_q-th) after it, and leave
 // their sums of the gain's gradient.  A lane takes every kSlots-th head of its token, the next one's pieces on their way meanwhile.
-template <typename T, int D, int LAYOUT, int kSlots>
+template <typename T, int D, int LAYOUT, int kSlots, int kPast>
 __global__ __launch_bounds__(kRotThreads, 4) void norm_backward_kernel(NormBackwardParams p, RopeTable rt) {
   using G = RowGeo<T, D, kSlots>;
-  typedef Chunk<T, false, false> Ch;
+  typedef Chunk<T, (kPast > 1), (kPast > 0)> Ch;
   constexpr int VEC = G::VEC, CH = G::CH, kVecs = kRotThreads / G::TPV;
   __shared__ float red[kVecs][D];
   const HeadRowsParams &r = p.rows;
@@ -240,10 +240,10 @@ __global__ __launch_bounds__(kRotThreads, 4) void norm_backward_kernel(NormBackw
   };
   auto load = [&](Pieces &w, int64_t t, int h) __attribute__((always_inline)) {
     const T *s = src + t * r.src_st[kind] + h * r.src_sh[kind], *g = grad + t * p.grad_st[kind] + h * p.grad_sh[kind];
-    w.x = *reinterpret_cast<const u32x4_t *>(s);
-    w.y = *reinterpret_cast<const u32x4_t *>(s + (CH / 2) * VEC);
-    w.gx = *reinterpret_cast<const u32x4_t *>(g);
-    w.gy = *reinterpret_cast<const u32x4_t *>(g + (CH / 2) * VEC);
+    w.x = load_row_piece<(kPast > 1)>((const char *)(s));
+    w.y = load_row_piece<(kPast > 1)>((const char *)(s + (CH / 2) * VEC));
+    w.gx = load_row_piece<(kPast > 1)>((const char *)(g));
+    w.gy = load_row_piece<(kPast > 1)>((const char *)(g + (CH / 2) * VEC));
     w.pos = r.positions ? r.positions[t] : (int)t;
   };
   int64_t t = (int64_t)first * G::TOK + threadIdx.x / G::TPT;
@@ -356,6 +356,16 @@ inline bool few_tokens(const HeadRowsParams &p) {
   const int heads = std::max(p.src[kRowsQ] ? p.n_heads[kRowsQ] : 0, p.n_heads[kRowsK]);
   return p.n_tokens <= (heads > kManySlots * 4 ? 2048 : 1024);
 }
+// Which accesses go past the caches, by the bytes that a call reads and writes (`tensors` for each of its own): none, 1 the stores, 2 the
+// loads as well.  us, none / stores / both, 32 over 8 heads of 128, bf16: forward 84 MB 17.0 / 17.5 / 18.5, 168 MB 36.1 / 29.9 / 32.1, 246 MB
+// 50.7 / 47.7 / 45.2, 655 MB 123.5 / 118.1 / 111.8; backward 63 MB 20.2 / 20.4 / 21.6, 126 MB 33.8 / 29.5 / 31.7, 252 MB 58.0 / 56.1 /
+// 53.8, 999 MB 196 / 190 / 184; keys and values into pages 67 MB 13.1 / 13.5 / 15.3, 131 MB 29.9 / 22.8 / 27.1, 260 MB 54.2 / 51.7 / 50.9.
+inline int past_caches(const HeadRowsParams &p, int tensors) {
+  int64_t rows = 0;
+  for (int kind = 0; kind < 3; ++kind) rows += p.src[kind] ? p.n_heads[kind] : 0;
+  const int64_t bytes = rows * p.n_tokens * p.head_dim * (p.dtype == 0 ? 2 : 4) * tensors;
+  return bytes > kCacheBytes * 3 / 4 ? 2 : bytes > kCacheBytes * 3 / 8 ? 1 : 0;
+}
 template <typename T, int D, int LAYOUT, bool kPaged>
 hipError_t launch_rows(const HeadRowsParams &p, const RopeTable &rt, hipStream_t stream) {
   if (few_tokens(p)) {
@@ -363,7 +373,11 @@ hipError_t launch_rows(const HeadRowsParams &p, const RopeTable &rt, hipStream_t
     head_rows_few_kernel<T, D, LAYOUT, kPaged><<<dim3((unsigned)(p.n_tokens + TOK - 1) / TOK, kPaged ? 3 : 2), kRotThreads, 0, stream>>>(p, rt);
   } else {
     constexpr int TOK = RowGeo<T, D, kManySlots>::TOK;
-    head_rows_kernel<T, D, LAYOUT, kPaged><<<(unsigned)((p.n_tokens + (int64_t)TOK - 1) / TOK), kRotThreads, 0, stream>>>(p, rt);
+    const unsigned wgs = (unsigned)((p.n_tokens + (int64_t)TOK - 1) / TOK);
+    const int past = past_caches(p, 2);
+    if (past == 2) head_rows_kernel<T, D, LAYOUT, kPaged, 2><<<wgs, kRotThreads, 0, stream>>>(p, rt);
+    else if (past == 1) head_rows_kernel<T, D, LAYOUT, kPaged, 1><<<wgs, kRotThreads, 0, stream>>>(p, rt);
+    else head_rows_kernel<T, D, LAYOUT, kPaged, 0><<<wgs, kRotThreads, 0, stream>>>(p, rt);
   }
   return hipGetLastError();
 }
@@ -375,11 +389,15 @@ template <typename T, int D, int LAYOUT>
 void launch_back_rows(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream) {
   // us a call, every fourth head / every sixteenth: 32 over 8 heads of 128, bf16, one token 13.1 / 9.6, 256 14.5 / 11.1, 512 15.7 / 13.4, 1,024
   // 18.4 / 18.4, 2,048 21.1 / 24.5; 16 over 8, fp32, 256 10.8 / 9.8, 1,024 15.2 / 16.6; 8 over 2 of 64, fp32, 64 9.0 / 9.0, 512 11.0 / 11.6.
-  const int heads = std::max(p.rows.n_heads[kRowsQ], p.rows.n_heads[kRowsK]);
+  const int heads = std::max(p.rows.n_heads[kRowsQ], p.rows.n_heads[kRowsK]), past = past_caches(p.rows, 3);
   if (p.rows.n_tokens <= (heads > kManySlots * 4 ? 512 : 256))
-    norm_backward_kernel<T, D, LAYOUT, kFewSlots><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
+    norm_backward_kernel<T, D, LAYOUT, kFewSlots, 0><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
+  else if (past == 2)
+    norm_backward_kernel<T, D, LAYOUT, kManySlots, 2><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
+  else if (past == 1)
+    norm_backward_kernel<T, D, LAYOUT, kManySlots, 1><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
   else
-    norm_backward_kernel<T, D, LAYOUT, kManySlots><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
+    norm_backward_kernel<T, D, LAYOUT, kManySlots, 0><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
 }
 template <typename T, int D>
 hipError_t launch_back(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream) {

@@ -586,3 +586,43 @@ def test_a_captured_decoding_step(ba):
         assert torch.equal(caches[0].k_pages, caches[1].k_pages) and torch.equal(caches[0].v_pages, caches[1].v_pages)
         lens += 1
         at += 1
+
+
+@pytest.mark.parametrize("tokens", [6000, 12000])
+def test_calls_larger_than_the_caches_give_the_bits_of_their_parts(ba, tokens):
+    """From 96 MB on stores go past the caches, from 192 MB on loads as well; parts of 2,500 tokens lie below, of 700 in the
+    kernel for few tokens."""
+    import torch
+    heads = ba.Heads(32, 8, 128, 500000.0)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    new = lambda h: torch.randn(tokens, h, 128, generator=gen, device="cuda").bfloat16()  # noqa: E731
+    q, k, gq, gk = new(32), new(8), new(32), new(8)
+    norm = ba.HeadNorm(rand(1, 128) + 1, rand(2, 128) + 1)
+    pos = torch.arange(tokens, dtype=torch.int32, device="cuda") * 3
+    whole = [torch.empty_like(x) for x in (q, k, q, k)]
+    gains = torch.empty(2, 2, 128, device="cuda")
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    ba.ba_norm_rotate(heads, norm, q, k, whole[0], whole[1], pos)
+    ba.ba_norm_rotate_backward(heads, norm, q, k, gq, gk, whole[2], whole[3], gains[0, 0], gains[0, 1], pos, ba.ROPE_APPLY, ws)
+    for size in (2500, 700):
+        sums = torch.zeros(2, 128, dtype=torch.float64, device="cuda")
+        for a in range(0, tokens, size):
+            s = slice(a, min(a + size, tokens))
+            part = [torch.empty_like(x[s]) for x in (q, k, q, k)]
+            ba.ba_norm_rotate(heads, norm, q[s], k[s], part[0], part[1], pos[s])
+            ba.ba_norm_rotate_backward(heads, norm, q[s], k[s], gq[s], gk[s], part[2], part[3], gains[1, 0], gains[1, 1], pos[s], ba.ROPE_APPLY, ws)
+            assert all(torch.equal(x, y[s]) for x, y in zip(part, whole))
+            sums += gains[1].double()
+        # (sums of 100,000 terms and more of random sign, in 32 bits within a workgroup: some hundreds of 2^-24 of their length)
+        assert ((gains[0].double() - sums).norm(dim=1) <= 1e-5 * sums.norm(dim=1)).all()
+    # keys and values of as many bytes into pages
+    n = tokens * 40 // 16
+    k, v = torch.randn(2, n, 8, 128, generator=gen, device="cuda").bfloat16()
+    at = torch.arange(n, dtype=torch.int32, device="cuda")
+    pools = torch.zeros(4, -(-n // 16), 16, 8, 128, dtype=torch.bfloat16, device="cuda")
+    table = torch.arange(pools.shape[1], dtype=torch.int32, device="cuda")[None]
+    ba.ba_paged_append(heads, norm, ba.PagedCache(pools[0], pools[1], table), None, k, v, None, at, torch.zeros_like(at))
+    for a in range(0, n, 4000):
+        s = slice(a, min(a + 4000, n))
+        ba.ba_paged_append(heads, norm, ba.PagedCache(pools[2], pools[3], table), None, k[s], v[s], None, at[s], torch.zeros_like(at[s]))
+    assert torch.equal(pools[0], pools[2]) and torch.equal(pools[1], pools[3])
