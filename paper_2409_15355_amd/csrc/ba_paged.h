@@ -74,6 +74,7 @@ struct PagedAttnParams {
   float *part_ml;           // [part][token][query head][4]: reference in log2 units, sum, what part_o is to be multiplied by
   int64_t part_rows;        // tokens * query heads
   int32_t max_parts;        // of a row
+  int32_t past_caches;      // keys and values are read past the caches
   int32_t direct;           // one part for every row: the result itself
 };
 // Groups of sequences that share a prefix, in the order of their sequences.

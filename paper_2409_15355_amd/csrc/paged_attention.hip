@@ -46,10 +46,26 @@ typedef __attribute__((address_space(3))) f32x4_t lds_f32x4;
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
 typedef const __attribute__((address_space(3))) bf16x8_t lds_bf16x8;
 
-// lds_dma16 with an address per lane: rows of different pages
+// lds_dma16, kPast: past the caches; and with an address per lane (rows of different pages)
+template <bool kPast>
+__device__ __forceinline__ void lds_dma16_page(const char *base, uint32_t offset, uint32_t lds_base) {
+  if constexpr (!kPast) {
+    lds_dma16(base, offset, lds_base);
+  } else {
+    const uint64_t b = (uint64_t)base;
+    const uint64_t bu = ((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) << 32) |
+                        (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+    lds_base = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_base);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt" : : "v"(offset), "s"(bu), "s"(lds_base) : "memory");
+  }
+}
+template <bool kPast>
 __device__ __forceinline__ void lds_dma16_from(const char *from, uint32_t lds_base) {
   lds_base = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_base);
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(lds_base) : "memory");
+  if constexpr (kPast)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(from), "s"(lds_base) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(lds_base) : "memory");
 }
 // value held by lane ^ 16
 __device__ __forceinline__ float other_sixteen(float x) {
@@ -136,6 +152,11 @@ struct PagedSource {
   // N wave instructions of keys and of values, a run's rows; chunks(u, &kchunk, &vchunk): what this lane fetches of its row in the u-th
   template <int N, typename Chunks>
   __device__ __forceinline__ void fetch(const Run &run, int lane_row, uint32_t k_to, uint32_t v_to, Chunks &&chunks) const {
+    if (p.past_caches) fetch_p<N, true>(run, lane_row, k_to, v_to, chunks);
+    else fetch_p<N, false>(run, lane_row, k_to, v_to, chunks);
+  }
+  template <int N, bool kPast, typename Chunks>
+  __device__ __forceinline__ void fetch_p(const Run &run, int lane_row, uint32_t k_to, uint32_t v_to, Chunks &&chunks) const {
     if constexpr (kAligned) {
       const int page = max(0, __builtin_amdgcn_readfirstlane(run.page));
       const char *k0 = k + behind(page, p.k_page_b16, run.row, p.k_rb), *v0 = v + behind(page, p.v_page_b16, run.row, p.v_rb);
@@ -143,8 +164,8 @@ struct PagedSource {
       for (int u = 0; u < N; ++u) {
         uint32_t kc, vc;
         chunks(u, kc, vc);
-        lds_dma16(k0, (uint32_t)(u * G::RPI + lane_row) * p.k_rb + kc, k_to + u * 1024);
-        lds_dma16(v0, (uint32_t)(u * G::RPI + lane_row) * p.v_rb + vc, v_to + u * 1024);
+        lds_dma16_page<kPast>(k0, (uint32_t)(u * G::RPI + lane_row) * p.k_rb + kc, k_to + u * 1024);
+        lds_dma16_page<kPast>(v0, (uint32_t)(u * G::RPI + lane_row) * p.v_rb + vc, v_to + u * 1024);
       }
     } else {
 #pragma unroll
@@ -153,8 +174,8 @@ struct PagedSource {
         chunks(u, kc, vc);
         int row;
         const int page = max(0, page_of(min(run.key + u * G::RPI + lane_row, it.k1 - 1), row));
-        lds_dma16_from(k + behind(page, p.k_page_b16, row, p.k_rb) + kc, k_to + u * 1024);
-        lds_dma16_from(v + behind(page, p.v_page_b16, row, p.v_rb) + vc, v_to + u * 1024);
+        lds_dma16_from<kPast>(k + behind(page, p.k_page_b16, row, p.k_rb) + kc, k_to + u * 1024);
+        lds_dma16_from<kPast>(v + behind(page, p.v_page_b16, row, p.v_rb) + vc, v_to + u * 1024);
       }
     }
   }
