@@ -200,8 +200,23 @@ void plan_paged(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, 
   auto chunk_of = [&](int64_t keys, int64_t least, int64_t most) {
     return (int32_t)std::min(most, std::max(least, (keys + 63) / 64 * 64));
   };
-  pl->chunk = chunk_of((prefix_work + own_work / 4) / slots, 128, kPagedMaxChunk);
-  pl->own_chunk = chunk_of((prefix_work + own_work) / (4 * slots), std::max<int64_t>(64, std::min<int64_t>(512, nq * G * 8)), 1024);
+  // One item a slot: each costs about as much as 100 keys of its own, so where the least chunks together are more than one
+  // round of the slots, they are doubled.  With that and without (us; calls of 8 key heads and 4 query heads each, one token a
+  // sequence): 16 sequences of 1,000 keys 16.9 and 23.8, 4 of 4,000 16.8 and 25.4, 1 of 16,000 13.9 and 16.2; 2 groups of 12
+  // after 4,000 keys 22 and 26.  A round of small ones is faster: 1 sequence of 2,000 keys 10.7 in 264 items, 11.1 in 136; 1
+  // of 4,000 with 8 tokens 17.6 in 504, 18.1 in 128.  The many-row walk reads a chunk in tiles of 32 keys behind barriers
+  // and writes more rows: 64 tokens of 4,000 keys 22.5 with 256 keys a chunk, 26.2 with 128.
+  // A call of one part needs no merge (3 us and more).  In one part and in several: 1 sequence of 250 keys 8.2 and 9.7, of 380
+  // 9.4 and 9.6, of 500 10.5 and 10.1; 16 of 500 11.4 and 14.5, of 1,020 16.4 and 19.2; with 16 tokens each 1 of 400
+  // keys 25.5 and 17.4, 16 of 380 23.8 and 26.2, of 1,000 41.3 and 37.5.
+  const int64_t rows = (int64_t)nq * G, walks = pl->n_seqs * hkv * pl->own_row_tiles;
+  const bool one_part = prefix_work == 0 && ((max_len <= 384 && rows <= 16) ||
+                                             (max_len <= (rows <= kPagedStreamRows ? 1024 : 512) && walks >= cus / 2));
+  const bool one_round = prefix_work / 128 + own_work / 64 <= slots;
+  const int64_t least_own = one_part ? max_len / 64 * 64 + 64 : one_round ? 64 : rows <= kPagedStreamRows ? 128 : 256;
+  // (the keys of the sequences' own are mostly fewer than max_len bounds them to: they weigh less where prefixes are cut)
+  pl->chunk = chunk_of((prefix_work + own_work / 4) / slots, one_round ? 128 : 256, kPagedMaxChunk);
+  pl->own_chunk = chunk_of((prefix_work + own_work) / slots, least_own, 1024);
   auto splits = [&](int64_t keys, int64_t chunk) { return (int32_t)((keys + chunk - 1) / chunk); };
   pl->own_splits = splits(max_len - least_prefix / 16 * 16, pl->own_chunk);
   pl->parts = least_prefix == 0 ? pl->own_splits : 0;

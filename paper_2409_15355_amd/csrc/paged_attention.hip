@@ -878,11 +878,13 @@ hipError_t launch_merge_w(const PagedAttnParams &p, const Groups &g, hipStream_t
   paged_merge_kernel<D, kWays, Groups><<<(unsigned)wgs, kMergeThreads, 0, stream>>>(p, g);
   return hipGetLastError();
 }
-// As many ways as leave each two parts, in launches that the chip holds at a time.
+// By rows and parts, us with 1 / 4 / 16 ways: 32 rows of 33 parts 8.0 / 4.5 / 4.4, of 250 39 / 14.4 / 6.0; 128 of 63 11.4 / 5.5 / 4.7; 512 of
+// 16 4.8 / 4.8 / 4.8, of 64 11.9 / 6.0 / 5.7; 1,024 of 64 11.8 / 6.6 / 8.0; 2,048 of 33 7.8 / 6.4 / 10.1; 3,072 of 9 5.5 / 5.5 / 12.0; 4,096 of 17 7.5 /
+// 8.2 / 15.1; 8,192 of 2 5.0 / 8.6 / 18.4.
 template <int D, typename Groups>
 hipError_t launch_merge_d(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
-  if (p.max_parts >= 32 && p.part_rows <= 1024) return launch_merge_w<D, 16>(p, g, stream);
-  if (p.max_parts >= 8 && p.part_rows <= 4096) return launch_merge_w<D, 4>(p, g, stream);
+  if (p.max_parts >= 32 && p.part_rows <= 512) return launch_merge_w<D, 16>(p, g, stream);
+  if (p.max_parts >= 8 && p.part_rows <= 2048) return launch_merge_w<D, 4>(p, g, stream);
   return launch_merge_w<D, 1>(p, g, stream);
 }
 

@@ -453,6 +453,19 @@ def test_paged_attention_long_and_cut_into_parts(ba):
     attention_case(ba, 72, 4, 4, 64, 32, [7003, 6500, 6400], groups=[(3, 6399)])
 
 
+@pytest.mark.parametrize("n,nq,max_len", [(1, 1, 384), (1, 1, 385), (3, 2, 383), (1, 5, 300), (70, 1, 1000), (70, 1, 1024), (70, 1, 1025),
+                                          (20, 9, 500), (20, 13, 512), (20, 13, 600), (2, 30, 2100)])
+def test_paged_attention_in_one_part_or_several(ba, n, nq, max_len):
+    """Lengths around those where a call is cut, one of them the bound itself."""
+    rng = np.random.default_rng(max_len + nq)
+    attention_case(ba, 80 + n, 8, 2, 64, 32, [max_len] + [int(x) for x in rng.integers(0, max_len + 1, n - 1)], nq=nq)
+
+
+@pytest.mark.parametrize("groups", [None, [(3, 0)]])
+def test_paged_attention_of_a_bound_of_zero(ba, groups):
+    attention_case(ba, 79, 8, 2, 64, 16, [5, 0, 1], nq=2, groups=groups, max_len=0)
+
+
 def test_paged_attention_lengths_beyond_the_bound_count_as_the_bound(ba):
     attention_case(ba, 73, 8, 2, 64, 16, [50, 10, 80], max_len=50)
 
