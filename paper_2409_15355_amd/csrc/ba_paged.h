@@ -45,7 +45,10 @@ hipError_t launch_norm_rotate_backward(const NormBackwardParams &p, const RopeTa
 
 // ---------------------------------------------------------------- attention over pages ----------
 constexpr int kPagedTileRows = 128;    // rows of a work item
-constexpr int kPagedStreamRows = 48;   // ... up to this many in a problem: all of them
+// ... up to this many in a problem: all of them, and the walk for few rows.  us, that walk and the one for many: 16 sequences of 2,000 keys,
+// 8 key heads of 128: 20 rows 34 / 35, 32 rows 36 / 37, 48 rows 41 / 39; 1 of 4,000: 20 rows 17.1 / 15.6, 32 rows 17.9 / 18.0, 48 rows 22 / 19; 64 of 4,000:
+// 32 rows 201 / 204, 48 rows 218 / 217.
+constexpr int kPagedStreamRows = 32;
 BA_HD int paged_tile_rows(int n_rows) { return n_rows > kPagedStreamRows ? kPagedTileRows : kPagedStreamRows; }
 constexpr int kPagedMaxChunk = 2048;  // keys of a work item at most: its part of the page table lies in LDS
 

@@ -257,7 +257,6 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem 
   auto issue = [&](int i, const auto &run) __attribute__((always_inline)) {
     const uint32_t to = (uint32_t)(uintptr_t)smem + ring + (uint32_t)(i % NB) * (2 * TB);
     int ln = lane;
-    if (RG > 2) asm volatile("" : "+v"(ln));  // (worked out anew: kept, the offsets take registers that the sums need)
     src.template fetch<OPS>(run, ln / G::CPR, to, to + TB, [&](int u, uint32_t &kchunk, uint32_t &vchunk) __attribute__((always_inline)) {
       const int line = (u * G::RPI + ln / G::CPR) / G::LPR, pos = ln % G::CPR;
       kchunk = (uint32_t)(pos ^ (line & (G::CPR - 1))) << 4;
@@ -314,7 +313,6 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem 
     for (int kk = 0; kk < KK; ++kk) kf[kk] = *(lds_bf16x8 *)(smem + (k_rd[kk] + buf));
     s16x4_t vf[DS];
     uint32_t swz = v_swz;
-    if (RG > 2) asm volatile("" : "+v"(swz));
     auto v_frag = [&](int ds) __attribute__((always_inline)) {
       return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(smem + (v_rd + buf + ((ds ^ swz) << 5))));
     };
@@ -407,7 +405,6 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem 
           }
         }
       }
-      if (RG > 1) __builtin_amdgcn_sched_barrier(0);  // (one group of rows after the other: together they need more registers than there are)
     }
   }
 
@@ -740,7 +737,6 @@ __global__ __launch_bounds__(kPThreads, 2) void paged_attn_kernel(PagedAttnParam
   };
   const int rows = it.n_rows - it.row0;
   if (it.n_rows > kPagedStreamRows) walk_shared<D, kAligned>(p, it, smem, lane, wave, stage);
-  else if (rows > 32) walk_stream<D, kAligned, 3>(p, it, smem, lane, wave, stage);
   else if (rows > 16) walk_stream<D, kAligned, 2>(p, it, smem, lane, wave, stage);
   else walk_stream<D, kAligned, 1>(p, it, smem, lane, wave, stage);
 }
@@ -879,7 +875,7 @@ hipError_t launch_merge_w(const PagedAttnParams &p, const Groups &g, hipStream_t
   return hipGetLastError();
 }
 // By rows and parts, us with 1 / 4 / 16 ways: 32 rows of 33 parts 8.0 / 4.5 / 4.4, of 250 39 / 14.4 / 6.0; 128 of 63 11.4 / 5.5 / 4.7; 512 of
-// 16 4.8 / 4.8 / 4.8, of 64 11.9 / 6.0 / 5.7; 1,024 of 64 11.8 / 6.6 / 8.0; 2,048 of 33 7.8 / 6.4 / 10.1; 3,072 of 9 5.5 / 5.5 / 12.0; 4,096 of 17 7.5 /
+// 16 4.8 / 4.8 / 4.8, of 64 11.9 / 6.0 / 5.7; 1,024 of 64 11.8 / 6.6 / 8.0; 2,048 of 33 7.8 / 6.4 / 10.1; 4,096 of 17 7.5 /
 // 8.2 / 15.1; 8,192 of 2 5.0 / 8.6 / 18.4.
 template <int D, typename Groups>
 hipError_t launch_merge_d(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
