@@ -460,7 +460,8 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem 
 // A key is read from memory once for 128 rows, and from LDS once for 32.  32 over 8 heads of 128, 64 sequences on 31,744 keys: 33.4 GFLOP in
 // 58.7 us, 570 TFLOP/s; matrix, vector and LDS instructions take 30 to 45 us each, and two waves a SIMD cover each other's only in part (the
 // tile behind a barrier, the softmax between two products).  Three workgroups a compute unit need 168 registers and 48 KB: 512 rows 87 us
-// against 91, but 256 rows 58.5 against 51.9; eight waves that take turns at the matrix units, with 64 keys a tile: 58.4 against 58.2.
+// against 91, but 256 rows 58.5 against 51.9; eight waves that take turns at the matrix units, with 64 keys a tile: 58.4 against 58.2.  The next tile's
+// score products between this one's exponentials: no change.
 template <int D, bool kAligned, typename Stage>
 __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, PagedItem &it, lds_char *smem, int lane, int wave, Stage &&stage) {
   using G = PGeo<D>;
