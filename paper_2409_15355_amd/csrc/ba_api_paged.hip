@@ -102,6 +102,13 @@ int32_t check_apart(const ba_tensor *a, const char *a_name, int a_heads, const b
 // other: so are the bits of its gain's gradient).
 void backward_wgs(int64_t tokens, const ba_heads *h, bool q, bool k, NormBackwardParams *p) {
   const int64_t hq = h->n_q_heads, all = hq + h->n_kv_heads;
+  p->heads = h->n_q_heads;
+  p->one_each = tokens * hq * h->head_dim * (p->rows.dtype == 0 ? 2 : 4) <= kNormBwdOneWgBytes;
+  if (p->one_each) {
+    p->wg_q = q;
+    p->n_wg = (int)q + k;
+    return;
+  }
   p->wg_q = q ? (int32_t)std::min<int64_t>(tokens, kNormBwdMaxWg * hq / all) : 0;
   p->n_wg = p->wg_q + (k ? (int32_t)std::min<int64_t>(tokens, std::max<int64_t>(1, kNormBwdMaxWg * (all - hq) / all)) : 0);
 }

@@ -39,15 +39,21 @@ struct NormBackwardParams {
   float *weight_grad[2];  // device [D], nullable
   float *partial;         // [workgroups][D]
   int32_t wg_q, n_wg;     // workgroups for the queries, and all of them
+  int32_t heads;          // the most of a tensor, also of one that is not there
+  int32_t one_each;       // one for each tensor: its sums are the gradient
 };
 constexpr int kNormBwdMaxWg = 1024;
+// Queries of this many bytes at most: a workgroup for each tensor, and no second launch for the gains' gradients.  us a call, one each / many: 32
+// heads of 128, bf16, 1 token 5.9 / 10.8, 4 (32 KB) 7.4 / 10.0, 6 9.1 / 10.1, 8 10.8 / 10.0; fp32, 2 (32 KB) 6.2 / 9.6; 4 heads of 64, bf16, 64 tokens
+// (32 KB) 8.6 / 10.2.
+constexpr int64_t kNormBwdOneWgBytes = 32768;
 hipError_t launch_norm_rotate_backward(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream);
 
 // ---------------------------------------------------------------- attention over pages ----------
 constexpr int kPagedTileRows = 128;    // rows of a work item
-// ... up to this many in a problem: all of them, and the walk for few rows.  us, that walk and the one for many: 16 sequences of 2,000 keys,
-// 8 key heads of 128: 20 rows 34 / 35, 32 rows 36 / 37, 48 rows 41 / 39; 1 of 4,000: 20 rows 17.1 / 15.6, 32 rows 17.9 / 18.0, 48 rows 22 / 19; 64 of 4,000:
-// 32 rows 201 / 204, 48 rows 218 / 217.
+// ... up to this many in a problem: all of them, and the walk for few rows.  us, that walk and the one for many, 8 key heads of 128:
+// 16 sequences of 2,000 keys, 20 rows 34 / 35, 32 rows 36 / 37, 48 rows 41 / 39; 1 of 4,000, 20 rows 17.1 / 15.6, 32 rows 17.9 / 18.0, 48
+// rows 22 / 19; 64 of 4,000, 32 rows 201 / 204, 48 rows 218 / 217.
 constexpr int kPagedStreamRows = 32;
 BA_HD int paged_tile_rows(int n_rows) { return n_rows > kPagedStreamRows ? kPagedTileRows : kPagedStreamRows; }
 constexpr int kPagedMaxChunk = 2048;  // keys of a work item at most: its part of the page table lies in LDS

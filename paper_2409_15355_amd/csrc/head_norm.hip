@@ -225,7 +225,8 @@ __global__ __launch_bounds__(kRotThreads) void head_rows_few_kernel(HeadRowsPara
 }
 
 // The first wg_q workgroups take queries, the others keys, a chunk of tokens each and every wg_q-th (n_wg - wg_q-th) after it, and leave
-// their sums of the gain's gradient.  A lane takes every kSlots-th head of its token, the next one's pieces on their way meanwhile.
+// their sums of the gain's gradient (one workgroup for each tensor: the gradient itself).  A lane takes every kSlots-th head of its token,
+// the next one's pieces on their way meanwhile.
 template <typename T, int D, int LAYOUT, int kSlots, int kPast>
 __global__ __launch_bounds__(kRotThreads, 4) void norm_backward_kernel(NormBackwardParams p, RopeTable rt) {
   using G = RowGeo<T, D, kSlots>;
@@ -320,7 +321,8 @@ __global__ __launch_bounds__(kRotThreads, 4) void norm_backward_kernel(NormBackw
     float sum = 0.f;
 #pragma unroll
     for (int v = 0; v < kVecs; ++v) sum += red[v][threadIdx.x];
-    p.partial[(int64_t)blockIdx.x * D + threadIdx.x] = sum;
+    if (!p.one_each) p.partial[(int64_t)blockIdx.x * D + threadIdx.x] = sum;
+    else if (p.weight_grad[kind]) p.weight_grad[kind][threadIdx.x] = sum;
   }
 }
 
@@ -392,8 +394,8 @@ template <typename T, int D, int LAYOUT>
 void launch_back_rows(const NormBackwardParams &p, const RopeTable &rt, hipStream_t stream) {
   // us a call, every fourth head / every sixteenth: 32 over 8 heads of 128, bf16, one token 13.1 / 9.6, 256 14.5 / 11.1, 512 15.7 / 13.4, 1,024
   // 18.4 / 18.4, 2,048 21.1 / 24.5; 16 over 8, fp32, 256 10.8 / 9.8, 1,024 15.2 / 16.6; 8 over 2 of 64, fp32, 64 9.0 / 9.0, 512 11.0 / 11.6.
-  const int heads = std::max(p.rows.n_heads[kRowsQ], p.rows.n_heads[kRowsK]), past = past_caches(p.rows, 3);
-  if (p.rows.n_tokens <= (heads > kManySlots * 4 ? 512 : 256))
+  const int heads = p.heads, past = past_caches(p.rows, 3);
+  if (p.one_each ? heads > 2 * kManySlots : p.rows.n_tokens <= (heads > kManySlots * 4 ? 512 : 256))
     norm_backward_kernel<T, D, LAYOUT, kFewSlots, 0><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
   else if (past == 2)
     norm_backward_kernel<T, D, LAYOUT, kManySlots, 2><<<p.n_wg, kRotThreads, 0, stream>>>(p, rt);
@@ -410,6 +412,7 @@ hipError_t launch_back(const NormBackwardParams &p, const RopeTable &rt, hipStre
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
+  if (p.one_each || (!p.weight_grad[0] && !p.weight_grad[1])) return hipSuccess;
   gain_sums_kernel<D><<<2 * D / kGainCols, kGainThreads, 0, stream>>>(p);
   return hipGetLastError();
 }

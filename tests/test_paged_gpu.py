@@ -181,6 +181,37 @@ def test_norm_rotate_backward(ba, hq, hkv, d, tokens, layout, mode, dtype):
     assert torch.equal(dwk2, dwk) and torch.equal(dk2, dk)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hq,hkv,d,tokens", [(32, 8, 128, 2), (32, 8, 128, 3), (32, 8, 128, 4), (32, 8, 128, 5), (8, 2, 64, 16), (8, 2, 64, 17),
+                                             (8, 2, 64, 33), (7, 7, 64, 11), (16, 1, 128, 1), (1, 1, 64, 256), (1, 1, 64, 257), (40, 2, 128, 1),
+                                             (32, 8, 128, 300)])
+def test_norm_rotate_backward_of_few_tokens(ba, hq, hkv, d, tokens, dtype):
+    """Around the size from which the gains' gradients take a launch of their own.  Few terms: a rotation's error goes with its pair's
+    length, however small the element that comes out."""
+    import torch
+    heads = ba.Heads(hq, hkv, d, 10000.0, rope_layout=0)
+    q, k = rand(31, tokens, hq, d, scale=2.0, dtype=dtype), rand(32, tokens, hkv, d, scale=0.2, dtype=dtype)
+    gq, gk = rand(33, tokens, hq, d, scale=0.1, dtype=dtype), rand(34, tokens, hkv, d, dtype=dtype)
+    wq, wk = (rand(s, d, scale=0.3, dtype="f32") + 1 for s in (35, 36))
+    pos = np.random.default_rng(37).integers(0, 30000, tokens)
+    dq, dk = torch.full_like(q, float("nan")), torch.full_like(k, float("nan"))
+    dwq, dwk = torch.full((d,), float("nan"), device="cuda"), torch.full((d,), float("nan"), device="cuda")
+    ws = torch.empty(ba.ba_norm_rotate_backward_workspace_bytes(heads, tokens), dtype=torch.uint8, device="cuda")
+    norm = ba.HeadNorm(wq, wk, 1e-6)
+    ba.ba_norm_rotate_backward(heads, norm, q, k, gq, gk, dq, dk, dwq, dwk, ints(pos), ba.ROPE_APPLY, ws)
+    for x, w, g, dx, dw in ((q, wq, gq, dq, dwq), (k, wk, gk, dk, dwk)):
+        g64 = rotate64(f64(g), -pos, 10000.0, 0)
+        ref, ref_w, size, _ = norm_back64(f64(x), f64(w), 1e-6, g64)
+        size_w = norm_back64(f64(x), f64(w), 1e-6, pair_size(f64(g), 0))[3]
+        assert (np.abs(f64(dx) - ref) <= 8e-6 * size + (BF16_STEP * np.abs(ref) if dtype == "bf16" else 0.0)).all()
+        assert (np.abs(f64(dw) - ref_w) <= 4e-6 * size_w).all()
+    dq2, dk2, dwk2 = gq.clone(), gk.clone(), torch.empty_like(dwk)
+    ba.ba_norm_rotate_backward(heads, norm, q, k, dq2, dk2, dq2, dk2, None, None, ints(pos), ba.ROPE_APPLY, ws)
+    assert torch.equal(dq2, dq) and torch.equal(dk2, dk)
+    ba.ba_norm_rotate_backward(heads, norm, None, k, None, gk, None, dk2, None, dwk2, ints(pos), ba.ROPE_APPLY, ws)
+    assert torch.equal(dwk2, dwk) and torch.equal(dk2, dk)
+
+
 def test_norm_rotate_backward_against_differences(ba):
     """Directional differences of the 32-bit forward pass, step 2^-8: their own error is some h^2 of the gradient's size
     (curvature of the norm) and 2^-24 / h of the outputs' (rounding), below 1e-3 of it together."""
