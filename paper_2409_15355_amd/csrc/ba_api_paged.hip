@@ -209,12 +209,12 @@ void plan_paged(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, 
   };
   // One item a slot: each costs about as much as 100 keys of its own, so where the least chunks together are more than one
   // round of the slots, they are doubled.  With that and without (us; calls of 8 key heads and 4 query heads each, one token a
-  // sequence): 16 sequences of 1,000 keys 16.9 and 23.8, 4 of 4,000 16.8 and 25.4, 1 of 16,000 13.9 and 16.2; 2 groups of 12
-  // after 4,000 keys 22 and 26.  A round of small ones is faster: 1 sequence of 2,000 keys 10.7 in 264 items, 11.1 in 136; 1
+  // sequence): 16 sequences of 1,000 keys 16.9 and 23.8, 4 of 4,000 16.8 and 25.4, 1 of 16,000 13.9 and 16.2; 4 groups of 32
+  // after 6,000 keys (2 key heads of 64) 17 and 22.  A round of small ones is faster: 1 sequence of 2,000 keys 10.7 in 264 items, 11.1 in 136; 1
   // of 4,000 with 8 tokens 17.6 in 504, 18.1 in 128.  The many-row walk reads a chunk in tiles of 32 keys behind barriers
   // and writes more rows: 64 tokens of 4,000 keys 22.5 with 256 keys a chunk, 26.2 with 128.
   // A call of one part needs no merge (3 us and more).  In one part and in several: 1 sequence of 250 keys 8.2 and 9.7, of 380
-  // 9.4 and 9.6, of 500 10.5 and 10.1; 16 of 500 11.4 and 14.5, of 1,020 16.4 and 19.2; with 16 tokens each 1 of 400
+  // 9.4 and 9.6, of 500 10.5 and 10.1; 16 of 500 11.4 and 14.5, of 1,020 16.4 and 19.2; with 32 tokens each 1 of 400
   // keys 25.5 and 17.4, 16 of 380 23.8 and 26.2, of 1,000 41.3 and 37.5.
   const int64_t rows = (int64_t)nq * G, walks = pl->n_seqs * hkv * pl->own_row_tiles;
   const bool one_part = prefix_work == 0 && ((max_len <= 384 && rows <= 16) ||
