@@ -223,7 +223,11 @@ void plan_paged(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, 
   const int64_t least_own = one_part ? max_len / 64 * 64 + 64 : one_round ? 64 : rows <= kPagedStreamRows ? 128 : 256;
   // (the keys of the sequences' own are mostly fewer than max_len bounds them to: they weigh less where prefixes are cut)
   pl->chunk = chunk_of((prefix_work + own_work / 4) / slots, one_round ? 128 : 256, kPagedMaxChunk);
-  pl->own_chunk = chunk_of((prefix_work + own_work) / slots, least_own, 1024);
+  // Cut at 1,024 keys so that ragged lengths even out (32 sequences of up to 8,000 keys, 4 tokens each 97 us, at 2,048 103, 8 tokens 106 and
+  // 113), at 2,048 where that still makes more than two rounds, and rows enough that an item's start and end count (128 of 500 to 3,000
+  // keys, 8 tokens 196 and 188, 48 of 500 to 6,000, 16 tokens 167 and 162; 256 of up to 2,000, one token 182 and 179; 128 of up to 8,000 328 and 330).
+  const int64_t most_own = rows > 16 && own_work > 2048 * 2 * slots ? 2048 : 1024;
+  pl->own_chunk = chunk_of((prefix_work + own_work) / slots, least_own, most_own);
   auto splits = [&](int64_t keys, int64_t chunk) { return (int32_t)((keys + chunk - 1) / chunk); };
   pl->own_splits = splits(max_len - least_prefix / 16 * 16, pl->own_chunk);
   pl->parts = least_prefix == 0 ? pl->own_splits : 0;

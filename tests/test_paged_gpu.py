@@ -492,6 +492,13 @@ def test_paged_attention_in_one_part_or_several(ba, n, nq, max_len):
     attention_case(ba, 80 + n, 8, 2, 64, 32, [max_len] + [int(x) for x in rng.integers(0, max_len + 1, n - 1)], nq=nq)
 
 
+@pytest.mark.parametrize("nq,rows", [(5, 1), (5, 16), (13, 48)])
+def test_paged_attention_in_the_longest_parts(ba, nq, rows):
+    """Many sequences under a long bound, few of which come near it."""
+    rng = np.random.default_rng(nq)
+    attention_case(ba, 90 + nq, 8, 2, 64, rows, [8200, 4097, 2049] + [int(x) for x in rng.integers(0, 30, 130)], nq=nq)
+
+
 @pytest.mark.parametrize("groups", [None, [(3, 0)]])
 def test_paged_attention_of_a_bound_of_zero(ba, groups):
     attention_case(ba, 79, 8, 2, 64, 16, [5, 0, 1], nq=2, groups=groups, max_len=0)
