@@ -190,17 +190,22 @@ struct PagedSource {
 };
 __device__ __forceinline__ uint32_t below(int lim) { return lim <= 0 ? 0u : lim >= 32 ? ~0u : (1u << lim) - 1u; }
 
-// A row's result: E consecutive dimensions of it at a time, of D.  top: the largest size among all D of o.
+// A row's result: E consecutive dimensions of it at a time, of D.  top: the largest finite size among all D of o.
 // Parts are kept as fp16, divided by their sum and by a power of two that brings the largest into [2^13, 2^14): 2^-11 of an element at
 // most, an eighth of what the result's own rounding to bf16 may take, and half the memory traffic of 32 bits (64 sequences over
 // 31,744 shared keys, 32 over 8 heads of 128: 33 MB out and in again, of 130 MB of keys and values).
 struct RowEnd {
   float m, l, inv, mult, scale;
 };
+// (An infinity or a NaN in one dimension stays what it is, and the others keep their power of two.)
+__device__ __forceinline__ float finite_size(float x) {
+  const float a = fabsf(x);
+  return a < INFINITY ? a : 0.f;
+}
 __device__ __forceinline__ RowEnd row_end(const PagedAttnParams &p, float m, float l, float top) {
   RowEnd e = {m, l, l == 0.f ? 0.f : 1.f / l, 1.f, 1.f};
   if (!p.direct) {
-    const int exp = max(-100, __builtin_amdgcn_frexp_expf(top * e.inv));  // (0 of an infinity or a NaN, which stay what they are)
+    const int exp = max(-100, __builtin_amdgcn_frexp_expf(top * e.inv));
     e.mult = e.inv * __builtin_ldexpf(1.f, 14 - exp);
     e.scale = __builtin_ldexpf(1.f, exp - 14);
   }
@@ -449,7 +454,7 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem 
     }
     float top = 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(acc[e]));
+    for (int e = 0; e < E; ++e) top = fmaxf(top, finite_size(acc[e]));
     const RowEnd end = row_end(p, m, lsum, max_over_sixteen(top));
     const int r = it.row0 + g * 16 + row;
     if (r < it.n_rows) write_row<D, E>(p, it, paged_row(p, it, r), end, d, acc, d == 0);
@@ -664,7 +669,7 @@ __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, PagedItem 
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) top = fmaxf(top, fabsf(oacc[dt][v]));
+    for (int v = 0; v < 16; ++v) top = fmaxf(top, finite_size(oacc[dt][v]));
   const RowEnd end = row_end(p, mb, l_run + other_half(l_run), fmaxf(top, other_half(top)));
   if (wave_row0 + col >= it.n_rows) return;
 #pragma unroll

@@ -1,0 +1,60 @@
+"""What the paged attention and the head norms do at their edges: values that are not finite, outputs in place or among other tensors'
+heads, and the forms of the walks that the other tests do not reach.  Tolerances as in test_paged_gpu.py: a result's rounding
+to bf16, the rounding of the probabilities to bf16, that of the parts of a call to fp16 (2^-11 of sum p |v|, a small share of
+what the probabilities are allowed)."""
+import math
+
+import numpy as np
+import pytest
+
+from test_paged_gpu import BF16_STEP, attend64, attention_case, f64, ints, paged, pools, put, rand
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def ba():
+    import torch
+    assert torch.cuda.is_available(), "GPU tests need a GPU"
+    from paper_2409_15355_amd import binding
+    binding.load()
+    return binding
+
+
+def workspace(ba, heads, n, nq, max_len, cu=None, prefix=None):
+    import torch
+    return torch.empty(max(256, ba.ba_paged_attention_workspace_bytes(heads, n, nq, max_len, cu, prefix)), dtype=torch.uint8, device="cuda")
+
+
+def close(got, ref, size):
+    return (np.abs(got - ref) <= BF16_STEP * (np.abs(ref) + size) + 1e-5).all()
+
+
+# ---- values that are not finite -----------------------------------------------------------------------------------
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("hq,hkv,d,nq", [(8, 2, 128, 1), (8, 2, 64, 5), (8, 2, 128, 12)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_a_value_that_is_not_finite_stays_in_its_dimension(ba, hq, hkv, d, nq, bad, shared):
+    """One element of one value row, in a call of many parts; the others are of a size that fp16 does not hold when it is brought to
+    2^14 by mistake."""
+    import torch
+    n, lens, rows, at, dim = 2, [2000, 2000], 16, 500, 5
+    heads = ba.Heads(hq, hkv, d, 10000.0)
+    k, v = rand(1, 2000, hkv, d), rand(2, 2000, hkv, d) * 3 + 10
+    q = rand(3, n * nq, hq, d)
+    v[at, 0, dim] = bad
+    kp, vp = k.view(125, rows, hkv, d), v.view(125, rows, hkv, d)
+    cache = ba.PagedCache(kp, vp, ints(np.tile(np.arange(125), (n, 1))))
+    cu, prefix = ([0, 2], [1900]) if shared else (None, None)
+    o = torch.full_like(q, 7.0)
+    ba.ba_paged_attention(heads, cache, q, o, None, ints(lens), 2000, cu, prefix, nq, workspace(ba, heads, n, nq, 2000, cu, prefix))
+    v64 = f64(v)
+    v64[at, 0, dim] = 0.0
+    for row in range(n * nq):
+        end = 2000 - nq + row % nq + 1
+        ref, _, size = attend64(f64(q)[row], f64(k)[:end], v64[:end], 1 / math.sqrt(d))
+        got = f64(o)[row]
+        hit = np.zeros_like(got, dtype=bool)
+        hit[: hq // hkv, dim] = True
+        assert (np.isnan(got[hit]).all() if math.isnan(bad) else (got[hit] == bad).all())
+        assert np.isfinite(got[~hit]).all() and close(got[~hit], ref[~hit], size[~hit])
