@@ -30,7 +30,7 @@ namespace {
 
 constexpr int kPWaves = 4;
 constexpr int kPThreads = kPWaves * 64;
-constexpr float kRebaseAbove = 1099511627776.0f;  // 2^40: a tile sum beyond this moves the reference
+constexpr float kRebaseAbove = 1099511627776.0f;  // 2^40: a lane's sum over a tile beyond this moves the row's reference
 constexpr int kTilesB = 65536;                    // LDS of the tiles, then the page table's part
 
 template <int D>
@@ -373,11 +373,11 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem 
         sum = (e4[0] + e4[1]) + (e4[2] + e4[3]);
       };
       exponentials();
-      if (__builtin_amdgcn_ballot_w64(!(sum < kRebaseAbove)) != 0) {
-        // (only the rows concerned: what another row's scores are changes no bit of this one)
-        float all = sum + other_sixteen(sum);
-        all += other_half(all);
-        const float m = !(all < kRebaseAbove) ? fmaxf(row_max(), mb[g]) : mb[g];
+      const uint64_t above = __builtin_amdgcn_ballot_w64(!(sum < kRebaseAbove));
+      if (above != 0) {
+        // (the rows of these lanes and no others: what another row's scores are changes no bit of this one)
+        const uint32_t rows = (uint32_t)above | (uint32_t)(above >> 32);
+        const float m = ((rows | rows >> 16) >> col) & 1 ? fmaxf(row_max(), mb[g]) : mb[g];
         const float alpha = m == mb[g] ? 1.f : __builtin_amdgcn_exp2f(mb[g] - m);
         mb[g] = m;
         l[g] *= alpha;
@@ -572,9 +572,10 @@ __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, PagedItem 
       sum = s0 + s1;
     };
     powers();
-    if (__builtin_amdgcn_ballot_w64(!(sum < kRebaseAbove)) != 0) {
-      // (only the rows concerned: what another row's scores are changes no bit of this one)
-      const float m = !(sum + other_half(sum) < kRebaseAbove) ? fmaxf(row_max(), mb) : mb;
+    const uint64_t above = __builtin_amdgcn_ballot_w64(!(sum < kRebaseAbove));
+    if (above != 0) {
+      // (the rows of these lanes and no others: what another row's scores are changes no bit of this one)
+      const float m = (((uint32_t)above | (uint32_t)(above >> 32)) >> col) & 1 ? fmaxf(row_max(), mb) : mb;
       const float alpha = m == mb ? 1.f : __builtin_amdgcn_exp2f(mb - m);
       mb = m;
       l_run *= alpha;

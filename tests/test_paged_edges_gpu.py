@@ -58,3 +58,34 @@ def test_a_value_that_is_not_finite_stays_in_its_dimension(ba, hq, hkv, d, nq, b
         hit[: hq // hkv, dim] = True
         assert (np.isnan(got[hit]).all() if math.isnan(bad) else (got[hit] == bad).all())
         assert np.isfinite(got[~hit]).all() and close(got[~hit], ref[~hit], size[~hit])
+
+
+# ---- one row's bits and another's scores ----------------------------------------------------------------------------
+@pytest.mark.parametrize("hq", [4, 20, 40])
+def test_no_score_changes_the_bits_of_another_row(ba, hq):
+    """Row 0's exponentials come near the bound from which a row's reference is raised, lane by lane, and add up to more; row 1's pass it by
+    far, or do not.  128 sequences and more: calls in one part, so that these keys are not the first of theirs."""
+    import torch
+    d, n, length = 64, 130, 96
+    heads = ba.Heads(hq, 1, d, softmax_scale=1.0)
+    k = torch.zeros(length, 1, d)
+    if hq <= 32:
+        k[[64, 68, 72, 76], 0, 0] = 27.5   # 2^39.7 in each of four lanes
+    else:
+        k[[64, 68], 0, 0] = 27.5           # ... of two
+    k[65, 0, 1] = 60.0
+    k, v = k.bfloat16().cuda(), rand(5, length, 1, d)
+    kp, vp = k.view(6, 16, 1, d), v.view(6, 16, 1, d)
+    cache = ba.PagedCache(kp, vp, ints(np.tile(np.arange(6), (n, 1))))
+    assert ba.ba_paged_attention_workspace_bytes(heads, n, 1, length) == 0  # (one part)
+    outs = []
+    for other in (0.0, 1.0):
+        q = torch.zeros(n, hq, d, device="cuda", dtype=torch.bfloat16)
+        q[:, 0, 0] = 1.0
+        q[:, 1, 1] = other
+        o, lse = torch.empty_like(q), torch.empty(n, hq, device="cuda")
+        ba.ba_paged_attention(heads, cache, q, o, lse, ints([length] * n), length)
+        ref, _, size = attend64(f64(q)[0], f64(k), f64(v), 1.0)
+        assert close(f64(o)[0], ref, size)
+        outs.append((o[:, 0].clone(), lse[:, 0].clone()))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
