@@ -21,22 +21,49 @@ namespace {
 struct Extent {
   int64_t lo, hi;           // bytes
   int64_t period, width;    // bytes from row to row, bytes of a row from its first head to its last
+  int64_t step, head;       // bytes from head to head, bytes of a head
+  int64_t rows;
+  int32_t heads;
 };
 Extent extent(const ba_tensor *t, int64_t tokens, int n_heads, int D) {
   const int64_t es = (int64_t)elt_size(t->dtype);
   Extent x;
   x.period = t->stride_tok * es;
-  x.width = ((n_heads - 1) * t->stride_head + D) * es;
+  x.step = t->stride_head * es;
+  x.head = D * es;
+  x.width = (n_heads - 1) * x.step + x.head;
+  x.rows = tokens;
+  x.heads = n_heads;
   x.lo = (int64_t)(uintptr_t)t->ptr;
   x.hi = x.lo + (tokens - 1) * x.period + x.width;
   return x;
 }
-// Whether no element is in both: apart altogether, or side by side in rows of one period (query and key heads of one projection).
+// Whether no element is in both: apart altogether, or among each other in rows of one period (query and key heads of one projection, side by
+// side or one after the other).  Rows of different periods that lie among each other are taken to meet.
 bool apart(const Extent &a, const Extent &b) {
   if (a.hi <= b.lo || b.hi <= a.lo) return true;
-  if (a.period != b.period) return false;
+  if (a.period != b.period || a.period == 0) return false;
   const int64_t d = ((b.lo - a.lo) % a.period + a.period) % a.period;
-  return d >= a.width && d + b.width <= a.period;
+  if (d >= a.width && d + b.width <= a.period) return true;
+  // a head of b that begins `by` bytes behind one of a in the same row meets it, or that of another row
+  auto meet = [&](int64_t by) {
+    int64_t m = -by / a.period;  // (rows between them, and the next: a period is a head at least)
+    if (m * a.period > -by) --m;
+    for (int i = 0; i < 2; ++i) {
+      const int64_t at = by + std::min(b.rows - 1, std::max(1 - a.rows, m + i)) * a.period;
+      if (at < a.head && at > -b.head) return true;
+    }
+    return false;
+  };
+  if (a.step == b.step) {  // (pairs of heads as far from each other are one case)
+    for (int32_t j = 1 - a.heads; j < b.heads; ++j)
+      if (meet(b.lo - a.lo + j * a.step)) return false;
+    return true;
+  }
+  for (int32_t i = 0; i < a.heads; ++i)
+    for (int32_t j = 0; j < b.heads; ++j)
+      if (meet(b.lo - a.lo + j * b.step - i * a.step)) return false;
+  return true;
 }
 bool same_place(const ba_tensor *a, const ba_tensor *b) {
   return a->ptr == b->ptr && a->stride_tok == b->stride_tok && a->stride_head == b->stride_head;

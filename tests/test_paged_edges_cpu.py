@@ -1,0 +1,22 @@
+"""Refusals around the paged attention and the head norms that depend on where tensors lie and on how large a call is.  Only calls that have
+to be refused: none of the addresses here is one."""
+import numpy as np
+import pytest
+
+from test_paged_cpu import HEADS, Q, QO, append, attend, back, cache, fake, lib, norm  # noqa: F401
+
+FAR = 1 << 44
+
+
+def test_heads_that_meet_are_refused_wherever_they_meet(lib):  # noqa: F811
+    """Heads 384 apart (three tensors' one after the other): a query head over a key head, in the same row or another."""
+    big = dict(st=8 * 384, sh=384)
+    for d in (0, 240, -240):  # bytes
+        assert norm(lib, q=fake(0x1000000, **big), qo=fake(0x1000000, **big), k=fake(0x1000000 + 768 + d, **big), ko=fake(FAR)) == -1, d
+    row = 8 * 384 * 2
+    k = fake(0x1000000 + 3 * row + 384 * 2 * 2 + 16, **big)  # row 3 of q's four, head 2 of eight
+    assert norm(lib, q=fake(0x1000000, **big), qo=fake(0x1000000, **big), k=k, ko=fake(FAR)) == -1
+    assert append(lib, q=fake(0x1000000, **big), qo=fake(0x1000000, **big), k=k) == -1
+    assert back(lib, dq=fake(0x4000000, **big), dk=fake(0x4000000 + row * 2 + 384 * 4 - 128, **big)) == -1
+    # steps that differ: key heads 512 apart, the second of them over a query head
+    assert norm(lib, q=fake(0x1000000, **big), qo=fake(0x1000000, **big), k=fake(0x1000000 + 512, st=8 * 384, sh=512), ko=fake(FAR)) == -1

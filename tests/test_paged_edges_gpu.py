@@ -89,3 +89,40 @@ def test_no_score_changes_the_bits_of_another_row(ba, hq):
         assert close(f64(o)[0], ref, size)
         outs.append((o[:, 0].clone(), lse[:, 0].clone()))
     assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
+# ---- where outputs lie ----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("tokens", [1, 50, 3000])
+def test_heads_of_query_key_and_value_one_after_the_other(ba, tokens):
+    """A projection laid out [tokens, heads, 3, D]: the heads of one tensor lie between those of the others, and each can be normed
+    where it lies, or appended."""
+    import torch
+    hq, d = 6, 64
+    heads = ba.Heads(hq, hq, d, 10000.0)
+    qkv = rand(151, tokens, hq, 3, d)
+    before = qkv.clone()
+    w = rand(152, d, dtype="f32") + 1
+    norm = ba.HeadNorm(w, w)
+    ref = [torch.empty(tokens, hq, d, dtype=qkv.dtype, device="cuda") for _ in range(2)]
+    ba.ba_norm_rotate(heads, norm, before[:, :, 0], before[:, :, 1], *ref)
+    ba.ba_norm_rotate(heads, norm, qkv[:, :, 0], qkv[:, :, 1], qkv[:, :, 0], qkv[:, :, 1])
+    assert torch.equal(qkv[:, :, 0], ref[0]) and torch.equal(qkv[:, :, 1], ref[1]) and torch.equal(qkv[:, :, 2], before[:, :, 2])
+    g = rand(153, tokens, hq, 3, d)
+    got, back = g.clone(), [torch.empty_like(x) for x in ref]
+    ws = torch.empty(ba.ba_norm_rotate_backward_workspace_bytes(heads, tokens), dtype=torch.uint8, device="cuda")
+    ba.ba_norm_rotate_backward(heads, norm, before[:, :, 0], before[:, :, 1], g[:, :, 0], g[:, :, 1], *back, ws=ws)
+    ba.ba_norm_rotate_backward(heads, norm, before[:, :, 0], before[:, :, 1], got[:, :, 0], got[:, :, 1], got[:, :, 0], got[:, :, 1], ws=ws)
+    assert torch.equal(got[:, :, 0], back[0]) and torch.equal(got[:, :, 1], back[1]) and torch.equal(got[:, :, 2], g[:, :, 2])
+    kp, vp = pools(1, -(-tokens // 16), 16, hq, d)
+    cache = ba.PagedCache(kp, vp, torch.arange(len(kp), dtype=torch.int32, device="cuda")[None])
+    at = torch.arange(tokens, dtype=torch.int32, device="cuda")
+    qkv.copy_(before)
+    ba.ba_paged_append(heads, norm, cache, qkv[:, :, 0], qkv[:, :, 1], qkv[:, :, 2], qkv[:, :, 0], at, torch.zeros_like(at))
+    assert torch.equal(qkv[:, :, 0], ref[0]) and torch.equal(qkv[:, :, 1:], before[:, :, 1:])
+    assert torch.equal(kp.reshape(-1, hq, d)[:tokens], ref[1]) and torch.equal(vp.reshape(-1, hq, d)[:tokens], before[:, :, 2])
+    # a row further on the heads do meet
+    if tokens > 1:
+        flat = before.view(-1)
+        moved = flat[3 * d * hq:].as_strided((tokens - 1, hq, d), (3 * d * hq, 3 * d, 1))
+        with pytest.raises(ba.BaError, match="overlap"):
+            ba.ba_norm_rotate(heads, norm, before[:-1, :, 0], None, moved, None)
