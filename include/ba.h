@@ -463,6 +463,7 @@ int32_t ba_paged_append(const ba_heads *heads, const ba_head_norm *norm, const b
  * A row that sees nothing (p < 0, or no page is there) is zero.  Tokens that a row does not see, and rows of a page that
  * no token has, have no part in it, whatever bits they hold.  lse_out: device, nullable, [n_seqs * q_per_seq][n_q_heads]
  * floats, the natural log of the sum of exp(scale * <q, k>); -infinity for such a row.
+ * o_out may be exactly q; any other overlap with q or the pages is an error.  lse_out and ws lie apart from everything else.
  *
  * Groups: host arrays, cu_group [n_groups + 1] (cu_group[0] = 0, cu_group[n_groups] = n_seqs) and prefix_len [n_groups]
  * (at most max_len).  The first prefix_len[g] tokens of sequences cu_group[g] .. cu_group[g + 1] - 1 are the same, and are

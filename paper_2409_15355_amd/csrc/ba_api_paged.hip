@@ -466,6 +466,12 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
   if ((rc = check_tensor(q, "q", false, heads->head_dim, heads->n_q_heads)) || (rc = check_tensor(o_out, "o_out", false, heads->head_dim, heads->n_q_heads)))
     return rc;
   if (max_len > (int64_t)cache->max_pages * cache->page_rows) return fail(BA_ERR_INVALID_ARG, "max_len reaches beyond the page table");
+  // (a work item reads the query rows that it writes and no others, but the pages are everybody's)
+  const Extent out = extent(o_out, (int64_t)n_seqs * q_per_seq, heads->n_q_heads, heads->head_dim);
+  if (!same_place(q, o_out) && !apart(out, extent(q, (int64_t)n_seqs * q_per_seq, heads->n_q_heads, heads->head_dim)))
+    return fail(BA_ERR_INVALID_ARG, "o_out overlaps q without being exactly in place");
+  if (!apart(pool_extent(&cache->k, cache->k_stride_page, cache, heads), out) || !apart(pool_extent(&cache->v, cache->v_stride_page, cache, heads), out))
+    return fail(BA_ERR_INVALID_ARG, "o_out overlaps the cache");
   if ((rc = check_groups(n_seqs, max_len, n_groups, cu_group, prefix_len))) return rc;
   if (!seq_len) return fail(BA_ERR_INVALID_ARG, "seq_len: null");
   if ((rc = check_int_array(seq_len, "seq_len")) || (rc = check_int_array(lse_out, "lse_out"))) return rc;

@@ -8,6 +8,14 @@ from test_paged_cpu import HEADS, Q, QO, append, attend, back, cache, fake, lib,
 FAR = 1 << 44
 
 
+def test_attention_refuses_outputs_over_what_it_reads(lib):  # noqa: F811
+    assert attend(lib, o=fake(0x1000100)) == -1 and b"overlap" in lib.ba_last_error()       # over q, not in place
+    assert attend(lib, o=fake(0x1000000, st=2048)) == -1 and b"overlap" in lib.ba_last_error()
+    assert attend(lib, o=fake(0x10000400)) == -1 and b"overlap" in lib.ba_last_error()      # inside the pages
+    assert attend(lib, o=fake(0x11000000 + 9 * 16 * 2048 + 15 * 2048)) == -1 and b"overlap" in lib.ba_last_error()  # their last row
+    assert attend(lib, q=fake(0x11000000), o=fake(0x11000000)) == -1                        # in place, but of the pages
+
+
 def test_heads_that_meet_are_refused_wherever_they_meet(lib):  # noqa: F811
     """Heads 384 apart (three tensors' one after the other): a query head over a key head, in the same row or another."""
     big = dict(st=8 * 384, sh=384)

@@ -92,6 +92,33 @@ def test_no_score_changes_the_bits_of_another_row(ba, hq):
 
 
 # ---- where outputs lie ----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("nq,lens,groups", [(1, [200, 33, 90], None), (3, [9000, 1, 4097], None), (13, [300, 40, 77], None), (4, [310, 305, 400], [(3, 300)])])
+def test_attention_in_place_of_its_queries(ba, nq, lens, groups):
+    import torch
+    heads, cache, q, o, lse, _, ws = attention_case(ba, 130 + nq, 8, 2, 128, 16, lens, nq=nq, groups=groups)
+    cu, prefix = (None, None) if groups is None else ([0, 3], [groups[0][1]])
+    same = q.clone()
+    ba.ba_paged_attention(heads, cache, same, same, None, ints(lens), max(lens), cu, prefix, nq, ws)
+    assert torch.equal(same, o)
+    # heads of both side by side in one tensor
+    both = torch.full((len(q), 8, 2, 128), 3.0, dtype=q.dtype, device="cuda")
+    both[:, :, 0] = q
+    ba.ba_paged_attention(heads, cache, both[:, :, 0], both[:, :, 1], None, ints(lens), max(lens), cu, prefix, nq, ws)
+    assert torch.equal(both[:, :, 1], o) and torch.equal(both[:, :, 0], q)
+
+
+def test_attention_does_not_write_over_what_it_reads(ba):
+    import torch
+    heads, cache, q, _, _, _, ws = attention_case(ba, 141, 8, 2, 128, 16, [100, 60], nq=2)
+    room = torch.zeros(6, 8, 128, dtype=q.dtype, device="cuda")
+    room[:4] = q
+    for o in (room[1:5], cache.k_pages.view(-1)[: 4 * 8 * 128].view(4, 8, 128)):
+        before = o.clone()
+        with pytest.raises(ba.BaError, match="overlap"):
+            ba.ba_paged_attention(heads, cache, room[:4], o, None, ints([100, 60]), 100, None, None, 2, ws)
+        assert torch.equal(o.view(torch.int16), before.view(torch.int16))
+
+
 @pytest.mark.parametrize("tokens", [1, 50, 3000])
 def test_heads_of_query_key_and_value_one_after_the_other(ba, tokens):
     """A projection laid out [tokens, heads, 3, D]: the heads of one tensor lie between those of the others, and each can be normed
