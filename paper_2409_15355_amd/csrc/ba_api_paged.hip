@@ -110,6 +110,12 @@ void set_pass(HeadRowsParams *p, const ba_heads *h, const ba_head_norm *norm, in
   p->positions = positions;
 }
 
+// As many tokens as a launch of the forward passes takes.
+int32_t check_tokens(int32_t n_tokens, const ba_heads *h, int32_t dtype) {
+  const int64_t per_wg = head_rows_tokens(h->head_dim, (int)elt_size(dtype));
+  return n_tokens <= kMaxWorkgroups * per_wg ? BA_OK : fail(BA_ERR_UNSUPPORTED, "more than %lld tokens in one call", (long long)(kMaxWorkgroups * per_wg));
+}
+
 // One tensor and its output of the norm passes: types, and exactly in place or apart.
 int32_t check_pair(const ba_tensor *x, const char *name, const ba_tensor *y, const char *y_name, const ba_heads *h, int n_heads, int64_t tokens) {
   int32_t rc;
@@ -277,6 +283,24 @@ size_t plan_bytes(const PagedPlan &pl, const ba_heads *h, int32_t nq) {
   return align256(rows * pl.parts * h->head_dim * 2) + align256(rows * pl.parts * 16);
 }
 
+// All plans of a call: whether they can be launched, and the workspace of the largest.
+int32_t check_plans(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, int32_t n_groups, const int32_t *cu_group,
+                    const int32_t *prefix_len, size_t *bytes) {
+  *bytes = 0;
+  PagedPlan pl;
+  int g = 0;
+  do {
+    plan_paged(h, n_seqs, nq, max_len, n_groups, cu_group, prefix_len, g, num_cus(), &pl);
+    if (pl.n_seqs > 0 && pl.items > kMaxWorkgroups) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
+    const size_t need = plan_bytes(pl, h, nq);
+    if (need > 0 && ((int64_t)pl.n_seqs * nq * h->n_q_heads + kPagedMergeRows - 1) / kPagedMergeRows > kMaxWorkgroups)
+      return fail(BA_ERR_UNSUPPORTED, "2^28 query rows and more in one launch");
+    *bytes = std::max(*bytes, need);
+    g = pl.group_end;
+  } while (g < n_groups);
+  return BA_OK;
+}
+
 int32_t check_paged_sizes(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len) {
   int32_t rc;
   if ((rc = check_heads(h, true))) return rc;
@@ -317,6 +341,7 @@ int32_t ba_norm_rotate(const ba_heads *heads, const ba_head_norm *norm, const ba
         (rc = check_apart(q_out, "q_out", hq, k_out, "k_out", hkv, n_tokens, D)))
       return rc;
   }
+  if ((rc = check_tokens(n_tokens, heads, q ? q->dtype : k->dtype))) return rc;
   HeadRowsParams p;
   memset(&p, 0, sizeof(p));
   if (q) set_source(&p, kRowsQ, q, hq), set_target(&p, kRowsQ, q_out);
@@ -414,6 +439,7 @@ int32_t ba_paged_append(const ba_heads *heads, const ba_head_norm *norm, const b
         (q && (!apart(pool, extent(q, n_tokens, hq, D)) || !apart(pool, extent(q_out, n_tokens, hq, D)))))
       return fail(BA_ERR_INVALID_ARG, "q, k, v or q_out overlap the cache");
   if (q && ((rc = check_apart(q_out, "q_out", hq, k, "k", hkv, n_tokens, D)) || (rc = check_apart(q_out, "q_out", hq, v, "v", hkv, n_tokens, D)))) return rc;
+  if ((rc = check_tokens(n_tokens, heads, BA_DTYPE_BF16))) return rc;
   HeadRowsParams p;
   memset(&p, 0, sizeof(p));
   if (q) set_source(&p, kRowsQ, q, hq), set_target(&p, kRowsQ, q_out);
@@ -443,15 +469,8 @@ size_t ba_paged_attention_workspace_bytes(const ba_heads *heads, int32_t n_seqs,
   if (check_paged_sizes(heads, n_seqs, q_per_seq, max_len) != BA_OK ||
       check_groups(n_seqs, max_len, n_groups, cu_group, prefix_len) != BA_OK)
     return 0;
-  size_t most = 0;
-  PagedPlan pl;
-  int g = 0;
-  do {
-    plan_paged(heads, n_seqs, q_per_seq, max_len, n_groups, cu_group, prefix_len, g, num_cus(), &pl);
-    most = std::max(most, plan_bytes(pl, heads, q_per_seq));
-    g = pl.group_end;
-  } while (g < n_groups);
-  return most;
+  size_t bytes;
+  return check_plans(heads, n_seqs, q_per_seq, max_len, n_groups, cu_group, prefix_len, &bytes) == BA_OK ? bytes : 0;
 }
 
 int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, const ba_tensor *q, const ba_tensor *o_out, float *lse_out,
@@ -475,7 +494,8 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
   if ((rc = check_groups(n_seqs, max_len, n_groups, cu_group, prefix_len))) return rc;
   if (!seq_len) return fail(BA_ERR_INVALID_ARG, "seq_len: null");
   if ((rc = check_int_array(seq_len, "seq_len")) || (rc = check_int_array(lse_out, "lse_out"))) return rc;
-  const size_t need = ba_paged_attention_workspace_bytes(heads, n_seqs, q_per_seq, max_len, n_groups, cu_group, prefix_len);
+  size_t need;
+  if ((rc = check_plans(heads, n_seqs, q_per_seq, max_len, n_groups, cu_group, prefix_len, &need))) return rc;
   if (need > 0 && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need))
     return fail(BA_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than %zu bytes", need);
 
@@ -485,7 +505,6 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
     plan_paged(heads, n_seqs, q_per_seq, max_len, n_groups, cu_group, prefix_len, g, num_cus(), &pl);
     g = pl.group_end;
     if (pl.n_seqs == 0) continue;
-    if (pl.items > INT32_MAX) return fail(BA_ERR_UNSUPPORTED, "more than 2^31 work items in one launch");
     const int64_t tok0 = (int64_t)pl.seq0 * q_per_seq;
     PagedAttnParams p;
     memset(&p, 0, sizeof(p));

@@ -6,6 +6,9 @@
 
 namespace ba {
 
+// Workgroups of 256 that a launch may have: the runtime counts its threads in 32 bits.
+constexpr int64_t kMaxWorkgroups = 0xffffffffll / 256;
+
 // ---------------------------------------------------------------- head norms, appending ----------
 enum { kRowsQ = 0, kRowsK = 1, kRowsV = 2 };
 
@@ -28,6 +31,9 @@ struct HeadRowsParams {
   int32_t page_rows;
   FastDiv page_div;
 };
+// Tokens of a workgroup in calls of many tokens (a lane for two 16-byte pieces, four heads at a time).
+constexpr int kRowsThreads = 256, kManySlots = 4;
+constexpr int head_rows_tokens(int head_dim, int elt_bytes) { return kRowsThreads / (head_dim * elt_bytes / 16 / 2 * kManySlots); }
 hipError_t launch_norm_rotate(const HeadRowsParams &p, const RopeTable &rt, hipStream_t stream);
 hipError_t launch_paged_append(const HeadRowsParams &p, const RopeTable &rt, hipStream_t stream);
 
@@ -57,6 +63,7 @@ constexpr int kPagedTileRows = 128;    // rows of a work item
 constexpr int kPagedStreamRows = 32;
 BA_HD int paged_tile_rows(int n_rows) { return n_rows > kPagedStreamRows ? kPagedTileRows : kPagedStreamRows; }
 constexpr int kPagedMaxChunk = 2048;  // keys of a work item at most: its part of the page table lies in LDS
+constexpr int kPagedMergeRows = 16;   // rows that a workgroup of the merge takes, at one way a row
 
 struct PagedAttnParams {
   const uint16_t *q;

@@ -21,7 +21,7 @@
 namespace ba {
 namespace {
 
-constexpr int kManySlots = 4, kFewSlots = 16;
+constexpr int kFewSlots = 16;
 // kSlots: heads of a token that a workgroup takes at a time
 template <typename T, int D, int kSlots>
 struct RowGeo {
@@ -378,6 +378,7 @@ hipError_t launch_rows(const HeadRowsParams &p, const RopeTable &rt, hipStream_t
     head_rows_few_kernel<T, D, LAYOUT, kPaged><<<dim3((unsigned)(p.n_tokens + TOK - 1) / TOK, kPaged ? 3 : 2), kRotThreads, 0, stream>>>(p, rt);
   } else {
     constexpr int TOK = RowGeo<T, D, kManySlots>::TOK;
+    static_assert(kRotThreads == kRowsThreads && TOK == head_rows_tokens(D, sizeof(T)), "what the size of a call is checked with");
     const unsigned wgs = (unsigned)((p.n_tokens + (int64_t)TOK - 1) / TOK);
     const int past = past_caches(p, 2);
     if (past == 2) head_rows_kernel<T, D, LAYOUT, kPaged, 2><<<wgs, kRotThreads, 0, stream>>>(p, rt);

@@ -876,7 +876,7 @@ template <int D, typename Groups>
 hipError_t launch_attn_d(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
   const int64_t items = p.prefix_items + (int64_t)p.n_seqs * p.n_kv_heads * p.own_row_tiles * p.own_splits;
   const int32_t chunk = std::max(p.chunk, p.own_chunk);
-  if (items < 1 || items > 0x7fffffff || chunk > kPagedMaxChunk) return hipErrorInvalidValue;
+  if (items < 1 || items > kMaxWorkgroups || chunk > kPagedMaxChunk) return hipErrorInvalidValue;
   const size_t lds = kTilesB + (size_t)(chunk / p.page_rows + 2) * 4;  // (a range may begin and end inside a page)
   static_assert(2 * (kTilesB + (kPagedMaxChunk + 2) * 4) <= 160 * 1024, "two workgroups a compute unit");
   return p.page_rows % 16 == 0 ? launch_attn_a<D, true>(p, g, (unsigned)items, lds, stream) : launch_attn_a<D, false>(p, g, (unsigned)items, lds, stream);
@@ -884,8 +884,9 @@ hipError_t launch_attn_d(const PagedAttnParams &p, const Groups &g, hipStream_t 
 template <int D, int kWays, typename Groups>
 hipError_t launch_merge_w(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
   constexpr int kRows = kMergeThreads / kMergeLanes / kWays;
+  static_assert(kRows * kWays == kPagedMergeRows && kMergeThreads == 256, "what the size of a call is checked with");
   const int64_t wgs = (p.part_rows + kRows - 1) / kRows;
-  if (wgs < 1 || wgs > 0x7fffffff) return hipErrorInvalidValue;
+  if (wgs < 1 || wgs > kMaxWorkgroups) return hipErrorInvalidValue;
   paged_merge_kernel<D, kWays, Groups><<<(unsigned)wgs, kMergeThreads, 0, stream>>>(p, g);
   return hipGetLastError();
 }

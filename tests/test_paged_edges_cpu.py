@@ -28,3 +28,24 @@ def test_heads_that_meet_are_refused_wherever_they_meet(lib):  # noqa: F811
     assert back(lib, dq=fake(0x4000000, **big), dk=fake(0x4000000 + row * 2 + 384 * 4 - 128, **big)) == -1
     # steps that differ: key heads 512 apart, the second of them over a query head
     assert norm(lib, q=fake(0x1000000, **big), qo=fake(0x1000000, **big), k=fake(0x1000000 + 512, st=8 * 384, sh=512), ko=fake(FAR)) == -1
+
+
+def test_calls_larger_than_a_launch_are_refused_ahead_of_every_launch(lib):  # noqa: F811
+    tokens = 1 << 27  # eight to a workgroup
+    k, ko = fake(FAR, st=256), fake(2 * FAR, st=256)
+    one = dict(q=None, qo=None, k=k, ko=ko, tokens=tokens)
+    assert norm(lib, **one) == -2
+    assert append(lib, q=None, qo=None, k=fake(FAR, st=256), v=fake(2 * FAR, st=256), tokens=tokens) == -2
+    n = 1 << 18
+    c = cache(n_seqs=n, max_pages=1 << 16, stride=1 << 16)
+    far = dict(q=fake(FAR), o=fake(2 * FAR), wsb=1 << 62)
+    assert attend(lib, c=c, max_len=1 << 20, **far) == -2
+    # ninety-seven groups in one launch's table and the next, and behind them what no launch takes
+    cu = np.concatenate([np.arange(0, 2 * 97 + 1, 2), [n]])
+    assert attend(lib, c=c, max_len=1 << 20, cu=cu, pre=[1 << 20] * 97 + [0], **far) == -2
+
+
+@pytest.mark.parametrize("n_seqs,q_per_seq,max_len", [(1 << 18, 1, 1 << 20)])
+def test_workspace_queries_reject_calls_larger_than_a_launch(lib, n_seqs, q_per_seq, max_len):  # noqa: F811
+    import ctypes
+    assert lib.ba_paged_attention_workspace_bytes(ctypes.byref(HEADS.c), n_seqs, q_per_seq, max_len, 0, None, None) == 0
