@@ -648,11 +648,13 @@ def ba_block_attention_prompts_backward(heads: Heads, q, k, v, o, lse, d_out, dq
                                                       _ip(offs), wp, wb, _stream_handle(stream)))
 
 
-def _tokens_of(*tensors) -> int:
-    for t in tensors:
-        if t is not None:
-            return int(t.shape[0])
-    raise ValueError("q and k: both None")
+def _tokens_of(q, k) -> int:
+    """Tokens of both, either may be None."""
+    if q is None and k is None:
+        raise ValueError("q and k: both None")
+    if q is not None and k is not None and q.shape[0] != k.shape[0]:
+        raise ValueError(f"q and k: {q.shape[0]} and {k.shape[0]} tokens")
+    return int((k if q is None else q).shape[0])
 
 
 def ba_norm_rotate(heads: Heads, norm: HeadNorm, q, k, q_out, k_out, positions=None, rope_mode: int = ROPE_APPLY, stream=None) -> None:

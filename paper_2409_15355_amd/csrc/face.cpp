@@ -186,6 +186,10 @@ int64_t tokens_of(PyObject *q, PyObject *k) {
   need(q != Py_None || k != Py_None);
   const at::Tensor &x = plain_tensor(q != Py_None ? q : k);
   need(x.dim() == 3 && x.size(0) <= INT32_MAX);
+  if (q != Py_None && k != Py_None) {
+    const at::Tensor &y = plain_tensor(k);
+    need(y.dim() == 3 && y.size(0) == x.size(0));
+  }
   return x.size(0);
 }
 struct Workspace {

@@ -153,3 +153,13 @@ def test_heads_of_query_key_and_value_one_after_the_other(ba, tokens):
         moved = flat[3 * d * hq:].as_strided((tokens - 1, hq, d), (3 * d * hq, 3 * d, 1))
         with pytest.raises(ba.BaError, match="overlap"):
             ba.ba_norm_rotate(heads, norm, before[:-1, :, 0], None, moved, None)
+
+
+def test_queries_and_keys_of_different_token_counts_are_refused(ba):
+    import torch
+    heads = ba.Heads(8, 2, 64)
+    q, k = rand(161, 5, 8, 64), rand(162, 7, 2, 64)
+    with pytest.raises(ValueError, match="tokens"):
+        ba.ba_norm_rotate(heads, ba.HeadNorm(), q, k, torch.empty_like(q), torch.empty_like(k))
+    with pytest.raises(ValueError, match="tokens"):
+        ba.ba_norm_rotate_backward(heads, ba.HeadNorm(), q, k, q, k, torch.empty_like(q), torch.empty_like(k), ws=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
