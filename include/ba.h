@@ -446,7 +446,7 @@ typedef struct ba_paged_cache {
  * rope_pos[t] = the shift of the token's passage, without norm.
  * A token whose sequence, position or page is not there (a negative position, say) is not kept; its query is written all
  * the same.  No two tokens of a call may go to the same row.  Nothing else of the cache changes.
- * q, k, v, q_out: bf16, q_out may be exactly q.  cache_pos, seq_of_token, rope_pos: device, n_tokens ints.
+ * q, k, v, q_out: bf16, q_out may be exactly q; any other overlap of an output, the pages among them, is an error.  cache_pos, seq_of_token, rope_pos: device, n_tokens ints.
  */
 int32_t ba_paged_append(const ba_heads *heads, const ba_head_norm *norm, const ba_paged_cache *cache,
                         const ba_tensor *q, const ba_tensor *k, const ba_tensor *v,

@@ -433,6 +433,8 @@ int32_t ba_paged_append(const ba_heads *heads, const ba_head_norm *norm, const b
   if ((rc = check_int_array(cache_pos, "cache_pos")) || (rc = check_int_array(seq_of_token, "seq_of_token")) ||
       (rc = check_int_array(rope_pos, "rope_pos")))
     return rc;
+  if (!apart(extent(&cache->k, cache->page_rows, hkv, D), extent(&cache->v, cache->page_rows, hkv, D)))
+    return fail(BA_ERR_INVALID_ARG, "cache: keys and values of a page overlap");
   const Extent pools[2] = {pool_extent(&cache->k, cache->k_stride_page, cache, heads), pool_extent(&cache->v, cache->v_stride_page, cache, heads)};
   for (const Extent &pool : pools)
     if (!apart(pool, extent(k, n_tokens, hkv, D)) || !apart(pool, extent(v, n_tokens, hkv, D)) ||

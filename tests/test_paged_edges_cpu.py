@@ -30,6 +30,13 @@ def test_heads_that_meet_are_refused_wherever_they_meet(lib):  # noqa: F811
     assert norm(lib, q=fake(0x1000000, **big), qo=fake(0x1000000, **big), k=fake(0x1000000 + 512, st=8 * 384, sh=512), ko=fake(FAR)) == -1
 
 
+def test_append_refuses_pages_in_which_keys_and_values_meet(lib):  # noqa: F811
+    one = fake(0x10000000)
+    assert append(lib, c=cache(k=one, v=one)) == -1 and b"overlap" in lib.ba_last_error()
+    assert append(lib, c=cache(k=one, v=fake(0x10000000 + 15 * 2048 + 256))) == -1 and b"overlap" in lib.ba_last_error()  # the last row's second head
+    assert append(lib, c=cache(k=fake(0x10000000, 512, 256), v=fake(0x10000000 + 128, 512, 256))) == -1  # half a head on
+
+
 def test_calls_larger_than_a_launch_are_refused_ahead_of_every_launch(lib):  # noqa: F811
     tokens = 1 << 27  # eight to a workgroup
     k, ko = fake(FAR, st=256), fake(2 * FAR, st=256)

@@ -155,6 +155,29 @@ def test_heads_of_query_key_and_value_one_after_the_other(ba, tokens):
             ba.ba_norm_rotate(heads, norm, before[:-1, :, 0], None, moved, None)
 
 
+@pytest.mark.parametrize("form", ["rows", "heads"])
+def test_pages_with_keys_and_values_beside_each_other(ba, form):
+    """[pages, rows, 2, heads, D] and [pages, rows, heads, 2, D]; attention may read one pool as both."""
+    import torch
+    hq, hkv, d, rows, n = 8, 2, 64, 16, 100
+    heads = ba.Heads(hq, hkv, d, 10000.0)
+    k, v, q = rand(171, n, hkv, d), rand(172, n, hkv, d), rand(173, 1, hq, d)
+    at = torch.arange(n, dtype=torch.int32, device="cuda")
+    table = ints(np.random.default_rng(2).permutation(7)[None])
+    outs = []
+    for together in (False, True):
+        kv = torch.zeros((2, 7, rows, hkv, d) if not together else (7, rows, 2, hkv, d) if form == "rows" else (7, rows, hkv, 2, d), dtype=k.dtype, device="cuda")
+        kp, vp = kv.unbind(0 if not together else 2 if form == "rows" else 3)
+        ba.ba_paged_append(heads, None, ba.PagedCache(kp, vp, table), None, k, v, None, at, torch.zeros_like(at))
+        for pair in ((kp, vp), (vp, vp)):
+            o = torch.empty_like(q)
+            ba.ba_paged_attention(heads, ba.PagedCache(*pair, table), q, o, None, ints([n]), n, ws=workspace(ba, heads, 1, 1, n))
+            outs.append(o)
+    assert torch.equal(outs[0], outs[2]) and torch.equal(outs[1], outs[3])
+    ref, _, size = attend64(f64(q)[0], f64(v), f64(v), 1 / math.sqrt(d))
+    assert close(f64(outs[1])[0], ref, size)
+
+
 def test_queries_and_keys_of_different_token_counts_are_refused(ba):
     import torch
     heads = ba.Heads(8, 2, 64)
