@@ -186,3 +186,117 @@ def test_queries_and_keys_of_different_token_counts_are_refused(ba):
         ba.ba_norm_rotate(heads, ba.HeadNorm(), q, k, torch.empty_like(q), torch.empty_like(k))
     with pytest.raises(ValueError, match="tokens"):
         ba.ba_norm_rotate_backward(heads, ba.HeadNorm(), q, k, q, k, torch.empty_like(q), torch.empty_like(k), ws=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+
+
+# ---- forms of the walks ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("hq,hkv,d,nq", [(8, 2, 64, 13), (8, 1, 128, 40)])
+@pytest.mark.parametrize("rows", [1, 7, 33, 100])
+def test_many_rows_over_pages_of_any_length(ba, hq, hkv, d, nq, rows):
+    attention_case(ba, 200 + rows, hq, hkv, d, rows, [40, 17, 300, 0, 5, 700], nq=nq)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows,form", [(7, "plain"), (48, "heads_first"), (33, "together")])
+def test_many_rows_over_a_prefix_in_pages_of_any_length(ba, d, rows, form):
+    attention_case(ba, 210 + rows, 8, 2, d, rows, [170, 163, 400, 151, 180, 90], nq=8, groups=[(5, 150), (1, 40)], form=form)
+
+
+@pytest.mark.parametrize("nq", [5, 13])
+@pytest.mark.parametrize("rows", [16, 7])
+def test_missing_pages_of_many_rows(ba, nq, rows):
+    attention_case(ba, 220 + rows, 8, 2, 128, rows, [200, 64, 33, 90, 700], nq=nq, holes=9)
+
+
+@pytest.mark.parametrize("nq", [5, 13])
+@pytest.mark.parametrize("q_scale", [30.0, 0.0])
+def test_large_scores_of_many_rows(ba, nq, q_scale):
+    attention_case(ba, 230 + nq, 8, 2, 128, 16, [500, 90], nq=nq, q_scale=q_scale)
+
+
+@pytest.mark.parametrize("hq", [20, 40, 200])
+def test_rising_scores_of_many_rows(ba, hq):
+    """Each tile's scores tower over those before it, for some rows."""
+    import torch
+    heads = ba.Heads(hq, 1, 64, softmax_scale=1.0)
+    n = 400
+    k = torch.zeros(n, 1, 64, device="cuda")
+    k[:, 0, 0] = torch.arange(n, device="cuda") // 16 * 16.0
+    kp, v = k.bfloat16().view(25, 16, 1, 64), rand(240, n, 1, 64)
+    q = torch.zeros(1, hq, 64, device="cuda")
+    q[0, :, 0] = torch.tensor([1.0, -1.0, 8.0, -8.0, 0.0], device="cuda").repeat(hq // 5)
+    o, lse = torch.empty(1, hq, 64, dtype=torch.bfloat16, device="cuda"), torch.empty(1, hq, device="cuda")
+    cache = ba.PagedCache(kp, v.view(25, 16, 1, 64), ints(np.arange(25)[None]))
+    ba.ba_paged_attention(heads, cache, q.bfloat16(), o, lse, ints([n]), n, ws=workspace(ba, heads, 1, 1, n))
+    ref, ref_lse, size = attend64(f64(q)[0], f64(k.bfloat16()), f64(v), 1.0)
+    assert close(f64(o)[0], ref, size) and (np.abs(f64(lse)[0] - ref_lse) <= 2e-5 * (1 + np.abs(ref_lse))).all()
+
+
+@pytest.mark.parametrize("nq", [1, 3, 9])
+@pytest.mark.parametrize("rows", [16, 10])
+def test_missing_pages_of_a_prefix(ba, nq, rows):
+    """They are missing for every member; what another member's table has in their place does not matter."""
+    import torch
+    hq, hkv, d, prefix, lens = 8, 2, 128, 150, [190, 170, 100, 151]
+    heads = ba.Heads(hq, hkv, d, 10000.0)
+    table, n_pages = paged(np.random.default_rng(7), lens, rows, 20, first_of=[0] * 4, prefix=[prefix] * 4)
+    kp, vp = pools(1, n_pages, rows, hkv, d)
+    keys = []
+    for s, n in enumerate(lens):
+        k, v = rand(250 + s, n, hkv, d), rand(260 + s, n, hkv, d)
+        if s:
+            c = min(prefix, n)
+            k[:c], v[:c] = keys[0][0][:c], keys[0][1][:c]
+        keys.append((k, v))
+        put(kp, table, s, 0, k), put(vp, table, s, 0, v)
+    seen = np.ones(200, dtype=bool)
+    for page, to in ((1, -1), (2, n_pages), (6, 2 ** 31 - 1)):
+        table[0, page] = to
+        seen[page * rows:(page + 1) * rows] = False
+    q = rand(270, 4 * nq, hq, d)
+    o, lse = torch.empty_like(q), torch.empty(4 * nq, hq, device="cuda")
+    cache = ba.PagedCache(kp, vp, ints(table.clip(-2 ** 31, 2 ** 31 - 1)))
+    ba.ba_paged_attention(heads, cache, q, o, lse, ints(lens), 200, [0, 4], [prefix], nq, workspace(ba, heads, 4, nq, 200, [0, 4], [prefix]))
+    for s in range(4):
+        for i in range(nq):
+            row, end = s * nq + i, lens[s] - nq + i + 1
+            ok = seen[:end]
+            ref, ref_lse, size = attend64(f64(q)[row], f64(keys[s][0])[:end][ok], f64(keys[s][1])[:end][ok], 1 / math.sqrt(d))
+            assert close(f64(o)[row], ref, size)
+            assert (np.abs(f64(lse)[row] - ref_lse) <= 2e-5 * (1 + np.abs(ref_lse))).all()
+
+
+@pytest.mark.parametrize("nq,rows,groups", [(1, 16, None), (7, 48, None), (9, 16, None), (9, 20, None), (4, 64, [(12, 60), (4, 0)])])
+def test_calls_that_read_past_the_caches(ba, nq, rows, groups):
+    """By the bound on their lengths: 96 MB of keys and values and more.  The sequences are short."""
+    rng = np.random.default_rng(nq)
+    low = 60 if groups else 0
+    assert 16 * 3000 * 8 * 128 * 4 > 1.5 * 96 * 2 ** 20
+    attention_case(ba, 280 + nq, 32, 8, 128, rows, [low + int(x) for x in rng.integers(0, 70, 15)] + [400], nq=nq, groups=groups, max_len=3000)
+
+
+def test_the_python_half_of_the_face_makes_the_same_calls(ba, monkeypatch):
+    """Norms, their backward, appends and attention without the native half that takes their arguments apart: the same bits."""
+    import torch
+    hq, hkv, d, tokens = 8, 2, 64, 40
+    heads = ba.Heads(hq, hkv, d, 10000.0)
+    norm = ba.HeadNorm(rand(301, d) + 1, rand(302, d) + 1, 1e-5)
+    q, k, v = rand(303, tokens, hq, d), rand(304, tokens, hkv, d), rand(305, tokens, hkv, d)
+    pos, at, seq = ints(np.arange(tokens) * 7), ints(np.arange(tokens) // 4), ints(np.arange(tokens) % 4)
+    calls = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(ba, "_native", ba._NoNative())
+        new = lambda x: torch.zeros_like(x)  # noqa: E731
+        out = [new(q), new(k), new(q), new(k), torch.zeros(d, device="cuda"), torch.zeros(d, device="cuda"), new(q)]
+        ba.ba_norm_rotate(heads, norm, q, k, out[0], out[1], pos)
+        ws = torch.empty(ba.ba_norm_rotate_backward_workspace_bytes(heads, tokens), dtype=torch.uint8, device="cuda")
+        ba.ba_norm_rotate_backward(heads, norm, q, k, out[0], out[1], out[2], out[3], out[4], out[5], pos, ba.ROPE_APPLY, ws)
+        kp, vp = torch.zeros(2, 8, 4, hkv, d, dtype=torch.bfloat16, device="cuda")
+        cache = ba.PagedCache(kp, vp, ints(np.arange(8).reshape(4, 2)[:, ::-1].copy()))
+        keep = at[:32], seq[:32], pos[:32]
+        ba.ba_paged_append(heads, norm, cache, q[:32], k[:32], v[:32], out[6], *keep)
+        o, lse = new(q[:8]), torch.zeros(8, hq, device="cuda")
+        ba.ba_paged_attention(heads, cache, q[:8], o, lse, ints([8, 7, 3, 0]), 8, [0, 4], [3], 2, workspace(ba, heads, 4, 2, 8, [0, 4], [3]))
+        calls.append(out + [kp, vp, o, lse])
+        assert all(bool(x.any()) for x in calls[-1])
+    assert all(torch.equal(a, b) for a, b in zip(*calls))
