@@ -310,7 +310,6 @@ class PagedCache:
         n_pages, rows, self.n_kv_heads, self.head_dim = k_pages.shape
         self.n_seqs, max_pages = page_table.shape
         k, v = (_tensor(t, name, layers=True) for name, t in (("k_pages", k_pages), ("v_pages", v_pages)))
-        self.max_rows = max_pages * rows
         self.known = _KnownCache(BaPagedCache(k, v, k_pages.stride(0), v_pages.stride(0), n_pages, rows, page_table.data_ptr(),
                                               page_table.stride(0), self.n_seqs, max_pages), self.n_kv_heads, self.head_dim)
         self.c = self.known.cache

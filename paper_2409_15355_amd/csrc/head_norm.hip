@@ -354,8 +354,10 @@ __global__ __launch_bounds__(kGainThreads) void gain_sums_kernel(NormBackwardPar
   if (way == 0) p.weight_grad[kind][col] = (float)red[0][threadIdx.x];
 }
 
-// Which of the two, us a call, many / few (Python face and all, which takes 4.7 of them).  32 over 8 heads of 128, bf16, norm and rotation: 64
-// tokens 7.6 / 5.2, 512 8.8 / 5.7, 1,024 9.7 / 7.8, 2,048 11.7 / 11.6, 4,096 17.0 / 19.5.  8 over 2 of 64, fp32: 1,024 5.6 / 5.2, 2,077 6.1 / 7.0.
+// Which of the two, us a call, many / few (Python face and all, without which none is made in less than 3.7).  32 over 8 heads of 128, norm and
+// rotation, bf16: 64 tokens 7.6 / 5.2, 512 8.2 / 5.1, 1,024 9.5 / 7.0, 2,048 11.3 / 11.1, 3,000 13.9 / 15.1; fp32: 512 7.5 / 6.5, 1,024 9.7 / 9.7,
+// 1,536 12.1 / 12.2, 2,048 16.1 / 15.1, 3,000 21.7 / 25.8; heads of 64, fp32: 1,024 7.6 / 6.3, 2,048 9.8 / 9.6.  16 over 8 of 128, bf16: 1,024
+// 6.9 / 5.5, 2,048 8.9 / 9.5; fp32: 768 6.4 / 6.1, 1,024 7.4 / 8.1.  8 over 2 of 64, fp32: 1,024 4.7 / 4.4, 1,536 5.0 / 5.3.
 // Keys and values of 8 heads into pages: 512 5.3 / 5.3, 2,048 6.5 / 7.8.  The first one's lanes wait for memory once for every sixteen heads.
 inline bool few_tokens(const HeadRowsParams &p) {
   const int heads = std::max(p.src[kRowsQ] ? p.n_heads[kRowsQ] : 0, p.n_heads[kRowsK]);

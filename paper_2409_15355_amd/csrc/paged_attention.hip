@@ -191,9 +191,10 @@ struct PagedSource {
 __device__ __forceinline__ uint32_t below(int lim) { return lim <= 0 ? 0u : lim >= 32 ? ~0u : (1u << lim) - 1u; }
 
 // A row's result: E consecutive dimensions of it at a time, of D.  top: the largest finite size among all D of o.
-// Parts are kept as fp16, divided by their sum and by a power of two that brings the largest into [2^13, 2^14): 2^-11 of an element at
-// most, an eighth of what the result's own rounding to bf16 may take, and half the memory traffic of 32 bits (64 sequences over
-// 31,744 shared keys, 32 over 8 heads of 128: 33 MB out and in again, of 130 MB of keys and values).
+// Parts are kept as fp16, divided by their sum and by a power of two that brings the largest into [2^13, 2^14): an element of a part is off by
+// 2^-11 of itself, or 2^-38 of the part's largest where that is more; the result by 2^-11 of sum p |v|, a quarter of what rounding P to bf16
+// may take.  Half the memory traffic of 32 bits (64 sequences over 31,744 shared keys, 32 over 8 heads of 128: 33 MB out and in
+// again, of 130 MB of keys and values).
 struct RowEnd {
   float m, l, inv, mult, scale;
 };
@@ -463,10 +464,11 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem 
 
 // ---- many rows: 32 a wave, tiles of 32 keys shared by the four -----------------------------------------------------------
 // A key is read from memory once for 128 rows, and from LDS once for 32.  32 over 8 heads of 128, 64 sequences on 31,744 keys: 33.4 GFLOP in
-// 58.7 us, 570 TFLOP/s; matrix, vector and LDS instructions take 30 to 45 us each, and two waves a SIMD cover each other's only in part (the
-// tile behind a barrier, the softmax between two products).  Three workgroups a compute unit need 168 registers and 48 KB: 512 rows 87 us
-// against 91, but 256 rows 58.5 against 51.9; eight waves that take turns at the matrix units, with 64 keys a tile: 58.4 against 58.2.  The next tile's
-// score products between this one's exponentials: no change.
+// 58.7 us, 570 TFLOP/s.  The matrix units are busy for 17 of them, vector instructions take 21 and LDS reads 9 (counters): what it waits for is a
+// wave's own chain (the tile behind a barrier, the softmax between two products), of which two waves a SIMD cover each other's only
+// in part.  Three workgroups a compute unit need 168 registers and 48 KB: 512 rows 87 us against 91, but 256 rows 58.5 against 51.9; eight
+// waves that take turns at the matrix units, with 64 keys a tile, and with the sequences' own items among theirs: 58.4 against 58.2.
+// The next tile's score products between this one's exponentials: no change.
 template <int D, bool kAligned, typename Stage>
 __device__ __forceinline__ void walk_shared(const PagedAttnParams &p, PagedItem &it, lds_char *smem, int lane, int wave, Stage &&stage) {
   using G = PGeo<D>;
