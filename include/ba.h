@@ -386,7 +386,8 @@ size_t ba_block_attention_prompts_backward_workspace_bytes(const ba_heads *heads
  *   y = R(positions[t]) (w o x / sqrt(mean(x^2) + eps)),   the mean over its head_dim elements,
  * in 32 bits, rounded once.  q [T, n_q_heads, D] with gains w = norm->q_weight into q_out, k [T, n_kv_heads, D] with
  * norm->k_weight into k_out; q and q_out, or k and k_out, may be null.  bf16 or fp32 (one type for all of them).
- * An output may be exactly its input (in place); any other overlap is an error.
+ * An output may be exactly its input (in place); any other overlap is an error.  Heads may lie between another tensor's where both have one
+ * token stride; tensors of different token strides that lie among each other count as overlapping.
  * rope_mode BA_ROPE_NONE norms only: in front of the entry points that rotate by themselves, and of
  * ba_block_attention_prompts with its backward.  With BA_ROPE_APPLY the rows are ready for BA_ROPE_NONE there.
  * positions: DEVICE, n_tokens ints, null -> a token's number.
