@@ -401,10 +401,10 @@ def _evict_plain(case, st):
 
 
 def _exponent(top):
-    """The least e with top <= 127 * 2^e, within limits."""
+    """The least e with top <= 127 * 2^e, within limits (an infinity's is the largest)."""
     m, e = torch.frexp(top)
     e = torch.where(m <= 127 / 128, e - 7, e - 6)
-    return torch.where(top == 0, MIN_EXP, e).clamp(MIN_EXP, MAX_EXP)
+    return torch.where(top == 0, MIN_EXP, torch.where(torch.isinf(top), MAX_EXP, e)).clamp(MIN_EXP, MAX_EXP)
 
 
 def _two_to(e):
@@ -429,7 +429,7 @@ def _bounds_plain(case, st, width):
     k = st["k_pages"][page].float()  # [pages, rows, KV heads, D]
     k = torch.where(torch.isnan(k), 0.0, k)
     new = new[:, :, None, None]
-    e = _exponent(torch.where(new & torch.isfinite(k), k.abs(), 0.0).amax(dim=(1, 3)))
+    e = _exponent(torch.where(new, k.abs(), 0.0).amax(dim=(1, 3)))
     old_e = torch.where(fresh[:, None], MIN_EXP, st["exps"][page].int())
     both = torch.maximum(e, old_e)
     scale, by = _two_to(-both)[..., None], _two_to(old_e - both)[..., None]
@@ -448,7 +448,7 @@ def _select_plain(case, st):
     n_seqs, n = len(st["lens"]), st["table"].shape[1]
     q = torch.where(torch.isnan(st["q"]), 0.0, st["q"].float())
     q = q.view(n_seqs, nq, hkv, hq // hkv, d).transpose(1, 2).reshape(n_seqs, hkv, nq * (hq // hkv), d)
-    e = _exponent(torch.where(torch.isfinite(q), q.abs(), 0.0).amax(-1))
+    e = _exponent(q.abs().amax(-1))
     c = torch.round(q * _two_to(-e)[..., None]).clamp(-127, 127)  # (half to even)
     page = st["table"].long().clamp(min=0)
     codes = st["codes"][page].float().permute(0, 2, 3, 4, 1)  # [sequences, KV heads, 2, D, pages]
