@@ -482,6 +482,109 @@ size_t ba_paged_attention_workspace_bytes(const ba_heads *heads, int32_t n_seqs,
                                           const int32_t *cu_group, const int32_t *prefix_len);
 
 /*
+ * Caches that grow long: which of their keys matter, and answers that read no others.  Two ways, which go together:
+ * keys that get little attention are evicted (ba_paged_key_weights, ba_paged_evict), or all stay and a step reads the pages that
+ * promise its queries the largest scores (ba_page_bounds, ba_page_select, ba_paged_attention_selected).
+ * seq_len, max_len, the groups and q_per_seq are those of ba_paged_attention; the page table is checked in the same way.
+ */
+
+/*
+ * Attention that the cached keys have been given, per sequence, KV head g and token t:
+ *   weights_out[s, g, t] = decay * weights_in[s, g, t] + sum_{i < q_per_seq, h in g, t <= p(i)} exp(scale * <q[i, h], k_t> - lse[i, h])
+ * with p(i) = seq_len[s] - q_per_seq + i; the sums in 32 bits.  q: rotated, as ba_paged_attention has them; lse: device, its lse_out
+ * ([n_seqs * q_per_seq][n_q_heads] floats; a row of -infinity adds nothing).  Nothing has been given to the call's own tokens before: for
+ * t >= seq_len[s] - q_per_seq the first term is left out, whatever weights_in holds there.  It is also left out with decay 0 or without weights_in.
+ * A token whose page is not there is given nothing.  Places of tokens that a sequence has not are left as they are.
+ * weights_in, weights_out: device floats, head g of sequence s from element (s * n_kv_heads + g) * stride_weights on (at least max_len);
+ * weights_out may be exactly weights_in, and lies apart from everything else.
+ * ws: 256-byte aligned, at least ba_paged_key_weights_workspace_bytes() bytes (may be null when that is 0).
+ * Two calls with the same arguments give the same bits; in another batch the last bits may differ.
+ */
+int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache, const ba_tensor *q,
+                             const float *lse, const float *weights_in, float *weights_out,
+                             int64_t stride_weights, float decay, int32_t q_per_seq,
+                             const int32_t *seq_len, int32_t max_len, int32_t n_groups,
+                             const int32_t *cu_group, const int32_t *prefix_len, void *ws,
+                             size_t ws_bytes, void *stream);
+size_t ba_paged_key_weights_workspace_bytes(const ba_heads *heads, int32_t n_seqs,
+                                            int32_t q_per_seq, int32_t max_len, int32_t n_groups,
+                                            const int32_t *cu_group, const int32_t *prefix_len);
+
+/*
+ * Every sequence of `cache` cut to n_keep tokens at most, into the pages of `to`.  A sequence of more tokens keeps, for each KV head, its first
+ * n_first and its last n_last ones and as many of the others as fit, those with the largest weights; of equal weights the earlier
+ * token (-0 equals 0; a NaN is less than everything).  A shorter one keeps all.  The kept tokens stay in order: the j-th one's key and value of that
+ * head become row j of the sequence in `to`, its number goes to kept_out [n_seqs][n_kv_heads][n_keep] (device ints; -1 behind the last one), its
+ * weight to weights_out (device floats, nullable, heads stride_out >= n_keep elements apart; places behind the last one stay as they
+ * are).  len_out (device, nullable): [n_seqs], the new lengths.  Keys keep the rotation of their old positions: a token that is
+ * appended afterwards goes to row len_out[s] and is rotated at its position in the text, as a step that appends takes the two apart.
+ * A token whose old or new page is not there is not copied; its new row stays as it is.
+ * `to`: as many sequences as `cache`, room for min(n_keep, max_len) tokens each; page_rows may differ.  Its pages may be of the same pool (then
+ * described alike: pointer and strides of rows, heads and pages), but none that a sequence of `cache` reads, and no page for two rows of its own.  Otherwise the pools lie apart.
+ * Other arrays of the call lie apart from what it writes.
+ * ws: 256-byte aligned, at least ba_paged_evict_workspace_bytes() bytes (may be null when that is 0).
+ */
+int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const ba_paged_cache *to,
+                       const float *weights, int64_t stride_weights, const int32_t *seq_len,
+                       int32_t max_len, int32_t n_keep, int32_t n_first, int32_t n_last,
+                       int32_t *kept_out, float *weights_out, int64_t stride_out, int32_t *len_out,
+                       void *ws, size_t ws_bytes, void *stream);
+size_t ba_paged_evict_workspace_bytes(const ba_heads *heads, int32_t n_seqs, int32_t max_len,
+                                      int32_t n_keep);
+
+/*
+ * Bounds of the pages' keys, in 8 bits: per page, KV head and dimension d
+ *   codes[page][head][0][d] = max over rows of ceil(k_d / 2^e), codes[page][head][1][d] = min over rows of floor(k_d / 2^e),
+ * within -127 .. 127, where e = exponents[page][head] is the least one in -60 .. 40 with |k_d| <= 127 * 2^e for all k_d of the page and head, or 40 if
+ * there is none (what is larger, infinities among it, has the code +-127).  A NaN counts as 0.  Rounding of roundings upwards (downwards) by powers of two is rounding once, so bounds that
+ * take new rows in are those of all rows together.
+ * ba_page_bounds takes in tokens from_token[s] .. seq_len[s] - 1 of every sequence (from_token null: from 0): pages that begin with one of them
+ * are bounded anew, a page that they continue is added to.  A page that is added to belongs to one sequence of the call; one that is bounded
+ * anew may be several's, with the same tokens.  Pages without new tokens stay as they are.
+ * codes: device, [n_pages][n_kv_heads][2][head_dim], 16-byte aligned; exponents: device, [n_pages][n_kv_heads].
+ */
+typedef struct ba_page_bound_table {
+  int8_t *codes;
+  int8_t *exponents;
+} ba_page_bound_table;
+int32_t ba_page_bounds(const ba_heads *heads, const ba_paged_cache *cache,
+                       const ba_page_bound_table *bounds, const int32_t *from_token,
+                       const int32_t *seq_len, int32_t max_len, void *stream);
+
+/*
+ * The pages that a step reads: for every sequence and KV head the n_select pages (or all, if it has fewer) with the largest
+ *   score(page) = max over the call's q_per_seq query rows i and heads h of the KV head of 2^(e_ih + e) sum_d max(c_ihd hi_d, c_ihd lo_d),
+ * a bound on what any key of the page scores, of the query in 8 bits: c_ihd = round(q_ihd / 2^e_ih), to nearest, ties to even, within -127 .. 127, e_ih as
+ * above for the row's values.  The sums are whole numbers and exact.  Of equal scores the earlier page.  Taken first, whatever they score: a sequence's first n_first
+ * pages, its last n_last ones, and those that hold its newest q_per_seq tokens; n_select has room for all of these.  A page that is not there is not taken.
+ * selected_out: device ints, [n_seqs][n_kv_heads][n_select], numbers of pages within the sequence (entries of its row of the page
+ * table), ascending, -1 behind the last.  scores_out: device floats, nullable, the same shape: their scores, -infinity behind the last.
+ * ws: 256-byte aligned, at least ba_page_select_workspace_bytes() bytes (may be null when that is 0).
+ */
+int32_t ba_page_select(const ba_heads *heads, const ba_paged_cache *cache,
+                       const ba_page_bound_table *bounds, const ba_tensor *q, int32_t q_per_seq,
+                       const int32_t *seq_len, int32_t max_len, int32_t n_select, int32_t n_first,
+                       int32_t n_last, int32_t *selected_out, float *scores_out, void *ws,
+                       size_t ws_bytes, void *stream);
+size_t ba_page_select_workspace_bytes(const ba_heads *heads, int32_t n_seqs, int32_t page_rows,
+                                      int32_t max_len);
+
+/*
+ * ba_paged_attention over the selected pages alone: row (i, h) sees the tokens t <= p(i) that lie in pages selected[s][g][0 .. n_select - 1] of its
+ * KV head g = h / (n_q_heads / n_kv_heads).  selected: device ints as ba_page_select leaves them, ascending; entries behind the first one that is not
+ * above the entry in front of it, or is negative, count for nothing, nor do pages that are not there.  lse_out: of these tokens.  Everything else as in ba_paged_attention
+ * without groups.
+ */
+int32_t ba_paged_attention_selected(const ba_heads *heads, const ba_paged_cache *cache,
+                                    const ba_tensor *q, const ba_tensor *o_out, float *lse_out,
+                                    int32_t q_per_seq, const int32_t *seq_len, int32_t max_len,
+                                    const int32_t *selected, int32_t n_select, void *ws,
+                                    size_t ws_bytes, void *stream);
+size_t ba_paged_attention_selected_workspace_bytes(const ba_heads *heads, int32_t n_seqs,
+                                                   int32_t q_per_seq, int32_t page_rows,
+                                                   int32_t max_len, int32_t n_select);
+
+/*
  * The schedule of a call, for inspection and tests: the work items the host planner hands to the
  * kernels, computed by the code the calls themselves use.  Host only: no device is touched, so
  * these run on a machine without a GPU.

@@ -34,6 +34,9 @@ EXPORTS = ["ba_version", "ba_status_string", "ba_last_error", "ba_profile_begin"
            "ba_block_attention_prompts_backward", "ba_block_attention_prompts_backward_workspace_bytes",
            "ba_norm_rotate", "ba_norm_rotate_backward", "ba_norm_rotate_backward_workspace_bytes",
            "ba_paged_append", "ba_paged_attention", "ba_paged_attention_workspace_bytes",
+           "ba_paged_key_weights", "ba_paged_key_weights_workspace_bytes", "ba_paged_evict", "ba_paged_evict_workspace_bytes",
+           "ba_page_bounds", "ba_page_select", "ba_page_select_workspace_bytes",
+           "ba_paged_attention_selected", "ba_paged_attention_selected_workspace_bytes",
            "ba_schedule_final_block", "ba_schedule_encode_blocks", "ba_schedule_prompts",
            "ba_measure_xcd_speed", "ba_measure_xcd_speed_workspace_bytes", "ba_diag_final_block_phases",
            "ba_diag_mfma_ceiling", "ba_diag_mfma_ceiling_workspace_bytes"]
@@ -68,12 +71,20 @@ class BaPagedCache(ctypes.Structure):
                 ("stride_table", ctypes.c_int64), ("n_seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
 
 
+class BaPageBoundTable(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("exponents", ctypes.c_void_p)]
+
+
 class _KnownNorm(ctypes.Structure):  # (as the native half of this face reads them)
     _fields_ = [("norm", BaHeadNorm), ("head_dim", ctypes.c_int32)]
 
 
 class _KnownCache(ctypes.Structure):
     _fields_ = [("cache", BaPagedCache), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class _KnownBounds(ctypes.Structure):
+    _fields_ = [("bounds", BaPageBoundTable), ("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
 
 
 class BaError(RuntimeError):
@@ -162,6 +173,25 @@ def load():
                                        ctypes.c_size_t, _VP]
     lib.ba_paged_attention_workspace_bytes.restype = ctypes.c_size_t
     lib.ba_paged_attention_workspace_bytes.argtypes = [_HP, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _I32P, _I32P]
+    _BP, _I32, _I64 = ctypes.POINTER(BaPageBoundTable), ctypes.c_int32, ctypes.c_int64
+    lib.ba_paged_key_weights.restype = _I32
+    lib.ba_paged_key_weights.argtypes = [_HP, _CP, _TP, _VP, _VP, _VP, _I64, ctypes.c_float, _I32, _VP, _I32, _I32, _I32P, _I32P, _VP, ctypes.c_size_t, _VP]
+    lib.ba_paged_key_weights_workspace_bytes.restype = ctypes.c_size_t
+    lib.ba_paged_key_weights_workspace_bytes.argtypes = [_HP, _I32, _I32, _I32, _I32, _I32P, _I32P]
+    lib.ba_paged_evict.restype = _I32
+    lib.ba_paged_evict.argtypes = [_HP, _CP, _CP, _VP, _I64, _VP, _I32, _I32, _I32, _I32, _VP, _VP, _I64, _VP, _VP, ctypes.c_size_t, _VP]
+    lib.ba_paged_evict_workspace_bytes.restype = ctypes.c_size_t
+    lib.ba_paged_evict_workspace_bytes.argtypes = [_HP, _I32, _I32, _I32]
+    lib.ba_page_bounds.restype = _I32
+    lib.ba_page_bounds.argtypes = [_HP, _CP, _BP, _VP, _VP, _I32, _VP]
+    lib.ba_page_select.restype = _I32
+    lib.ba_page_select.argtypes = [_HP, _CP, _BP, _TP, _I32, _VP, _I32, _I32, _I32, _I32, _VP, _VP, _VP, ctypes.c_size_t, _VP]
+    lib.ba_page_select_workspace_bytes.restype = ctypes.c_size_t
+    lib.ba_page_select_workspace_bytes.argtypes = [_HP, _I32, _I32, _I32]
+    lib.ba_paged_attention_selected.restype = _I32
+    lib.ba_paged_attention_selected.argtypes = [_HP, _CP, _TP, _TP, _VP, _I32, _VP, _I32, _VP, _I32, _VP, ctypes.c_size_t, _VP]
+    lib.ba_paged_attention_selected_workspace_bytes.restype = ctypes.c_size_t
+    lib.ba_paged_attention_selected_workspace_bytes.argtypes = [_HP, _I32, _I32, _I32, _I32, _I32]
     _WP = ctypes.POINTER(BaWorkItem)
     lib.ba_schedule_final_block.restype = ctypes.c_int64
     lib.ba_schedule_final_block.argtypes = [_HP, ctypes.c_int32, _I32P, _I32P, ctypes.c_int32, _WP, ctypes.c_int64]
@@ -215,6 +245,9 @@ def _load_native(lib):
                                    "ba_final_block_attention_cached", "ba_block_attention_prompts", "ba_block_attention_prompts_backward")))
                 _face.setup_paged(HeadNorm, PagedCache, tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in
                                                               ("ba_norm_rotate", "ba_norm_rotate_backward", "ba_paged_append", "ba_paged_attention")))
+                _face.setup_long(PageBounds, tuple(ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in
+                                                   ("ba_paged_key_weights", "ba_paged_evict", "ba_page_bounds", "ba_page_select",
+                                                    "ba_paged_attention_selected")))
                 return _face
             why = f"it was built for torch {built_for}, this is {torch.__version__}"
     import warnings
@@ -318,6 +351,29 @@ class PagedCache:
         if (self.n_kv_heads, self.head_dim) != (heads.n_kv_heads, heads.head_dim):
             raise ValueError(f"cache: {self.n_kv_heads} heads of {self.head_dim}, the call's head description says "
                              f"{heads.n_kv_heads} of {heads.head_dim}")
+
+
+class PageBounds:
+    """Bounds of a cache's pages (ba_page_bound_table): ``codes`` int8 [pages, KV heads, 2, D] and ``exponents`` int8 [pages, KV heads],
+    contiguous, on the GPU.  Keeps them alive."""
+
+    def __init__(self, codes, exponents):
+        import torch
+        for name, t, dims in (("codes", codes, 4), ("exponents", exponents, 2)):
+            if not t.is_cuda or t.dtype != torch.int8 or t.dim() != dims or not t.is_contiguous():
+                raise ValueError(f"{name}: expected a contiguous int8 tensor of {dims} dimensions in GPU memory")
+        if codes.shape[2] != 2 or tuple(codes.shape[:2]) != tuple(exponents.shape):
+            raise ValueError("codes and exponents: expected [pages, heads, 2, head_dim] and [pages, heads]")
+        self.codes, self.exponents = codes, exponents
+        self.n_pages, self.n_kv_heads, _, self.head_dim = codes.shape
+        self.known = _KnownBounds(BaPageBoundTable(codes.data_ptr(), exponents.data_ptr()), self.n_pages, self.n_kv_heads, self.head_dim)
+        self.c = self.known.bounds
+
+    def _check(self, heads: "Heads", cache: PagedCache) -> None:
+        if (self.n_kv_heads, self.head_dim) != (heads.n_kv_heads, heads.head_dim):
+            raise ValueError(f"bounds: {self.n_kv_heads} heads of {self.head_dim}, the call's head description says {heads.n_kv_heads} of {heads.head_dim}")
+        if self.n_pages < cache.k_pages.shape[0]:
+            raise ValueError(f"bounds: {self.n_pages} pages, the cache has {cache.k_pages.shape[0]}")
 
 
 _dtype_codes = None  # torch dtype -> BA_DTYPE_*, filled on first use (torch is imported lazily)
@@ -732,6 +788,125 @@ def ba_paged_attention(heads: Heads, cache: PagedCache, q, o_out, lse_out, seq_l
     _check(load().ba_paged_attention(ctypes.byref(heads.c), ctypes.byref(cache.c), _ref(tq), _ref(to), lse, q_per_seq,
                                      _dev_ints(seq_len, "seq_len", cache.n_seqs), max_len, _n_groups(cu, pre), _ip(cu), _ip(pre), wp, wb,
                                      _stream_handle(stream)))
+
+
+def _per_key(t, name: str, heads: Heads, n_seqs: int, least: int):
+    """float32 [sequences, KV heads, at least `least`], sequences n_kv_heads heads apart -> pointer and floats from head to head (None stays None)."""
+    if t is None:
+        return None, 0
+    import torch
+    if not t.is_cuda or t.dtype != torch.float32 or t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name}: expected a float32 [sequences, heads, tokens] tensor in GPU memory, its rows contiguous")
+    if t.shape[1] != heads.n_kv_heads or t.shape[0] < n_seqs or t.shape[2] < least:
+        raise ValueError(f"{name}: {tuple(t.shape)}, the call needs [{n_seqs}, {heads.n_kv_heads}, {least}] at least")
+    stride = t.stride(1) if heads.n_kv_heads > 1 else t.stride(0) if t.shape[0] > 1 else max(t.shape[2], 1)
+    if t.shape[0] > 1 and t.stride(0) != heads.n_kv_heads * stride:
+        raise ValueError(f"{name}: the heads of all sequences have to be equally far apart")
+    return ctypes.c_void_p(t.data_ptr()), stride
+
+
+def _lists(t, name: str, heads: Heads, n_seqs: int, floats: bool = False, width: Optional[int] = None):
+    """int32 (float32) [sequences, KV heads, n], contiguous, on the GPU -> pointer and n (None stays None)."""
+    if t is None:
+        return None, 0
+    import torch
+    if not t.is_cuda or t.dtype != (torch.float32 if floats else torch.int32) or t.dim() != 3 or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {'float32' if floats else 'int32'} [sequences, heads, n] tensor in GPU memory")
+    if t.shape[0] < n_seqs or t.shape[1] != heads.n_kv_heads or (width is not None and t.shape[2] != width):
+        raise ValueError(f"{name}: {tuple(t.shape)}, the call has {n_seqs} sequences of {heads.n_kv_heads} heads" + (f" and {width} entries" if width is not None else ""))
+    return ctypes.c_void_p(t.data_ptr()), int(t.shape[2])
+
+
+def ba_paged_key_weights_workspace_bytes(heads: Heads, n_seqs: int, q_per_seq: int, max_len: int, cu_group=None, prefix_len=None) -> int:
+    cu, pre = _ints(cu_group), _ints(prefix_len)
+    return int(load().ba_paged_key_weights_workspace_bytes(ctypes.byref(heads.c), n_seqs, q_per_seq, max_len, _n_groups(cu, pre), _ip(cu), _ip(pre)))
+
+
+def ba_paged_key_weights(heads: Heads, cache: PagedCache, q, lse, weights_in, weights_out, decay: float, seq_len, max_len: int, cu_group=None,
+                         prefix_len=None, q_per_seq: int = 1, ws=None, stream=None) -> None:
+    """weights_in (may be None, or weights_out itself), weights_out: float32 [sequences, KV heads, at least max_len]."""
+    if _done(_face().key_weights(heads, q, lse, weights_in, weights_out, seq_len, cu_group, prefix_len, cache, decay, max_len, q_per_seq, ws, stream)):
+        return
+    cache._check(heads)
+    n = cache.n_seqs * q_per_seq
+    cu, pre = _ints(cu_group), _ints(prefix_len)
+    tq, lse_p = _tensor(q, "q", heads.n_q_heads, heads.head_dim, n), _lse(lse, "lse", n, heads.n_q_heads)
+    (wi, si), (wo, so) = (_per_key(t, name, heads, cache.n_seqs, max_len) for name, t in (("weights_in", weights_in), ("weights_out", weights_out)))
+    if weights_in is not None and weights_out is not None and si != so:
+        raise ValueError("weights_in and weights_out: one layout for both")
+    wp, wb = _ws(ws)
+    _check(load().ba_paged_key_weights(ctypes.byref(heads.c), ctypes.byref(cache.c), _ref(tq), lse_p, wi, wo, so, float(decay), q_per_seq,
+                                       _dev_ints(seq_len, "seq_len", cache.n_seqs), max_len, _n_groups(cu, pre), _ip(cu), _ip(pre), wp, wb,
+                                       _stream_handle(stream)))
+
+
+def ba_paged_evict_workspace_bytes(heads: Heads, n_seqs: int, max_len: int, n_keep: int) -> int:
+    return int(load().ba_paged_evict_workspace_bytes(ctypes.byref(heads.c), n_seqs, max_len, n_keep))
+
+
+def ba_paged_evict(heads: Heads, cache: PagedCache, to: PagedCache, weights, seq_len, max_len: int, n_keep: int, n_first: int, n_last: int, kept_out,
+                   weights_out=None, len_out=None, ws=None, stream=None) -> None:
+    """kept_out: int32 [sequences, KV heads, n_keep]; weights_out: float32 [sequences, KV heads, at least n_keep]; len_out: int32 [sequences]."""
+    if _done(_face().evict(heads, weights, seq_len, kept_out, weights_out, len_out, cache, to, max_len, n_keep, n_first, n_last, ws, stream)):
+        return
+    cache._check(heads)
+    to._check(heads)
+    n = cache.n_seqs
+    w, sw = _per_key(weights, "weights", heads, n, max_len)
+    wo, so = _per_key(weights_out, "weights_out", heads, n, n_keep)
+    kept, _ = _lists(kept_out, "kept_out", heads, n, width=n_keep)
+    wp, wb = _ws(ws)
+    _check(load().ba_paged_evict(ctypes.byref(heads.c), ctypes.byref(cache.c), ctypes.byref(to.c), w, sw, _dev_ints(seq_len, "seq_len", n), max_len, n_keep,
+                                 n_first, n_last, kept, wo, so, _dev_ints(len_out, "len_out", n), wp, wb, _stream_handle(stream)))
+
+
+def ba_page_bounds(heads: Heads, cache: PagedCache, bounds: PageBounds, from_token, seq_len, max_len: int, stream=None) -> None:
+    """from_token (may be None), seq_len: int32 [sequences] on the GPU."""
+    if _done(_face().page_bounds(heads, from_token, seq_len, cache, bounds, max_len, stream)):
+        return
+    cache._check(heads)
+    bounds._check(heads, cache)
+    _check(load().ba_page_bounds(ctypes.byref(heads.c), ctypes.byref(cache.c), ctypes.byref(bounds.c), _dev_ints(from_token, "from_token", cache.n_seqs),
+                                 _dev_ints(seq_len, "seq_len", cache.n_seqs), max_len, _stream_handle(stream)))
+
+
+def ba_page_select_workspace_bytes(heads: Heads, n_seqs: int, page_rows: int, max_len: int) -> int:
+    return int(load().ba_page_select_workspace_bytes(ctypes.byref(heads.c), n_seqs, page_rows, max_len))
+
+
+def ba_page_select(heads: Heads, cache: PagedCache, bounds: PageBounds, q, seq_len, max_len: int, selected_out, scores_out=None, n_first: int = 1,
+                   n_last: int = 1, q_per_seq: int = 1, ws=None, stream=None) -> None:
+    """selected_out: int32 [sequences, KV heads, n_select]; scores_out: float32 of that shape, or None."""
+    if _done(_face().page_select(heads, q, seq_len, selected_out, scores_out, cache, bounds, max_len, n_first, n_last, q_per_seq, ws, stream)):
+        return
+    cache._check(heads)
+    bounds._check(heads, cache)
+    n = cache.n_seqs
+    tq = _tensor(q, "q", heads.n_q_heads, heads.head_dim, n * q_per_seq)
+    sel, n_select = _lists(selected_out, "selected_out", heads, n)
+    scores, _ = _lists(scores_out, "scores_out", heads, n, floats=True, width=n_select)
+    wp, wb = _ws(ws)
+    _check(load().ba_page_select(ctypes.byref(heads.c), ctypes.byref(cache.c), ctypes.byref(bounds.c), _ref(tq), q_per_seq,
+                                 _dev_ints(seq_len, "seq_len", n), max_len, n_select, n_first, n_last, sel, scores, wp, wb, _stream_handle(stream)))
+
+
+def ba_paged_attention_selected_workspace_bytes(heads: Heads, n_seqs: int, q_per_seq: int, page_rows: int, max_len: int, n_select: int) -> int:
+    return int(load().ba_paged_attention_selected_workspace_bytes(ctypes.byref(heads.c), n_seqs, q_per_seq, page_rows, max_len, n_select))
+
+
+def ba_paged_attention_selected(heads: Heads, cache: PagedCache, q, o_out, lse_out, seq_len, max_len: int, selected, q_per_seq: int = 1, ws=None,
+                                stream=None) -> None:
+    """selected: int32 [sequences, KV heads, n_select] as ba_page_select leaves them."""
+    if _done(_face().paged_attention_selected(heads, q, o_out, lse_out, seq_len, selected, cache, max_len, q_per_seq, ws, stream)):
+        return
+    cache._check(heads)
+    n = cache.n_seqs * q_per_seq
+    tq, to = _tensor(q, "q", heads.n_q_heads, heads.head_dim, n), _tensor(o_out, "o_out", heads.n_q_heads, heads.head_dim, n)
+    lse = _lse(lse_out, "lse_out", n, heads.n_q_heads)
+    sel, n_select = _lists(selected, "selected", heads, cache.n_seqs)
+    wp, wb = _ws(ws)
+    _check(load().ba_paged_attention_selected(ctypes.byref(heads.c), ctypes.byref(cache.c), _ref(tq), _ref(to), lse, q_per_seq,
+                                              _dev_ints(seq_len, "seq_len", cache.n_seqs), max_len, sel, n_select, wp, wb, _stream_handle(stream)))
 
 
 def _schedule(fn, *args):

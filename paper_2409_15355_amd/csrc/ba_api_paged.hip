@@ -9,22 +9,15 @@
 
 #include "../../include/ba.h"
 #include "ba_api_common.h"
+#include "ba_api_paged.h"
 #include "ba_internal.h"
 #include "ba_paged.h"
 #include "ba_plan.h"
 
 namespace ba {
 namespace api {
-namespace {
 
 // ---- where a tensor lies: its rows [0, tokens) -------------------------------------------------------
-struct Extent {
-  int64_t lo, hi;           // bytes
-  int64_t period, width;    // bytes from row to row, bytes of a row from its first head to its last
-  int64_t step, head;       // bytes from head to head, bytes of a head
-  int64_t rows;
-  int32_t heads;
-};
 Extent extent(const ba_tensor *t, int64_t tokens, int n_heads, int D) {
   const int64_t es = (int64_t)elt_size(t->dtype);
   Extent x;
@@ -69,6 +62,72 @@ bool same_place(const ba_tensor *a, const ba_tensor *b) {
   return a->ptr == b->ptr && a->stride_tok == b->stride_tok && a->stride_head == b->stride_head;
 }
 
+int32_t check_int_array(const void *p, const char *name) {
+  return (uintptr_t)p & 3 ? fail(BA_ERR_ALIGNMENT, "%s: not aligned to its type", name) : BA_OK;
+}
+
+int32_t check_apart(const ba_tensor *a, const char *a_name, int a_heads, const ba_tensor *b, const char *b_name, int b_heads, int64_t tokens, int D) {
+  if (!a || !b || apart(extent(a, tokens, a_heads, D), extent(b, tokens, b_heads, D))) return BA_OK;
+  return fail(BA_ERR_INVALID_ARG, "%s overlaps %s", a_name, b_name);
+}
+
+// ---- the paged cache -----------------------------------------------------------------------------------
+int32_t check_cache(const ba_paged_cache *c, const ba_heads *h) {
+  int32_t rc;
+  if (!c) return fail(BA_ERR_INVALID_ARG, "cache: null");
+  if ((rc = check_tensor(&c->k, "cache k", false, h->head_dim, h->n_kv_heads))) return rc;
+  if ((rc = check_tensor(&c->v, "cache v", false, h->head_dim, h->n_kv_heads))) return rc;
+  if (c->n_pages < 1 || c->page_rows < 1) return fail(BA_ERR_INVALID_ARG, "cache: at least one page of at least one row");
+  if (c->n_seqs < 0 || c->max_pages < 0) return fail(BA_ERR_INVALID_ARG, "cache: negative sequence or page count");
+  if (((c->k_stride_page | c->v_stride_page) * 2) & 15) return fail(BA_ERR_ALIGNMENT, "cache: page strides must be 16-byte aligned");
+  if (c->k_stride_page < 0 || c->v_stride_page < 0) return fail(BA_ERR_INVALID_ARG, "cache: negative page stride");
+  if (std::max(c->k_stride_page, c->v_stride_page) >= (int64_t)1 << 35)  // (counted in 32-bit units of 16 bytes)
+    return fail(BA_ERR_UNSUPPORTED, "cache: pages of 64 GB and more");
+  if (c->n_seqs > 0 && c->max_pages > 0) {
+    if (!c->page_table) return fail(BA_ERR_INVALID_ARG, "page_table: null");
+    if (c->stride_table < 0 || (c->n_seqs > 1 && c->stride_table < c->max_pages))
+      return fail(BA_ERR_INVALID_ARG, "page_table: rows of the table overlap");
+    if ((rc = check_int_array(c->page_table, "page_table"))) return rc;
+  }
+  if ((int64_t)c->max_pages * c->page_rows > 0x7fffffff - 1024)
+    return fail(BA_ERR_UNSUPPORTED, "cache: sequences of 2^31 rows and more");
+  return BA_OK;
+}
+Extent pool_extent(const ba_tensor *t, int64_t stride_page, const ba_paged_cache *c, const ba_heads *h) {
+  Extent x = extent(t, c->page_rows, h->n_kv_heads, h->head_dim);
+  x.hi += (int64_t)(c->n_pages - 1) * stride_page * 2;
+  x.period = 0;  // (nothing lies side by side with its rows)
+  return x;
+}
+
+int32_t check_groups(int32_t n_seqs, int32_t max_len, int32_t n_groups, const int32_t *cu_group, const int32_t *prefix_len) {
+  if (n_groups < 0) return fail(BA_ERR_INVALID_ARG, "negative group count");
+  if (n_groups == 0) return BA_OK;
+  if (!cu_group || !prefix_len) return fail(BA_ERR_INVALID_ARG, "cu_group / prefix_len: null");
+  if (cu_group[0] != 0) return fail(BA_ERR_INVALID_ARG, "cu_group[0] must be 0");
+  for (int g = 0; g < n_groups; ++g) {
+    if (cu_group[g + 1] < cu_group[g]) return fail(BA_ERR_INVALID_ARG, "group %d: cu_group decreases", g);
+    if (prefix_len[g] < 0 || prefix_len[g] > max_len) return fail(BA_ERR_INVALID_ARG, "group %d: prefix_len outside 0 .. max_len", g);
+  }
+  if (cu_group[n_groups] != n_seqs) return fail(BA_ERR_INVALID_ARG, "cu_group ends at %d, the call has %d sequences", cu_group[n_groups], n_seqs);
+  return BA_OK;
+}
+
+int32_t check_paged_sizes(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len) {
+  int32_t rc;
+  if ((rc = check_heads(h, true))) return rc;
+  if (n_seqs < 0) return fail(BA_ERR_INVALID_ARG, "negative sequence count");
+  if (nq < 1) return fail(BA_ERR_INVALID_ARG, "q_per_seq must be positive");
+  if (max_len < 0) return fail(BA_ERR_INVALID_ARG, "negative max_len");
+  // (row, key and item numbers are 32-bit)
+  if (max_len > (1 << 30)) return fail(BA_ERR_UNSUPPORTED, "max_len beyond 2^30");
+  if ((int64_t)n_seqs * nq > (1 << 28) || (int64_t)n_seqs * nq * h->n_q_heads > (1 << 28))
+    return fail(BA_ERR_UNSUPPORTED, "more than 2^28 query rows in one call");
+  return BA_OK;
+}
+
+namespace {
+
 int32_t check_norm(const ba_head_norm *n) {
   if (n->dtype != BA_DTYPE_BF16 && n->dtype != BA_DTYPE_F32) return fail(BA_ERR_UNSUPPORTED, "norm: dtype %d of the gains not supported", n->dtype);
   if (!(n->eps > 0.f) || !std::isfinite(n->eps)) return fail(BA_ERR_INVALID_ARG, "norm: eps must be positive");
@@ -78,10 +137,6 @@ int32_t check_norm(const ba_head_norm *n) {
 int32_t check_rope_mode(int32_t rope_mode) {
   return rope_mode == BA_ROPE_NONE || rope_mode == BA_ROPE_APPLY ? BA_OK : fail(BA_ERR_INVALID_ARG, "rope_mode %d unknown", rope_mode);
 }
-int32_t check_int_array(const void *p, const char *name) {
-  return (uintptr_t)p & 3 ? fail(BA_ERR_ALIGNMENT, "%s: not aligned to its type", name) : BA_OK;
-}
-
 void set_source(HeadRowsParams *p, int kind, const ba_tensor *t, int n_heads) {
   p->src[kind] = t->ptr;
   p->src_st[kind] = t->stride_tok;
@@ -126,11 +181,6 @@ int32_t check_pair(const ba_tensor *x, const char *name, const ba_tensor *y, con
     return fail(BA_ERR_INVALID_ARG, "%s overlaps %s without being exactly in place", y_name, name);
   return BA_OK;
 }
-int32_t check_apart(const ba_tensor *a, const char *a_name, int a_heads, const ba_tensor *b, const char *b_name, int b_heads, int64_t tokens, int D) {
-  if (!a || !b || apart(extent(a, tokens, a_heads, D), extent(b, tokens, b_heads, D))) return BA_OK;
-  return fail(BA_ERR_INVALID_ARG, "%s overlaps %s", a_name, b_name);
-}
-
 // Workgroups of the backward pass: as many as the chip holds at a time, shared out by heads (each tensor's share is the same without the
 // other: so are the bits of its gain's gradient).
 void backward_wgs(int64_t tokens, const ba_heads *h, bool q, bool k, NormBackwardParams *p) {
@@ -146,35 +196,6 @@ void backward_wgs(int64_t tokens, const ba_heads *h, bool q, bool k, NormBackwar
   p->n_wg = p->wg_q + (k ? (int32_t)std::min<int64_t>(tokens, std::max<int64_t>(1, kNormBwdMaxWg * (all - hq) / all)) : 0);
 }
 
-// ---- the paged cache -----------------------------------------------------------------------------------
-int32_t check_cache(const ba_paged_cache *c, const ba_heads *h) {
-  int32_t rc;
-  if (!c) return fail(BA_ERR_INVALID_ARG, "cache: null");
-  if ((rc = check_tensor(&c->k, "cache k", false, h->head_dim, h->n_kv_heads))) return rc;
-  if ((rc = check_tensor(&c->v, "cache v", false, h->head_dim, h->n_kv_heads))) return rc;
-  if (c->n_pages < 1 || c->page_rows < 1) return fail(BA_ERR_INVALID_ARG, "cache: at least one page of at least one row");
-  if (c->n_seqs < 0 || c->max_pages < 0) return fail(BA_ERR_INVALID_ARG, "cache: negative sequence or page count");
-  if (((c->k_stride_page | c->v_stride_page) * 2) & 15) return fail(BA_ERR_ALIGNMENT, "cache: page strides must be 16-byte aligned");
-  if (c->k_stride_page < 0 || c->v_stride_page < 0) return fail(BA_ERR_INVALID_ARG, "cache: negative page stride");
-  if (std::max(c->k_stride_page, c->v_stride_page) >= (int64_t)1 << 35)  // (counted in 32-bit units of 16 bytes)
-    return fail(BA_ERR_UNSUPPORTED, "cache: pages of 64 GB and more");
-  if (c->n_seqs > 0 && c->max_pages > 0) {
-    if (!c->page_table) return fail(BA_ERR_INVALID_ARG, "page_table: null");
-    if (c->stride_table < 0 || (c->n_seqs > 1 && c->stride_table < c->max_pages))
-      return fail(BA_ERR_INVALID_ARG, "page_table: rows of the table overlap");
-    if ((rc = check_int_array(c->page_table, "page_table"))) return rc;
-  }
-  if ((int64_t)c->max_pages * c->page_rows > 0x7fffffff - 1024)
-    return fail(BA_ERR_UNSUPPORTED, "cache: sequences of 2^31 rows and more");
-  return BA_OK;
-}
-Extent pool_extent(const ba_tensor *t, int64_t stride_page, const ba_paged_cache *c, const ba_heads *h) {
-  Extent x = extent(t, c->page_rows, h->n_kv_heads, h->head_dim);
-  x.hi += (int64_t)(c->n_pages - 1) * stride_page * 2;
-  x.period = 0;  // (nothing lies side by side with its rows)
-  return x;
-}
-
 // ---- plan of an attention call ---------------------------------------------------------------------------
 // Sequences [seq0, seq0 + n_seqs) with at most kMost groups that share something.
 struct PagedPlan {
@@ -185,19 +206,6 @@ struct PagedPlan {
   int64_t keys;   // of all prefixes, and as many as the sequences may have of their own
   PagedGroups groups;
 };
-
-int32_t check_groups(int32_t n_seqs, int32_t max_len, int32_t n_groups, const int32_t *cu_group, const int32_t *prefix_len) {
-  if (n_groups < 0) return fail(BA_ERR_INVALID_ARG, "negative group count");
-  if (n_groups == 0) return BA_OK;
-  if (!cu_group || !prefix_len) return fail(BA_ERR_INVALID_ARG, "cu_group / prefix_len: null");
-  if (cu_group[0] != 0) return fail(BA_ERR_INVALID_ARG, "cu_group[0] must be 0");
-  for (int g = 0; g < n_groups; ++g) {
-    if (cu_group[g + 1] < cu_group[g]) return fail(BA_ERR_INVALID_ARG, "group %d: cu_group decreases", g);
-    if (prefix_len[g] < 0 || prefix_len[g] > max_len) return fail(BA_ERR_INVALID_ARG, "group %d: prefix_len outside 0 .. max_len", g);
-  }
-  if (cu_group[n_groups] != n_seqs) return fail(BA_ERR_INVALID_ARG, "cu_group ends at %d, the call has %d sequences", cu_group[n_groups], n_seqs);
-  return BA_OK;
-}
 
 // The plan of the sequences from those of group g0 on.  Without groups: of all of them.
 void plan_paged(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, int32_t n_groups, const int32_t *cu_group,
@@ -283,6 +291,25 @@ size_t plan_bytes(const PagedPlan &pl, const ba_heads *h, int32_t nq) {
   return align256(rows * pl.parts * h->head_dim * 2) + align256(rows * pl.parts * 16);
 }
 
+// The plan of a call over listed pages of `keys` keys at most: as without groups, in parts whose lists fit a workgroup.
+void plan_selected(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t keys, int cus, PagedPlan *pl) {
+  plan_paged(h, n_seqs, nq, keys, 0, nullptr, nullptr, 0, cus, pl);
+  pl->own_chunk = std::min(pl->own_chunk, kSelectedMaxChunk / 64 * 64);
+  pl->parts = pl->own_splits = std::max(1, (keys + pl->own_chunk - 1) / pl->own_chunk);
+  pl->items = (int64_t)n_seqs * h->n_kv_heads * pl->own_row_tiles * pl->own_splits;
+}
+int32_t selected_keys(int32_t page_rows, int32_t max_len, int32_t n_select) {
+  return (int32_t)std::min<int64_t>((int64_t)n_select * page_rows, max_len);
+}
+int32_t check_selected_plan(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t page_rows, int32_t max_len, int32_t n_select, PagedPlan *pl, size_t *bytes) {
+  plan_selected(h, n_seqs, nq, selected_keys(page_rows, max_len, n_select), num_cus(), pl);
+  if (pl->items > kMaxWorkgroups) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
+  *bytes = plan_bytes(*pl, h, nq);
+  if (*bytes > 0 && ((int64_t)n_seqs * nq * h->n_q_heads + kPagedMergeRows - 1) / kPagedMergeRows > kMaxWorkgroups)
+    return fail(BA_ERR_UNSUPPORTED, "2^28 query rows and more in one launch");
+  return BA_OK;
+}
+
 // All plans of a call: whether they can be launched, and the workspace of the largest.
 int32_t check_plans(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, int32_t n_groups, const int32_t *cu_group,
                     const int32_t *prefix_len, size_t *bytes) {
@@ -301,17 +328,69 @@ int32_t check_plans(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_l
   return BA_OK;
 }
 
-int32_t check_paged_sizes(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len) {
+// Query rows and outputs of an attention call.
+int32_t check_rows(const ba_heads *heads, const ba_paged_cache *cache, const ba_tensor *q, const ba_tensor *o_out, int32_t n_seqs, int32_t q_per_seq,
+                   int32_t max_len) {
   int32_t rc;
-  if ((rc = check_heads(h, true))) return rc;
-  if (n_seqs < 0) return fail(BA_ERR_INVALID_ARG, "negative sequence count");
-  if (nq < 1) return fail(BA_ERR_INVALID_ARG, "q_per_seq must be positive");
-  if (max_len < 0) return fail(BA_ERR_INVALID_ARG, "negative max_len");
-  // (row, key and item numbers are 32-bit)
-  if (max_len > (1 << 30)) return fail(BA_ERR_UNSUPPORTED, "max_len beyond 2^30");
-  if ((int64_t)n_seqs * nq > (1 << 28) || (int64_t)n_seqs * nq * h->n_q_heads > (1 << 28))
-    return fail(BA_ERR_UNSUPPORTED, "more than 2^28 query rows in one call");
+  const int64_t tokens = (int64_t)n_seqs * q_per_seq;
+  if ((rc = check_tensor(q, "q", false, heads->head_dim, heads->n_q_heads)) || (rc = check_tensor(o_out, "o_out", false, heads->head_dim, heads->n_q_heads)))
+    return rc;
+  if (max_len > (int64_t)cache->max_pages * cache->page_rows) return fail(BA_ERR_INVALID_ARG, "max_len reaches beyond the page table");
+  // (a work item reads the query rows that it writes and no others, but the pages are everybody's)
+  const Extent out = extent(o_out, tokens, heads->n_q_heads, heads->head_dim);
+  if (!same_place(q, o_out) && !apart(out, extent(q, tokens, heads->n_q_heads, heads->head_dim)))
+    return fail(BA_ERR_INVALID_ARG, "o_out overlaps q without being exactly in place");
+  if (!apart(pool_extent(&cache->k, cache->k_stride_page, cache, heads), out) || !apart(pool_extent(&cache->v, cache->v_stride_page, cache, heads), out))
+    return fail(BA_ERR_INVALID_ARG, "o_out overlaps the cache");
   return BA_OK;
+}
+// What a launch for the sequences of a plan is told.
+void set_attention(PagedAttnParams *p, const ba_heads *heads, const ba_paged_cache *cache, const ba_tensor *q, const ba_tensor *o_out, float *lse_out,
+                   int32_t q_per_seq, const int32_t *seq_len, int32_t max_len, const PagedPlan &pl, void *ws) {
+  const int64_t tok0 = (int64_t)pl.seq0 * q_per_seq;
+  memset(p, 0, sizeof(*p));
+  p->q = (const uint16_t *)q->ptr + tok0 * q->stride_tok;
+  p->q_st = q->stride_tok, p->q_sh = q->stride_head;
+  p->o = (uint16_t *)o_out->ptr + tok0 * o_out->stride_tok;
+  p->o_st = o_out->stride_tok, p->o_sh = o_out->stride_head;
+  p->lse = lse_out ? lse_out + tok0 * heads->n_q_heads : nullptr;
+  p->k = (const uint16_t *)cache->k.ptr, p->v = (const uint16_t *)cache->v.ptr;
+  p->k_sh = cache->k.stride_head, p->v_sh = cache->v.stride_head;
+  p->k_page_b16 = (uint32_t)(cache->k_stride_page / 8), p->v_page_b16 = (uint32_t)(cache->v_stride_page / 8);
+  p->k_rb = (uint32_t)cache->k.stride_tok * 2, p->v_rb = (uint32_t)cache->v.stride_tok * 2;
+  p->page_table = cache->page_table + (int64_t)pl.seq0 * cache->stride_table;
+  p->stride_table = cache->stride_table;
+  p->n_pages = cache->n_pages, p->page_rows = cache->page_rows;
+  p->group = heads->n_q_heads / heads->n_kv_heads;
+  p->page_div = make_fast_div((uint32_t)cache->page_rows);
+  p->group_div = make_fast_div((uint32_t)p->group);
+  p->nq_div = make_fast_div((uint32_t)q_per_seq);
+  p->seq_len = seq_len + pl.seq0;
+  p->cap = max_len;
+  p->n_seqs = pl.n_seqs, p->nq = q_per_seq, p->n_kv_heads = heads->n_kv_heads;
+  p->scale_log2e = scale_log2e(heads);
+  p->chunk = pl.chunk, p->own_chunk = pl.own_chunk, p->prefix_items = pl.prefix_items;
+  p->own_splits = pl.own_splits, p->own_row_tiles = pl.own_row_tiles;
+  p->part_rows = (int64_t)pl.n_seqs * q_per_seq * heads->n_q_heads;
+  p->max_parts = pl.parts;
+  // Keys and values are read once a step (twice by two row tiles, at the same time), the next step's after all other layers'.  us with / without
+  // the hint, 32 over 8 heads of 128, sequences of their own: 65 MB 27.5 / 25.7 (found again in the cache in front of HBM when the
+  // calls of a program have no more than that), 262 MB 52.3 / 58.8, 1.05 GB 177 / 193, 1.98 GB 340 / 370; 48 drafts of 4 tokens, 175 MB 46.4 / 51.3.
+  p->past_caches = pl.keys * heads->n_kv_heads * heads->head_dim * 4 > kCacheBytes * 3 / 8;
+  p->direct = pl.parts <= 1 && pl.groups.n == 0;
+  p->part_o = (uint16_t *)ws;
+  p->part_ml = (float *)((char *)ws + align256((size_t)p->part_rows * pl.parts * heads->head_dim * 2));
+}
+template <typename Groups>
+hipError_t run_attention(const PagedAttnParams &p, const Groups &groups, int head_dim, hipStream_t stream) {
+  hipError_t e;
+  {
+    ProfileScope ps(BA_PROFILE_ATTENTION, stream);
+    e = launch_paged_attention(p, groups, head_dim, stream);
+  }
+  if (e != hipSuccess || p.direct) return e;
+  ProfileScope ps(BA_PROFILE_COMBINE, stream);
+  return launch_paged_merge(p, groups, head_dim, stream);
 }
 
 }  // namespace
@@ -484,15 +563,7 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
   const int32_t n_seqs = cache->n_seqs;
   if ((rc = check_paged_sizes(heads, n_seqs, q_per_seq, max_len))) return rc;
   if (n_seqs == 0) return check_groups(0, max_len, n_groups, cu_group, prefix_len);  // (tensors without rows need not lie anywhere)
-  if ((rc = check_tensor(q, "q", false, heads->head_dim, heads->n_q_heads)) || (rc = check_tensor(o_out, "o_out", false, heads->head_dim, heads->n_q_heads)))
-    return rc;
-  if (max_len > (int64_t)cache->max_pages * cache->page_rows) return fail(BA_ERR_INVALID_ARG, "max_len reaches beyond the page table");
-  // (a work item reads the query rows that it writes and no others, but the pages are everybody's)
-  const Extent out = extent(o_out, (int64_t)n_seqs * q_per_seq, heads->n_q_heads, heads->head_dim);
-  if (!same_place(q, o_out) && !apart(out, extent(q, (int64_t)n_seqs * q_per_seq, heads->n_q_heads, heads->head_dim)))
-    return fail(BA_ERR_INVALID_ARG, "o_out overlaps q without being exactly in place");
-  if (!apart(pool_extent(&cache->k, cache->k_stride_page, cache, heads), out) || !apart(pool_extent(&cache->v, cache->v_stride_page, cache, heads), out))
-    return fail(BA_ERR_INVALID_ARG, "o_out overlaps the cache");
+  if ((rc = check_rows(heads, cache, q, o_out, n_seqs, q_per_seq, max_len))) return rc;
   if ((rc = check_groups(n_seqs, max_len, n_groups, cu_group, prefix_len))) return rc;
   if (!seq_len) return fail(BA_ERR_INVALID_ARG, "seq_len: null");
   if ((rc = check_int_array(seq_len, "seq_len")) || (rc = check_int_array(lse_out, "lse_out"))) return rc;
@@ -507,50 +578,9 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
     plan_paged(heads, n_seqs, q_per_seq, max_len, n_groups, cu_group, prefix_len, g, num_cus(), &pl);
     g = pl.group_end;
     if (pl.n_seqs == 0) continue;
-    const int64_t tok0 = (int64_t)pl.seq0 * q_per_seq;
     PagedAttnParams p;
-    memset(&p, 0, sizeof(p));
-    p.q = (const uint16_t *)q->ptr + tok0 * q->stride_tok;
-    p.q_st = q->stride_tok, p.q_sh = q->stride_head;
-    p.o = (uint16_t *)o_out->ptr + tok0 * o_out->stride_tok;
-    p.o_st = o_out->stride_tok, p.o_sh = o_out->stride_head;
-    p.lse = lse_out ? lse_out + tok0 * heads->n_q_heads : nullptr;
-    p.k = (const uint16_t *)cache->k.ptr, p.v = (const uint16_t *)cache->v.ptr;
-    p.k_sh = cache->k.stride_head, p.v_sh = cache->v.stride_head;
-    p.k_page_b16 = (uint32_t)(cache->k_stride_page / 8), p.v_page_b16 = (uint32_t)(cache->v_stride_page / 8);
-    p.k_rb = (uint32_t)cache->k.stride_tok * 2, p.v_rb = (uint32_t)cache->v.stride_tok * 2;
-    p.page_table = cache->page_table + (int64_t)pl.seq0 * cache->stride_table;
-    p.stride_table = cache->stride_table;
-    p.n_pages = cache->n_pages, p.page_rows = cache->page_rows;
-    p.group = heads->n_q_heads / heads->n_kv_heads;
-    p.page_div = make_fast_div((uint32_t)cache->page_rows);
-    p.group_div = make_fast_div((uint32_t)p.group);
-    p.nq_div = make_fast_div((uint32_t)q_per_seq);
-    p.seq_len = seq_len + pl.seq0;
-    p.cap = max_len;
-    p.n_seqs = pl.n_seqs, p.nq = q_per_seq, p.n_kv_heads = heads->n_kv_heads;
-    p.scale_log2e = scale_log2e(heads);
-    p.chunk = pl.chunk, p.own_chunk = pl.own_chunk, p.prefix_items = pl.prefix_items;
-    p.own_splits = pl.own_splits, p.own_row_tiles = pl.own_row_tiles;
-    p.part_rows = (int64_t)pl.n_seqs * q_per_seq * heads->n_q_heads;
-    p.max_parts = pl.parts;
-    // Keys and values are read once a step (twice by two row tiles, at the same time), the next step's after all other layers'.  us with / without
-    // the hint, 32 over 8 heads of 128, sequences of their own: 65 MB 27.5 / 25.7 (found again in the cache in front of HBM when the
-    // calls of a program have no more than that), 262 MB 52.3 / 58.8, 1.05 GB 177 / 193, 1.98 GB 340 / 370; 48 drafts of 4 tokens, 175 MB 46.4 / 51.3.
-    p.past_caches = pl.keys * heads->n_kv_heads * heads->head_dim * 4 > kCacheBytes * 3 / 8;
-    p.direct = pl.parts <= 1 && pl.groups.n == 0;
-    p.part_o = (uint16_t *)ws;
-    p.part_ml = (float *)((char *)ws + align256((size_t)p.part_rows * pl.parts * heads->head_dim * 2));
-    auto run = [&](const auto &groups) {
-      hipError_t e;
-      {
-        ProfileScope ps(BA_PROFILE_ATTENTION, stream);
-        e = launch_paged_attention(p, groups, heads->head_dim, stream);
-      }
-      if (e != hipSuccess || p.direct) return e;
-      ProfileScope ps(BA_PROFILE_COMBINE, stream);
-      return launch_paged_merge(p, groups, heads->head_dim, stream);
-    };
+    set_attention(&p, heads, cache, q, o_out, lse_out, q_per_seq, seq_len, max_len, pl, ws);
+    auto run = [&](const auto &groups) { return run_attention(p, groups, heads->head_dim, stream); };
     hipError_t e;
     if (pl.groups.n <= PagedGroupsSmall::kGroups) {  // (a small table: many large argument blocks in flight hold up the queue)
       PagedGroupsSmall few;
@@ -568,6 +598,38 @@ int32_t ba_paged_attention(const ba_heads *heads, const ba_paged_cache *cache, c
     if (e != hipSuccess) return device_fail(e, "paged attention launch");
   } while (g < n_groups);
   return BA_OK;
+}
+
+size_t ba_paged_attention_selected_workspace_bytes(const ba_heads *heads, int32_t n_seqs, int32_t q_per_seq, int32_t page_rows, int32_t max_len,
+                                                   int32_t n_select) {
+  if (check_paged_sizes(heads, n_seqs, q_per_seq, max_len) != BA_OK || page_rows < 1 || n_select < 1 || n_seqs == 0) return 0;
+  PagedPlan pl;
+  size_t bytes;
+  return check_selected_plan(heads, n_seqs, q_per_seq, page_rows, max_len, n_select, &pl, &bytes) == BA_OK ? bytes : 0;
+}
+
+int32_t ba_paged_attention_selected(const ba_heads *heads, const ba_paged_cache *cache, const ba_tensor *q, const ba_tensor *o_out, float *lse_out,
+                                    int32_t q_per_seq, const int32_t *seq_len, int32_t max_len, const int32_t *selected, int32_t n_select, void *ws,
+                                    size_t ws_bytes, void *stream) {
+  int32_t rc;
+  if ((rc = check_heads(heads, true)) || (rc = check_cache(cache, heads))) return rc;
+  const int32_t n_seqs = cache->n_seqs;
+  if ((rc = check_paged_sizes(heads, n_seqs, q_per_seq, max_len))) return rc;
+  if (n_select < 1) return fail(BA_ERR_INVALID_ARG, "n_select must be positive");
+  if (n_seqs == 0) return BA_OK;  // (tensors without rows need not lie anywhere)
+  if ((rc = check_rows(heads, cache, q, o_out, n_seqs, q_per_seq, max_len))) return rc;
+  if (!seq_len || !selected) return fail(BA_ERR_INVALID_ARG, "seq_len / selected: null");
+  if ((rc = check_int_array(seq_len, "seq_len")) || (rc = check_int_array(selected, "selected")) || (rc = check_int_array(lse_out, "lse_out"))) return rc;
+  PagedPlan pl;
+  size_t need;
+  if ((rc = check_selected_plan(heads, n_seqs, q_per_seq, cache->page_rows, max_len, n_select, &pl, &need))) return rc;
+  if (need > 0 && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need))
+    return fail(BA_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than %zu bytes", need);
+  PagedAttnParams p;
+  set_attention(&p, heads, cache, q, o_out, lse_out, q_per_seq, seq_len, max_len, pl, ws);
+  const PagedSelection sel = {selected, n_select, cache->max_pages, selected_keys(cache->page_rows, max_len, n_select)};
+  const hipError_t e = run_attention(p, sel, heads->head_dim, (hipStream_t)stream);
+  return e == hipSuccess ? BA_OK : device_fail(e, "paged attention launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,95 @@
+// Internal interface between the C boundary (ba_api_long.hip) and the kernels that keep long caches affordable: weights of cached keys
+// (key_weights.hip), eviction by them (evict.hip), bounds of pages and selection by them (page_select.hip).
+#pragma once
+
+#include "ba_internal.h"
+#include "ba_paged.h"
+
+namespace ba {
+
+// Keys (or values) in pages, as a kernel sees them.
+struct PagedRowsParams {
+  const uint16_t *base;      // page 0, row 0, head 0
+  int64_t sh;                // head stride, elements
+  uint32_t page_b16;         // from page to page, in units of 16 bytes
+  uint32_t rb;               // bytes from row to row
+};
+struct PagedTableParams {
+  const int32_t *table;
+  int64_t stride;
+  int32_t n_pages, page_rows, max_pages;
+  FastDiv page_div;
+};
+
+// ---------------------------------------------------------------- weights of cached keys ----------
+struct KeyWeightsParams {
+  const uint16_t *q;
+  int64_t q_st, q_sh;
+  const float *lse;        // [tokens][query heads]
+  PagedRowsParams k;
+  PagedTableParams pages;
+  const int32_t *seq_len;
+  int32_t cap;             // no sequence is taken to be longer
+  int32_t n_seqs, nq, group, n_kv_heads;
+  int32_t rows, padded;    // query rows of a sequence and KV head; padded to 4, or to a multiple of 8
+  FastDiv group_div, padded_div;
+  float scale_log2e, decay;
+  const float *w_in;       // null: nothing was given before
+  float *w_out;
+  int64_t w_stride;
+  int32_t prefix_items, own_chunks;
+};
+constexpr int key_weights_keys(int tiles) { return 128 * tiles; }  // keys of a work item: `tiles` of 32 a wave
+// tiles: 1 or 2
+template <typename Groups>
+hipError_t launch_key_weights(const KeyWeightsParams &p, const Groups &g, int head_dim, int tiles, hipStream_t stream);
+
+// ---------------------------------------------------------------- eviction ----------
+struct EvictParams {
+  const float *weights;
+  int64_t w_stride;
+  const int32_t *seq_len;
+  int32_t cap, n_seqs, n_kv_heads, head_dim;
+  int32_t n_keep, n_first, n_last;
+  int32_t *kept;           // [sequences][KV heads][n_keep]
+  float *w_out;            // nullable
+  int64_t w_out_stride;
+  int32_t *len_out;        // nullable
+  PagedRowsParams k, v, to_k, to_v;
+  PagedTableParams from, to;
+};
+constexpr int64_t kMaxPickWorkgroups = 0xffffffffll / 1024;
+constexpr int kEvictCopyRows = 64;  // kept rows that a workgroup copies
+hipError_t launch_evict_pick(const EvictParams &p, hipStream_t stream);
+hipError_t launch_evict_copy(const EvictParams &p, hipStream_t stream);
+
+// ---------------------------------------------------------------- bounds of pages, selection ----------
+constexpr int kBoundMinExp = -60, kBoundMaxExp = 40;
+struct PageBoundsParams {
+  PagedRowsParams k;
+  PagedTableParams pages;
+  int8_t *codes, *exps;
+  const int32_t *from, *seq_len;
+  int32_t cap, n_seqs, n_kv_heads;
+};
+hipError_t launch_page_bounds(const PageBoundsParams &p, int head_dim, hipStream_t stream);
+
+constexpr int kScorePages = 128;  // pages that a workgroup scores
+struct PageSelectParams {
+  const uint16_t *q;
+  int64_t q_st, q_sh;
+  PagedTableParams pages;
+  const int8_t *codes, *exps;
+  const int32_t *seq_len;
+  int32_t cap, n_seqs, n_kv_heads, nq, group;
+  FastDiv group_div;
+  int32_t n_select, n_first, n_last;
+  int32_t *selected;
+  float *scores_out;       // nullable
+  float *scores;           // [sequences][KV heads][score_stride]
+  int64_t score_stride;
+};
+hipError_t launch_page_scores(const PageSelectParams &p, int head_dim, hipStream_t stream);
+hipError_t launch_page_pick(const PageSelectParams &p, hipStream_t stream);
+
+}  // namespace ba

@@ -103,6 +103,14 @@ struct PagedGroupsT {
 using PagedGroups = PagedGroupsT<96>;
 using PagedGroupsSmall = PagedGroupsT<8>;
 
+// In place of the groups: the pages that every sequence and KV head reads.
+struct PagedSelection {
+  const int32_t *pages;  // [sequences][KV heads][n], numbers within the sequence
+  int32_t n, max_pages;
+  int32_t keys;          // of the listed pages at most: min(n * page_rows, cap)
+};
+constexpr int kSelectedMaxChunk = 1152;  // keys of a work item at most: its part of the list lies in LDS as well
+
 template <typename Groups>
 hipError_t launch_paged_attention(const PagedAttnParams &p, const Groups &g, int head_dim, hipStream_t stream);
 template <typename Groups>

@@ -42,7 +42,14 @@ struct {
   decltype(&ba_paged_append) paged_append;
   decltype(&ba_paged_attention) paged_attention;
 } paged;
-PyTypeObject *heads_type, *norm_type, *cache_type;
+struct {
+  decltype(&ba_paged_key_weights) key_weights;
+  decltype(&ba_paged_evict) evict;
+  decltype(&ba_page_bounds) page_bounds;
+  decltype(&ba_page_select) page_select;
+  decltype(&ba_paged_attention_selected) attention_selected;
+} longer;
+PyTypeObject *heads_type, *norm_type, *cache_type, *bounds_type;
 PyObject *name_c, *name_known, *name_cuda_stream, *get_device, *get_raw_stream;
 
 // Arguments that are not the plain case.
@@ -90,6 +97,16 @@ struct NormArg : Held<KnownNorm> {
 };
 struct CacheArg : Held<KnownCache> {
   CacheArg(PyObject *o, const ba_heads *heads) : Held(o, cache_type, name_known) { need(h->n_kv_heads == heads->n_kv_heads && h->head_dim == heads->head_dim); }
+};
+
+struct KnownBounds {
+  ba_page_bound_table bounds;
+  int32_t n_pages, n_kv_heads, head_dim;
+};
+struct BoundsArg : Held<KnownBounds> {
+  BoundsArg(PyObject *o, const ba_heads *heads, const ba_paged_cache &cache) : Held(o, bounds_type, name_known) {
+    need(h->n_kv_heads == heads->n_kv_heads && h->head_dim == heads->head_dim && h->n_pages >= cache.n_pages);
+  }
 };
 
 bool is_int32_array(PyObject *o) {
@@ -178,6 +195,31 @@ T *device_array(PyObject *o, at::ScalarType type, int64_t n) {
   need(x.scalar_type() == type && x.dim() == 1 && x.is_contiguous() && x.size(0) >= n);
   return (T *)x.data_ptr();
 }
+// float32 [sequences, KV heads, at least `least`], sequences n_kv_heads heads apart
+struct PerKey {
+  float *p = nullptr;
+  int64_t stride = 0;
+  PerKey(PyObject *o, int64_t heads, int64_t seqs, int64_t least) {
+    if (o == Py_None) return;
+    const at::Tensor &x = plain_tensor(o);
+    need(x.scalar_type() == at::kFloat && x.dim() == 3);
+    const auto size = x.sizes(), st = x.strides();
+    need((size[2] <= 1 || st[2] == 1) && size[1] == heads && size[0] >= seqs && size[2] >= least);
+    stride = heads > 1 ? st[1] : size[0] > 1 ? st[0] : std::max<int64_t>(size[2], 1);
+    need(size[0] <= 1 || st[0] == heads * stride);
+    p = (float *)x.data_ptr();
+  }
+};
+// [sequences, KV heads, n]; width: n, or -1 for any
+template <typename T>
+T *device_lists(PyObject *o, at::ScalarType type, int64_t seqs, int64_t heads, int64_t width, int32_t *n = nullptr) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor &x = plain_tensor(o);
+  need(x.scalar_type() == type && x.dim() == 3 && x.is_contiguous() && x.size(0) >= seqs && x.size(1) == heads && (width < 0 || x.size(2) == width) &&
+       x.size(2) <= INT32_MAX);
+  if (n) *n = (int32_t)x.size(2);
+  return (T *)x.data_ptr();
+}
 float *gain_grad(PyObject *o, int64_t d) {
   need(o == Py_None || plain_tensor(o).numel() == d);
   return device_array<float>(o, at::kFloat, d);
@@ -209,6 +251,10 @@ int32_t int_of(PyObject *o) {
   const long v = PyLong_AsLongAndOverflow(o, &overflow);
   need(!overflow && v == (int32_t)v);
   return (int32_t)v;
+}
+float float_of(PyObject *o) {
+  need(PyFloat_CheckExact(o));
+  return (float)PyFloat_AS_DOUBLE(o);
 }
 void *stream_of(PyObject *o) {
   PyObject *h = nullptr;
@@ -454,6 +500,100 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+PyObject *key_weights(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 14, 5, 7, [&] {
+    const HeadsArg h(a[0]);
+    const CacheArg cache(a[8], h.h);
+    const Ints cu(a[6]), prefix(a[7]);
+    need(!cu.p == !prefix.p && (!cu.p || cu.n == prefix.n + 1));
+    const float decay = float_of(a[9]);
+    const int32_t max_len = int_of(a[10]), nq = int_of(a[11]);
+    const int64_t seqs = cache.h->cache.n_seqs, T = seqs * std::max(nq, 0), hq = h.h->n_q_heads, hkv = h.h->n_kv_heads;
+    const TensorArg q(a[1], hq, h.h->head_dim, T);
+    const float *const lse = lse_of(a[2], T, hq);
+    const PerKey in(a[3], hkv, seqs, max_len), out(a[4], hkv, seqs, max_len);
+    need(!in.p || !out.p || in.stride == out.stride);
+    const int32_t *const len = device_array<int32_t>(a[5], at::kInt, seqs);
+    const Workspace ws(a[12]);
+    void *const stream = stream_of(a[13]);
+    return unlocked([&] {
+      return longer.key_weights(h.h, &cache.h->cache, q.p, lse, in.p, out.p, out.stride, decay, nq, len, max_len, (int32_t)prefix.n, cu.p, prefix.p, ws.p,
+                                ws.bytes, stream);
+    });
+  });
+}
+
+PyObject *evict(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 14, 5, 5, [&] {
+    const HeadsArg h(a[0]);
+    const CacheArg cache(a[6], h.h), to(a[7], h.h);
+    const int32_t max_len = int_of(a[8]), n_keep = int_of(a[9]), n_first = int_of(a[10]), n_last = int_of(a[11]);
+    const int64_t seqs = cache.h->cache.n_seqs, hkv = h.h->n_kv_heads;
+    const PerKey w(a[1], hkv, seqs, max_len), out(a[4], hkv, seqs, n_keep);
+    const int32_t *const len = device_array<int32_t>(a[2], at::kInt, seqs);
+    int32_t *const kept = device_lists<int32_t>(a[3], at::kInt, seqs, hkv, n_keep), *const new_len = device_array<int32_t>(a[5], at::kInt, seqs);
+    const Workspace ws(a[12]);
+    void *const stream = stream_of(a[13]);
+    return unlocked([&] {
+      return longer.evict(h.h, &cache.h->cache, &to.h->cache, w.p, w.stride, len, max_len, n_keep, n_first, n_last, kept, out.p, out.stride, new_len, ws.p,
+                          ws.bytes, stream);
+    });
+  });
+}
+
+PyObject *page_bounds(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 7, 2, 2, [&] {
+    const HeadsArg h(a[0]);
+    const CacheArg cache(a[3], h.h);
+    const BoundsArg bounds(a[4], h.h, cache.h->cache);
+    const int64_t seqs = cache.h->cache.n_seqs;
+    const int32_t *const from = device_array<int32_t>(a[1], at::kInt, seqs), *const len = device_array<int32_t>(a[2], at::kInt, seqs);
+    const int32_t max_len = int_of(a[5]);
+    void *const stream = stream_of(a[6]);
+    return unlocked([&] { return longer.page_bounds(h.h, &cache.h->cache, &bounds.h->bounds, from, len, max_len, stream); });
+  });
+}
+
+PyObject *page_select(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 13, 4, 4, [&] {
+    const HeadsArg h(a[0]);
+    const CacheArg cache(a[5], h.h);
+    const BoundsArg bounds(a[6], h.h, cache.h->cache);
+    const int32_t max_len = int_of(a[7]), n_first = int_of(a[8]), n_last = int_of(a[9]), nq = int_of(a[10]);
+    const int64_t seqs = cache.h->cache.n_seqs, hkv = h.h->n_kv_heads;
+    const TensorArg q(a[1], h.h->n_q_heads, h.h->head_dim, seqs * std::max(nq, 0));
+    const int32_t *const len = device_array<int32_t>(a[2], at::kInt, seqs);
+    int32_t n_select = 0;
+    int32_t *const selected = device_lists<int32_t>(a[3], at::kInt, seqs, hkv, -1, &n_select);
+    float *const scores = device_lists<float>(a[4], at::kFloat, seqs, hkv, n_select);
+    const Workspace ws(a[11]);
+    void *const stream = stream_of(a[12]);
+    return unlocked([&] {
+      return longer.page_select(h.h, &cache.h->cache, &bounds.h->bounds, q.p, nq, len, max_len, n_select, n_first, n_last, selected, scores, ws.p, ws.bytes,
+                                stream);
+    });
+  });
+}
+
+PyObject *paged_attention_selected(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return guarded(a, n, 11, 5, 5, [&] {
+    const HeadsArg h(a[0]);
+    const CacheArg cache(a[6], h.h);
+    const int32_t max_len = int_of(a[7]), nq = int_of(a[8]);
+    const int64_t seqs = cache.h->cache.n_seqs, T = seqs * std::max(nq, 0), hq = h.h->n_q_heads, d = h.h->head_dim;
+    const TensorArg q(a[1], hq, d, T), o(a[2], hq, d, T);
+    float *const lse = lse_of(a[3], T, hq);
+    const int32_t *const len = device_array<int32_t>(a[4], at::kInt, seqs);
+    int32_t n_select = 0;
+    const int32_t *const selected = device_lists<int32_t>(a[5], at::kInt, seqs, h.h->n_kv_heads, -1, &n_select);
+    const Workspace ws(a[9]);
+    void *const stream = stream_of(a[10]);
+    return unlocked([&] {
+      return longer.attention_selected(h.h, &cache.h->cache, q.p, o.p, lse, nq, len, max_len, selected, n_select, ws.p, ws.bytes, stream);
+    });
+  });
+}
+
 // setup(Heads class, current_device(), raw_stream(device) or None, addresses of the entry points in the order of `lib`)
 PyObject *setup(PyObject *, PyObject *args) {
   PyObject *type, *dev, *raw;
@@ -485,6 +625,20 @@ PyObject *setup_paged(PyObject *, PyObject *args) {
   Py_RETURN_NONE;
 }
 
+// setup_long(PageBounds class, addresses of the entry points in the order of `longer`)
+PyObject *setup_long(PyObject *, PyObject *args) {
+  PyObject *bounds;
+  unsigned long long at[5];
+  if (!PyArg_ParseTuple(args, "O!(KKKKK)", &PyType_Type, &bounds, at, at + 1, at + 2, at + 3, at + 4)) return nullptr;
+  Py_INCREF(bounds);
+  bounds_type = (PyTypeObject *)bounds;
+  static_assert(sizeof(longer) == 5 * sizeof(void *), "an address each");
+  void *p[5];
+  for (int i = 0; i < 5; ++i) p[i] = (void *)(uintptr_t)at[i];
+  memcpy(&longer, p, sizeof(longer));
+  Py_RETURN_NONE;
+}
+
 #define FAST(name, fn) {name, (PyCFunction)(void (*)(void))(fn), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, nullptr},
                          {"setup_paged", setup_paged, METH_VARARGS, nullptr},
@@ -499,6 +653,12 @@ PyMethodDef methods[] = {{"setup", setup, METH_VARARGS, nullptr},
                          FAST("norm_rotate_backward", norm_rotate_backward),
                          FAST("paged_append", paged_append),
                          FAST("paged_attention", paged_attention),
+                         {"setup_long", setup_long, METH_VARARGS, nullptr},
+                         FAST("key_weights", key_weights),
+                         FAST("evict", evict),
+                         FAST("page_bounds", page_bounds),
+                         FAST("page_select", page_select),
+                         FAST("paged_attention_selected", paged_attention_selected),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_face", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -108,6 +108,31 @@ __device__ __forceinline__ PagedRow paged_row(const PagedAttnParams &p, const Pa
   w.limit = min(it.k1, length_of(p, it.seq0 + seq) - p.nq + (tok - seq * p.nq) + 1);
   return w;
 }
+// Pages that a list names, ascending: what the walk takes for a sequence is the listed pages one after the other.
+struct SelectedItem : PagedItem {
+  lds_char *list;  // numbers of the item's pages within the sequence
+  int n_list;
+};
+// (the tokens that a row sees are the first ones of that sequence, too: those of the pages before the one its last token is in, and
+// what it sees of that one)
+__device__ __forceinline__ PagedRow paged_row(const PagedAttnParams &p, const SelectedItem &it, int r) {
+  PagedRow w = paged_row(p, static_cast<const PagedItem &>(it), r);
+  const int tok = (int)fast_div((uint32_t)r, p.group_div), seq = (int)fast_div((uint32_t)tok, p.nq_div);
+  const int limit = max(0, length_of(p, it.seq0 + seq) - p.nq + (tok - seq * p.nq) + 1);
+  const int page = (int)fast_div((uint32_t)limit, p.page_div);
+  const lds_int *const list = (const lds_int *)it.list;
+  w.limit = 0;
+  if (it.n_list <= 0) return w;
+  int lo = 0, hi = it.n_list;  // the first that is not before it
+  if (list[hi - 1] < page) lo = hi;
+  while (hi > lo) {
+    const int mid = (lo + hi) >> 1;
+    if (list[mid] < page) lo = mid + 1; else hi = mid;
+  }
+  const int64_t keys = (int64_t)(it.page0 + lo) * p.page_rows + (lo < it.n_list && list[lo] == page ? limit - page * p.page_rows : 0);
+  w.limit = lo == it.n_list ? it.k1 : (int)(keys < it.k1 ? keys : it.k1);
+  return w;
+}
 __device__ __forceinline__ int wave_min(int x) {
 #pragma unroll
   for (int m = 1; m < 64; m *= 2) x = min(x, __shfl_xor(x, m));
@@ -249,8 +274,8 @@ __device__ __forceinline__ float max_over_sixteen(float x) {
 // tie the waves' loads together; they meet only at the end.  32 over 8 heads of 128: 128 sequences of up to 8,000 keys, 1.98 GB, 324 us,
 // 6.1 TB/s; 1 of 2,064 keys 6.5 us, of them launch 2.4, the page table 0.8, keys and products 1.8, the end 1.6.
 // stage(): puts the item's part of the page table into LDS (the rows are asked for first, and arrive meanwhile)
-template <int D, bool kAligned, int RG, typename Stage>
-__device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem &it, lds_char *smem, int lane, int wave, Stage &&stage) {
+template <int D, bool kAligned, int RG, typename Item, typename Stage>
+__device__ __forceinline__ void walk_stream(const PagedAttnParams &p, Item &it, lds_char *smem, int lane, int wave, Stage &&stage) {
   using G = PGeo<D>;
   constexpr int KK = D / 32, DS = D / 16;
   constexpr uint32_t TB = 16 * G::ROWB;              // a tile of keys, then one of values
@@ -469,8 +494,8 @@ __device__ __forceinline__ void walk_stream(const PagedAttnParams &p, PagedItem 
 // in part.  Three workgroups a compute unit need 168 registers and 48 KB: 512 rows 87 us against 91, but 256 rows 58.5 against 51.9; eight
 // waves that take turns at the matrix units, with 64 keys a tile, and with the sequences' own items among theirs: 58.4 against 58.2.
 // The next tile's score products between this one's exponentials: no change.
-template <int D, bool kAligned, typename Stage>
-__device__ __forceinline__ void walk_shared(const PagedAttnParams &p, PagedItem &it, lds_char *smem, int lane, int wave, Stage &&stage) {
+template <int D, bool kAligned, typename Item, typename Stage>
+__device__ __forceinline__ void walk_shared(const PagedAttnParams &p, Item &it, lds_char *smem, int lane, int wave, Stage &&stage) {
   using G = PGeo<D>;
   constexpr int KCH = D / 16, DT = D / 32, GPR = G::ROWB / 64;
   constexpr uint32_t TB = 32 * G::ROWB;
@@ -757,6 +782,73 @@ __global__ __launch_bounds__(kPThreads, 2) void paged_attn_kernel(PagedAttnParam
   else walk_stream<D, kAligned, 1>(p, it, smem, lane, wave, stage);
 }
 
+// The same over listed pages: an item is a range of the keys of the listed pages one after the other.  Entries from the first one on that is
+// negative or not above the one in front of it are nobody's.
+template <int D, bool kAligned>
+__global__ __launch_bounds__(kPThreads, 2) void paged_selected_kernel(PagedAttnParams p, PagedSelection sel) {
+  extern __shared__ __attribute__((aligned(1024))) char smem_generic[];
+  lds_char *smem = (lds_char *)smem_generic;
+  SelectedItem it;
+  int rel = (int)blockIdx.x;
+  it.kvh = rel % p.n_kv_heads;
+  rel /= p.n_kv_heads;
+  it.n_rows = p.nq * p.group;
+  it.row0 = rel % p.own_row_tiles * paged_tile_rows(it.n_rows);
+  rel /= p.own_row_tiles;
+  it.seq0 = rel % p.n_seqs;
+  it.part = rel / p.n_seqs;
+  it.k_lo = it.k0 = it.part * p.own_chunk;
+  it.page0 = (int)fast_div((uint32_t)it.k0, p.page_div);
+  it.k1 = min(min(sel.keys, it.k0 + p.own_chunk), length_of(p, it.seq0));
+  if (it.k0 >= it.k1) {
+    if (!p.direct) return;  // (the merge knows)
+    it.k_lo = it.k0 = it.k1 = it.page0 = 0;
+  }
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = it.k1 > it.k0 ? (int)fast_div((uint32_t)(it.k1 - 1), p.page_div) - it.page0 + 1 : 0;
+  const int32_t *const list = sel.pages + ((int64_t)it.seq0 * p.n_kv_heads + it.kvh) * sel.n, *const table = p.page_table + it.seq0 * p.stride_table;
+  lds_int *const ids = (lds_int *)(smem + kTilesB), *const entries = ids + n, *const ends = entries + n;
+  it.list = (lds_char *)entries;
+  int valid = it.page0 + n, bad = 0;
+#pragma unroll 1
+  for (int i = threadIdx.x; i < it.page0 + n; i += kPThreads) {
+    const int e = list[i], before = i ? list[i - 1] : -1;
+    if (e <= before) valid = min(valid, i);
+    if (i < it.page0) continue;
+    const int id = e >= 0 && e < sel.max_pages ? table[e] : -1;
+    const bool ok = id >= 0 && id < p.n_pages;
+    ids[i - it.page0] = ok ? id : -1;
+    entries[i - it.page0] = e;
+    bad |= !ok;
+  }
+  valid = wave_min(valid);
+  if (lane == 0) ends[wave] = valid;
+  it.holes = __syncthreads_or(bad) != 0;
+  valid = min(min(ends[0], ends[1]), min(ends[2], ends[3]));
+  it.n_list = max(0, valid - it.page0);
+  const int64_t valid_keys = (int64_t)valid * p.page_rows;
+  if (valid_keys < it.k1) it.k1 = (int)valid_keys;
+  if (it.k1 <= it.k0) it.k_lo = it.k0 = it.k1 = 0;
+  auto stage = [] {};
+  const int rows = it.n_rows - it.row0;
+  if (it.n_rows > kPagedStreamRows) walk_shared<D, kAligned>(p, it, smem, lane, wave, stage);
+  else if (rows > 16) walk_stream<D, kAligned, 2>(p, it, smem, lane, wave, stage);
+  else walk_stream<D, kAligned, 1>(p, it, smem, lane, wave, stage);
+}
+// parts of a sequence's rows
+__device__ __forceinline__ int parts_of(const PagedAttnParams &p, const PagedSelection &sel, int seq) {
+  return (min(sel.keys, length_of(p, seq)) + p.own_chunk - 1) / p.own_chunk;
+}
+template <typename Groups>
+__device__ __forceinline__ int parts_of(const PagedAttnParams &p, const Groups &groups, int seq) {
+  const int g = group_of(groups, seq);
+  const int prefix = g < 0 ? 0 : groups.prefix[g];
+  // (a sequence that ends in its prefix has no part of its own)
+  const int len = length_of(p, seq), own = len > prefix ? (len - prefix / 16 * 16 + p.own_chunk - 1) / p.own_chunk : 0;
+  return (g < 0 ? 0 : groups.splits[g]) + own;
+}
+
 // o = sum_i w_i o_i / sum_i w_i over a row's parts, w_i = 2^(m_i - m) l_i, m = max m_i: sixteen lanes a row, kWays times over (every
 // kWays-th part each).  References and sums arrive together, a lane per part, ahead of the outputs.
 // Bound by launch and by the way to memory and back twice: 32 rows of 33 parts 4.3 us; 2,048 rows of 33 parts, 16 MB, 6.4.
@@ -768,11 +860,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnPar
   const int64_t my_row = (int64_t)blockIdx.x * kRows + slot, row = min(my_row, p.part_rows - 1);
   const int tok = (int)(row / hq), head = (int)(row - (int64_t)tok * hq);
   const int seq = (int)fast_div((uint32_t)tok, p.nq_div);
-  const int g = group_of(groups, seq);
-  const int prefix = g < 0 ? 0 : groups.prefix[g];
-  // (a sequence that ends in its prefix has no part of its own)
-  const int len = length_of(p, seq), own = len > prefix ? (len - prefix / 16 * 16 + p.own_chunk - 1) / p.own_chunk : 0;
-  const int parts = (g < 0 ? 0 : groups.splits[g]) + own;
+  const int parts = parts_of(p, groups, seq);
   const int n = parts > way ? (parts - way + kWays - 1) / kWays : 0;  // this way's: way, way + kWays, ...
   auto end_of = [&](int i) __attribute__((always_inline)) {
     return i < n ? *reinterpret_cast<const f32x4_t *>(p.part_ml + ((way + (int64_t)i * kWays) * p.part_rows + row) * 4) : f32x4_t{-INFINITY, 0.f, 0.f, 0.f};
@@ -858,6 +946,19 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnPar
   }
 }
 
+// LDS behind the tiles: entries of the page table for `pages` pages
+template <int D, bool kAligned, typename Groups>
+struct AttnKernel {
+  static constexpr int kMaxChunk = kPagedMaxChunk;
+  static constexpr size_t table_bytes(int pages) { return (size_t)pages * 4; }
+  static constexpr auto *kernel = &paged_attn_kernel<D, kAligned, Groups>;
+};
+template <int D, bool kAligned>
+struct AttnKernel<D, kAligned, PagedSelection> {
+  static constexpr int kMaxChunk = kSelectedMaxChunk;
+  static constexpr size_t table_bytes(int pages) { return (size_t)pages * 8 + kPWaves * 4; }
+  static constexpr auto *kernel = &paged_selected_kernel<D, kAligned>;
+};
 template <int D, bool kAligned, typename Groups>
 hipError_t launch_attn_a(const PagedAttnParams &p, const Groups &g, unsigned items, size_t lds, hipStream_t stream) {
   // (a launch of more than 64 KB of LDS has to be allowed first, on every device)
@@ -866,21 +967,22 @@ hipError_t launch_attn_a(const PagedAttnParams &p, const Groups &g, unsigned ite
   hipError_t e = hipGetDevice(&dev);
   if (e != hipSuccess) return e;
   if (dev >= 16 || !told[dev].load(std::memory_order_acquire)) {
-    e = hipFuncSetAttribute(reinterpret_cast<const void *>(&paged_attn_kernel<D, kAligned, Groups>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            kTilesB + (kPagedMaxChunk + 2) * 4);
+    e = hipFuncSetAttribute(reinterpret_cast<const void *>(AttnKernel<D, kAligned, Groups>::kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
+                            kTilesB + (int)AttnKernel<D, kAligned, Groups>::table_bytes(AttnKernel<D, kAligned, Groups>::kMaxChunk + 2));
     if (e != hipSuccess) return e;
     if (dev < 16) told[dev].store(true, std::memory_order_release);
   }
-  paged_attn_kernel<D, kAligned, Groups><<<items, kPThreads, lds, stream>>>(p, g);
+  AttnKernel<D, kAligned, Groups>::kernel<<<items, kPThreads, lds, stream>>>(p, g);
   return hipGetLastError();
 }
 template <int D, typename Groups>
 hipError_t launch_attn_d(const PagedAttnParams &p, const Groups &g, hipStream_t stream) {
   const int64_t items = p.prefix_items + (int64_t)p.n_seqs * p.n_kv_heads * p.own_row_tiles * p.own_splits;
   const int32_t chunk = std::max(p.chunk, p.own_chunk);
-  if (items < 1 || items > kMaxWorkgroups || chunk > kPagedMaxChunk) return hipErrorInvalidValue;
-  const size_t lds = kTilesB + (size_t)(chunk / p.page_rows + 2) * 4;  // (a range may begin and end inside a page)
-  static_assert(2 * (kTilesB + (kPagedMaxChunk + 2) * 4) <= 160 * 1024, "two workgroups a compute unit");
+  using Kernel = AttnKernel<D, true, Groups>;
+  if (items < 1 || items > kMaxWorkgroups || chunk > Kernel::kMaxChunk) return hipErrorInvalidValue;
+  const size_t lds = kTilesB + Kernel::table_bytes(chunk / p.page_rows + 2);  // (a range may begin and end inside a page)
+  static_assert(2 * (kTilesB + Kernel::table_bytes(Kernel::kMaxChunk + 2)) <= 160 * 1024, "two workgroups a compute unit");
   return p.page_rows % 16 == 0 ? launch_attn_a<D, true>(p, g, (unsigned)items, lds, stream) : launch_attn_a<D, false>(p, g, (unsigned)items, lds, stream);
 }
 template <int D, int kWays, typename Groups>
@@ -916,5 +1018,7 @@ template hipError_t launch_paged_attention(const PagedAttnParams &, const PagedG
 template hipError_t launch_paged_attention(const PagedAttnParams &, const PagedGroupsSmall &, int, hipStream_t);
 template hipError_t launch_paged_merge(const PagedAttnParams &, const PagedGroups &, int, hipStream_t);
 template hipError_t launch_paged_merge(const PagedAttnParams &, const PagedGroupsSmall &, int, hipStream_t);
+template hipError_t launch_paged_attention(const PagedAttnParams &, const PagedSelection &, int, hipStream_t);
+template hipError_t launch_paged_merge(const PagedAttnParams &, const PagedSelection &, int, hipStream_t);
 
 }  // namespace ba
