@@ -58,7 +58,8 @@ void set_table(PagedTableParams *p, const ba_paged_cache *c) {
 // ---- weights of cached keys --------------------------------------------------------------------------------
 struct WeightsPlan {
   int32_t seq0, n_seqs, group_end;
-  int32_t tiles, prefix_items, own_chunks;
+  int32_t prefix_items, own_chunks;
+  bool many;
   int64_t items;
   PagedGroups groups;
 };
@@ -70,7 +71,7 @@ int32_t padded_rows(const ba_heads *h, int32_t nq) {
 void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, int32_t n_groups, const int32_t *cu_group, const int32_t *prefix_len,
                   int g0, WeightsPlan *pl) {
   memset(pl, 0, sizeof(*pl));
-  int32_t least_prefix = 0, most_members = 1;
+  int32_t least_prefix = 0;
   if (n_groups == 0) {
     pl->n_seqs = n_seqs;
   } else {
@@ -86,16 +87,16 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
         pl->groups.seq0[i] = cu_group[g] - pl->seq0;
         pl->groups.members[i] = members;
         pl->groups.prefix[i] = prefix_len[g];
-        most_members = std::max(most_members, members);
       }
       if (members > 0) least_prefix = std::min(least_prefix, shares ? prefix_len[g] : 0);
     }
     pl->group_end = g;
     pl->n_seqs = cu_group[g] - pl->seq0;
   }
-  const int64_t rows = (int64_t)padded_rows(h, nq) * most_members;
-  pl->tiles = rows >= 64 ? 2 : 1;
-  const int32_t keys = key_weights_keys(pl->tiles);
+  // us, the kernel for few rows and the one for many, 8 KV heads of 128: 1 sequence of 32,000 keys, 16 rows 14.6 / 16.8, 32 15.3 / 13.6, 48 19.2 / 19.4,
+  // 64 19.9 / 15.3, 128 28.2 / 20.2, 1,024 139 / 84; of 2,000, 32 rows 5.0 / 5.5, 64 5.9 / 6.8, 256 15.1 / 11.9, 1,024 52 / 36.
+  pl->many = nq * (h->n_q_heads / h->n_kv_heads) >= 32;
+  const int32_t keys = pl->many ? kWeightsManyKeys : kWeightsFewKeys;
   int64_t items = 0;
   for (int i = 0; i < pl->groups.n; ++i) {
     pl->groups.item0[i] = (int32_t)std::min<int64_t>(items, INT32_MAX);
@@ -185,9 +186,9 @@ int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache,
       for (int i = 0; i < few.n; ++i)
         few.seq0[i] = pl.groups.seq0[i], few.members[i] = pl.groups.members[i], few.prefix[i] = pl.groups.prefix[i], few.item0[i] = pl.groups.item0[i];
       few.item0[few.n] = pl.groups.item0[few.n];
-      e = launch_key_weights(p, few, D, pl.tiles, (hipStream_t)stream);
+      e = launch_key_weights(p, few, D, pl.many, (hipStream_t)stream);
     } else {
-      e = launch_key_weights(p, pl.groups, D, pl.tiles, (hipStream_t)stream);
+      e = launch_key_weights(p, pl.groups, D, pl.many, (hipStream_t)stream);
     }
     if (e != hipSuccess) return device_fail(e, "key weights launch");
   } while (g < n_groups);

@@ -39,10 +39,9 @@ struct KeyWeightsParams {
   int64_t w_stride;
   int32_t prefix_items, own_chunks;
 };
-constexpr int key_weights_keys(int tiles) { return 128 * tiles; }  // keys of a work item: `tiles` of 32 a wave
-// tiles: 1 or 2
+constexpr int kWeightsFewKeys = 128, kWeightsManyKeys = 256;  // keys of a work item of the kernels for few and for many rows a sequence
 template <typename Groups>
-hipError_t launch_key_weights(const KeyWeightsParams &p, const Groups &g, int head_dim, int tiles, hipStream_t stream);
+hipError_t launch_key_weights(const KeyWeightsParams &p, const Groups &g, int head_dim, bool many, hipStream_t stream);
 
 // ---------------------------------------------------------------- eviction ----------
 struct EvictParams {

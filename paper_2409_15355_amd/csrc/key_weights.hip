@@ -6,7 +6,6 @@
 // or of what a sequence has behind it.  S = Q K^T by v_mfma_f32_32x32x16_bf16 with the keys as columns: a lane owns a key, its
 // registers run over the rows, so the sum over rows is a lane's own and is stored as 128 consecutive bytes a half-wave.  A wave's
 // keys come straight from the pages into its registers, once; the query rows go round through LDS in tiles of 32, for all waves.
-// A sequence's rows begin at a multiple of 4 (of 8 if it has more than 4): a quad of accumulators is one sequence's.
 #include "ba_device.h"
 #include "ba_lds.h"
 #include "ba_long.h"
@@ -25,16 +24,14 @@ typedef const __attribute__((address_space(3))) bf16x8_t lds_bf16x8;
 
 __device__ __forceinline__ int clamped_length(const int32_t *seq_len, int cap, int seq) { return max(0, min(seq_len[seq], cap)); }
 
-template <int D, int NT, typename Groups>
-__global__ __launch_bounds__(kWThreads) void key_weights_kernel(KeyWeightsParams p, Groups groups) {
-  constexpr int CPR = D / 8, KCH = D / 16, ROWB = D * 2, LPR = 256 / ROWB;
-  constexpr uint32_t TB = 32 * ROWB;                       // a tile of query rows
-  constexpr int RPP = kWThreads / CPR, PIECES = 32 / RPP;  // rows a pass of the threads stages, passes
-  constexpr int kMeta = 3 * 32 * 4 + 16;
-  __shared__ __attribute__((aligned(16))) char smem_generic[2 * (TB + kMeta)];
-  lds_char *const smem = (lds_char *)smem_generic;
-
-  int seq0, n_mem, kvh, key0, key_end;
+struct WeightsItem {
+  int seq0, n_mem;    // the sequences whose rows it takes
+  int kvh;
+  int key0, key_end;  // keys from key0 on, below key_end
+};
+template <int KEYS, typename Groups>
+__device__ __forceinline__ WeightsItem weights_item(const KeyWeightsParams &p, const Groups &groups) {
+  WeightsItem it;
   if ((int)blockIdx.x < p.prefix_items) {
     const int id = (int)blockIdx.x;
     int lo = 0, hi = groups.n;
@@ -43,183 +40,381 @@ __global__ __launch_bounds__(kWThreads) void key_weights_kernel(KeyWeightsParams
       if (groups.item0[mid] <= id) lo = mid; else hi = mid;
     }
     const int rel = id - groups.item0[lo];
-    seq0 = groups.seq0[lo];
-    n_mem = groups.members[lo];
-    kvh = rel % p.n_kv_heads;
-    key0 = rel / p.n_kv_heads * key_weights_keys(NT);
-    key_end = groups.prefix[lo];
+    it.seq0 = groups.seq0[lo];
+    it.n_mem = groups.members[lo];
+    it.kvh = rel % p.n_kv_heads;
+    it.key0 = rel / p.n_kv_heads * KEYS;
+    it.key_end = groups.prefix[lo];
   } else {
     int rel = (int)blockIdx.x - p.prefix_items;
-    kvh = rel % p.n_kv_heads;
+    it.kvh = rel % p.n_kv_heads;
     rel /= p.n_kv_heads;
     const int chunk = rel % p.own_chunks;
-    seq0 = rel / p.own_chunks;
-    n_mem = 1;
+    it.seq0 = rel / p.own_chunks;
+    it.n_mem = 1;
     int lo = 0, hi = groups.n;  // its group
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (groups.seq0[mid] <= seq0) lo = mid; else hi = mid;
+      if (groups.seq0[mid] <= it.seq0) lo = mid; else hi = mid;
     }
-    const bool in = groups.n > 0 && groups.seq0[lo] <= seq0 && seq0 < groups.seq0[lo] + groups.members[lo];
-    key0 = (in ? groups.prefix[lo] : 0) + chunk * key_weights_keys(NT);
-    key_end = clamped_length(p.seq_len, p.cap, seq0);
+    const bool in = groups.n > 0 && groups.seq0[lo] <= it.seq0 && it.seq0 < groups.seq0[lo] + groups.members[lo];
+    it.key0 = (in ? groups.prefix[lo] : 0) + chunk * KEYS;
+    it.key_end = clamped_length(p.seq_len, p.cap, it.seq0);
   }
-  if (key0 >= key_end) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int col = lane & 31, hf = lane >> 5;
-  const int item_last = min(key_end, key0 + key_weights_keys(NT)) - 1;
-
-  // ---- a wave's keys ------------------------------------------------------------------------------------------
+  return it;
+}
+// A wave's keys, the B operand: lane = key, chunk 2 kk + half of its row.
+template <int D, int NT>
+struct WaveKeys {
   int key[NT];
   bool there[NT];
-  bf16x8_t kf[NT][KCH];
+  bf16x8_t frag[NT][D / 16];
+  __device__ __forceinline__ void load(const KeyWeightsParams &p, const WeightsItem &it, int key0, int lane) {
 #pragma unroll
-  for (int t = 0; t < NT; ++t) {
-    key[t] = key0 + (wave * NT + t) * 32 + col;
-    const int k = min(key[t], key_end - 1), page_at = (int)fast_div((uint32_t)k, p.pages.page_div);
-    int page = page_at < p.pages.max_pages ? p.pages.table[seq0 * p.pages.stride + page_at] : -1;
-    there[t] = page >= 0 && page < p.pages.n_pages;
-    page = there[t] ? page : 0;  // (some row that is there: its sums are dropped)
-    const char *row = (const char *)(p.k.base + kvh * p.k.sh) + ((uint64_t)(uint32_t)page * p.k.page_b16 << 4) +
-                      (uint64_t)(uint32_t)(k - page_at * p.pages.page_rows) * p.k.rb + hf * 16;
+    for (int t = 0; t < NT; ++t) {
+      key[t] = key0 + t * 32 + (lane & 31);
+      const int k = min(key[t], it.key_end - 1), page_at = (int)fast_div((uint32_t)k, p.pages.page_div);
+      int page = page_at < p.pages.max_pages ? p.pages.table[it.seq0 * p.pages.stride + page_at] : -1;
+      there[t] = page >= 0 && page < p.pages.n_pages;
+      page = there[t] ? page : 0;  // (some row that is there: its sums are dropped)
+      const char *row = (const char *)(p.k.base + it.kvh * p.k.sh) + ((uint64_t)(uint32_t)page * p.k.page_b16 << 4) +
+                        (uint64_t)(uint32_t)(k - page_at * p.pages.page_rows) * p.k.rb + (lane >> 5) * 16;
 #pragma unroll
-    for (int kk = 0; kk < KCH; ++kk) kf[t][kk] = *reinterpret_cast<const bf16x8_t *>(row + kk * 32);
+      for (int kk = 0; kk < D / 16; ++kk) frag[t][kk] = *reinterpret_cast<const bf16x8_t *>(row + kk * 32);
+    }
   }
+};
 
-  // ---- query rows, a tile of 32 at a time ---------------------------------------------------------------------
-  const int n_rows = n_mem * p.padded, n_tiles = (n_rows + 31) / 32;
-  auto tok_of = [&](int r, int &head, int &i) __attribute__((always_inline)) {  // row -> its token, -1: padding
-    const int j = (int)fast_div((uint32_t)r, p.padded_div), at = r - j * p.padded;
+// Query rows go from memory straight into LDS, two tiles ahead.
+constexpr int kRowsTiles = 2, kRowsBuffers = 3;
+static_assert(kWThreads / 64 * 32 * kRowsTiles == kWeightsManyKeys && kWThreads / 64 * 32 == kWeightsFewKeys, "what the plan counts with");
+// 16 bytes a lane from `from` to LDS bytes [lds_base + 16 lane, +16), as lds_dma16
+__device__ __forceinline__ void lds_dma16_lane(const char *from, uint32_t lds_base) {
+  lds_base = (uint32_t)__builtin_amdgcn_readfirstlane((int)lds_base);
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(from), "s"(lds_base) : "memory");
+}
+
+// ---- few rows a sequence: 32 keys a wave ----------------------------------------------------------------------------
+// A sequence's rows begin at a multiple of 4 (of 8 if it has more than 4): a quad of accumulators is one sequence's, and a tile of rows is
+// several's.  kEven: without padding, and 32 rows on is the same head, so every tile lies as far from the one before.
+template <int D, bool kFour, bool kEven, typename Groups>
+__global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsParams p, Groups groups) {
+  constexpr int NB = kRowsBuffers;
+  constexpr int CPR = D / 8, KCH = D / 16, ROWB = D * 2, LPR = 256 / ROWB, RPI = 1024 / ROWB;  // RPI: rows of a load instruction
+  constexpr int OPS = 32 / RPI / (kWThreads / 64);                                             // of a wave and tile
+  constexpr uint32_t TB = 32 * ROWB;
+  constexpr int kNoted = 16, kNotes = 3 * 32 * 4;  // tiles whose notes lie in LDS at a time; bytes of a tile's
+  __shared__ __attribute__((aligned(1024))) char smem_generic[NB * TB + kNoted * (kNotes + 4)];
+  lds_char *const smem = (lds_char *)smem_generic, *const notes_at = smem + NB * TB;
+  lds_i *const all_at = (lds_i *)(notes_at + kNoted * kNotes);
+  const WeightsItem item = weights_item<kWeightsFewKeys>(p, groups);
+  if (item.key0 >= item.key_end) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, hf = lane >> 5;
+  const int item_last = min(item.key_end, item.key0 + kWeightsFewKeys) - 1;
+  const int n_rows = item.n_mem * p.padded, n_tiles = (n_rows + 31) / 32;
+
+  // row r: its sequence, token and head; false: padding (a row that is there in its place)
+  auto place = [&](int r, int &j, int &i, int64_t &tok, int &head) __attribute__((always_inline)) {
+    const bool there = r < n_rows;
+    r = min(r, n_rows - 1);
+    j = (int)fast_div((uint32_t)r, p.padded_div);
+    const int at = min(r - j * p.padded, p.rows - 1);
     i = (int)fast_div((uint32_t)at, p.group_div);
-    head = kvh * p.group + at - i * p.group;
-    return r < n_rows && at < p.rows ? (seq0 + j) * p.nq + i : -1;
+    tok = (int64_t)(item.seq0 + j) * p.nq + i;
+    head = item.kvh * p.group + at - i * p.group;
+    return there && r - j * p.padded < p.rows;
   };
-  u32x4_t piece[PIECES];
-  float my_nl = 0.f;
-  int my_limit = 0, my_len = 0;
-  auto load_tile = [&](int tile) __attribute__((always_inline)) {
+  auto where = [&](int u, int tile) __attribute__((always_inline)) {
+    const int row = (wave * OPS + u) * RPI + lane / CPR;
+    int j, i, head;
+    int64_t tok;
+    place(tile * 32 + row, j, i, tok, head);
+    return (const char *)(p.q + tok * p.q_st + head * p.q_sh) + (((lane % CPR) ^ ((row / LPR) & (CPR - 1))) << 4);
+  };
+  const char *from_even[OPS];
+  const int64_t tile_step = 32 / p.group * p.q_st * 2;
+  if constexpr (kEven)
 #pragma unroll
-    for (int u = 0; u < PIECES; ++u) {
-      int head, i;
-      const int tok = tok_of(tile * 32 + u * RPP + (int)threadIdx.x / CPR, head, i);
-      piece[u] = u32x4_t{0, 0, 0, 0};
-      if (tok >= 0) piece[u] = *reinterpret_cast<const u32x4_t *>(p.q + tok * p.q_st + head * p.q_sh + threadIdx.x % CPR * 8);
-    }
-    if (threadIdx.x < 32) {
-      const int r = tile * 32 + (int)threadIdx.x;
-      int head, i;
-      const int tok = tok_of(r, head, i);
-      my_len = clamped_length(p.seq_len, p.cap, min(seq0 + (int)fast_div((uint32_t)min(r, n_rows - 1), p.padded_div), p.n_seqs - 1));
-      my_limit = 0;
-      if (tok >= 0) {
-        const float l = p.lse[(int64_t)tok * (p.n_kv_heads * p.group) + head];
-        my_nl = -l * 1.4426950408889634f;
-        my_limit = l == -INFINITY ? 0 : my_len - p.nq + i + 1;
-      }
-    }
-  };
-  auto store_tile = [&](int tile) __attribute__((always_inline)) {
-    lds_char *const to = smem + (tile & 1) * (TB + kMeta);
+    for (int u = 0; u < OPS; ++u) from_even[u] = where(u, 0);
+  auto issue = [&](uint32_t to, int tile) __attribute__((always_inline)) {
+    const bool whole = kEven && tile * 32 + 32 <= n_rows;  // (the last one may reach beyond the rows)
 #pragma unroll
-    for (int u = 0; u < PIECES; ++u) {
-      const int row = u * RPP + threadIdx.x / CPR, c = threadIdx.x % CPR;
-      *(lds_u32x4 *)(to + row * ROWB + ((c ^ ((row / LPR) & (CPR - 1))) << 4)) = piece[u];
-    }
-    if (threadIdx.x < 32) {
-      ((lds_f *)(to + TB))[threadIdx.x] = my_nl;
-      ((lds_i *)(to + TB))[32 + threadIdx.x] = my_limit;
-      ((lds_i *)(to + TB))[64 + threadIdx.x] = my_len;
-      // whether every row of the tile sees all of the item's keys
-      const bool all = (uint32_t)__builtin_amdgcn_ballot_w64(my_limit > item_last) == ~0u;
-      if (threadIdx.x == 0) ((lds_i *)(to + TB))[96] = all;
+    for (int u = 0; u < OPS; ++u) {
+      const char *from;
+      if (whole) from = from_even[u], from_even[u] += tile_step;
+      else from = where(u, tile);
+      lds_dma16_lane(from, (uint32_t)(uintptr_t)smem + to + (wave * OPS + u) * 1024);
     }
   };
-  load_tile(0);
-  store_tile(0);
-  __syncthreads();
-
-  float sum[NT];
-#pragma unroll
-  for (int t = 0; t < NT; ++t) sum[t] = 0.f;
-  // the weights of sequence seq0 + j: what there was, and the new sum
-  auto finish = [&](int t, int j, float total, int len) __attribute__((always_inline)) {
-    if (key[t] > item_last || key[t] >= len) return;
-    const int64_t at = ((int64_t)(seq0 + j) * p.n_kv_heads + kvh) * p.w_stride + key[t];
-    float w = there[t] ? total : 0.f;
-    if (p.w_in && key[t] < len - p.nq) w = __builtin_fmaf(p.decay, p.w_in[at], w);
-    p.w_out[at] = w;
-  };
+  // what the rows of the next kNoted tiles have beside them: -lse in log2 units, the key that each ends before, the sequence's length; whether all
+  // of a tile see all keys
+  auto note = [&](int tile0) __attribute__((always_inline)) {
 #pragma unroll 1
-  for (int tile = 0; tile < n_tiles; ++tile) {
-    if (tile + 1 < n_tiles) load_tile(tile + 1);
-    lds_char *const from = smem + (tile & 1) * (TB + kMeta);
-    const bool all = ((lds_i *)(from + TB))[96] != 0;
-    f32x16_t s[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) s[t][v] = 0.f;
-#pragma unroll
-    for (int kk = 0; kk < KCH; ++kk) {
-      const bf16x8_t qf = *(lds_bf16x8 *)(from + col * ROWB + (((2 * kk + hf) ^ ((col / LPR) & (CPR - 1))) << 4));
-#pragma unroll
-      for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[t][kk], s[t], 0, 0, 0);
+    for (int n = threadIdx.x; n < min(kNoted, n_tiles - tile0) * 32; n += kWThreads) {
+      int j, i, head;
+      int64_t tok;
+      const bool there = place(tile0 * 32 + n, j, i, tok, head);
+      const float lse = p.lse[tok * (p.n_kv_heads * p.group) + head];
+      const int len = clamped_length(p.seq_len, p.cap, item.seq0 + j), limit = there && lse != -INFINITY ? len - p.nq + i + 1 : 0;
+      lds_char *const to = notes_at + n / 32 * kNotes;
+      ((lds_f *)to)[n % 32] = -lse * 1.4426950408889634f;
+      ((lds_i *)to)[32 + n % 32] = limit;
+      ((lds_i *)to)[64 + n % 32] = len;
+      const uint64_t see_all = __builtin_amdgcn_ballot_w64(limit > item_last);  // (two tiles to a wave)
+      if (n % 32 == 0) all_at[n / 32] = (uint32_t)(see_all >> (lane & 32)) == ~0u;
     }
+  };
+  issue(0, 0);
+  WaveKeys<D, 1> k;
+  k.load(p, item, item.key0 + wave * 32, lane);
+  const int key = k.key[0];
+  note(0);
+
+  const uint32_t q_rd = col * ROWB + ((hf ^ ((col / LPR) & (CPR - 1))) << 4);  // (chunk pairs kk on are an exclusive or away)
+  float sum = 0.f;
+  int j = 0, left = p.padded;  // (more than 4 rows a sequence: the one that the next eight rows belong to, its rows from there on)
+  const int64_t from_seq = p.n_kv_heads * p.w_stride, list = ((int64_t)item.seq0 * p.n_kv_heads + item.kvh) * p.w_stride;
+  const int64_t mine = list + key + (kFour ? hf * from_seq : 0);
+  const bool stores = key <= item_last && (kFour || hf == 0);
+  // which sequences end in a tile, and what they had: asked for a tile ahead (whether it counts is seen later)
+  int64_t at[4], next_at[4];  // of their weights, behind `mine`; -1: none ends with these eight rows
+  float old[4], next_old[4];
+  auto ahead = [&](int tile) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int r0 = tile * 32 + i * 8;  // this lane's rows: r0 + hf * 4 + (0 .. 3)
-      if (r0 >= n_rows) break;
-      const f32x4_t nl = *(const lds_f32x4 *)(from + TB + (i * 8 + hf * 4) * 4);
-      const i32x4_t limit = *(const lds_i32x4 *)(from + TB + (32 + i * 8 + hf * 4) * 4);
-      const int len = ((const lds_i *)(from + TB))[64 + i * 8 + hf * 4];
+      next_at[i] = -1;
+      if (tile * 32 + i * 8 < n_rows) {
+        if constexpr (kFour) next_at[i] = (tile * 8 + i * 2) * from_seq;
+        else if ((left -= 8) == 0) next_at[i] = j++ * from_seq, left = p.padded;
+      }
+      next_old[i] = 0.f;
+      if (p.w_in && next_at[i] >= 0 && stores && (!kFour || tile * 32 + i * 8 + hf * 4 < n_rows)) next_old[i] = (p.w_in + mine)[next_at[i]];
+    }
+  };
+  ahead(0);
+  if (n_tiles > 1) issue(TB, 1);
+  lds_wait();
+  uint32_t buffer = 0;
+#pragma unroll 1
+  for (int tile = 0; tile < n_tiles; ++tile) {
+    if (tile + 1 < n_tiles) dma_wait<OPS>(); else dma_wait<0>();
+    wg_barrier();  // the tile is there, and its notes; nobody needs the one before
+    if (tile > 0 && tile % kNoted == 0) {
+      note(tile);
+      lds_wait();
+      wg_barrier();
+    }
+    const uint32_t from = q_rd + buffer;
+    buffer = buffer == (NB - 1) * TB ? 0 : buffer + TB;
 #pragma unroll
-      for (int t = 0; t < NT; ++t) {
+    for (int i = 0; i < 4; ++i) at[i] = next_at[i], old[i] = next_old[i];
+    if (tile + 1 < n_tiles) ahead(tile + 1);
+    if (tile + 2 < n_tiles) issue(buffer == (NB - 1) * TB ? 0 : buffer + TB, tile + 2);
+    lds_char *const beside = notes_at + tile % kNoted * kNotes;
+    f32x16_t s;
+#pragma unroll
+    for (int kk = 0; kk < KCH; ++kk) {
+      const f32x16_t zero = {};
+      const bf16x8_t qf = *(lds_bf16x8 *)(smem + (from ^ (kk << 5)));
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, k.frag[0][kk], kk ? s : zero, 0, 0, 0);
+    }
+    auto sums = [&](auto masked) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // this lane's rows: tile * 32 + i * 8 + hf * 4 + (0 .. 3)
+        if (tile * 32 + i * 8 >= n_rows) break;
+        const f32x4_t nl = *(const lds_f32x4 *)(beside + (i * 8 + hf * 4) * 4);
+        i32x4_t limit = {0, 0, 0, 0};
+        if constexpr (decltype(masked)::value) limit = *(const lds_i32x4 *)(beside + (32 + i * 8 + hf * 4) * 4);
         float e[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-          e[c] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i * 4 + c], p.scale_log2e, nl[c]));
-          if (!all && key[t] >= limit[c]) e[c] = 0.f;
+          e[c] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i * 4 + c], p.scale_log2e, nl[c]));
+          if constexpr (decltype(masked)::value) e[c] = key < limit[c] ? e[c] : 0.f;
         }
-        const float quad = (e[0] + e[1]) + (e[2] + e[3]);
-        if (p.padded == 4) {
-          if (r0 + hf * 4 < n_rows) finish(t, r0 / 4 + hf, quad, len);
-        } else {
-          sum[t] += quad;
+        sum += (e[0] + e[1]) + (e[2] + e[3]);
+        if (at[i] >= 0) {
+          float total = sum;
+          if constexpr (!kFour) total += other_half(total);
+          sum = 0.f;
+          const int len = ((const lds_i *)beside)[64 + i * 8 + (kFour ? hf * 4 : 0)];
+          if (stores && key < len && (!kFour || tile * 32 + i * 8 + hf * 4 < n_rows))
+            (p.w_out + mine)[at[i]] = __builtin_fmaf(p.decay, key < len - p.nq ? old[i] : 0.f, k.there[0] ? total : 0.f);
         }
       }
-      if (p.padded > 4) {
-        const int j = (int)fast_div((uint32_t)r0, p.padded_div);
-        if (r0 + 8 == (j + 1) * p.padded) {  // the sequence's last rows
+    };
+    if (__builtin_amdgcn_readfirstlane(all_at[tile % kNoted]) != 0) sums(std::false_type{});
+    else sums(std::true_type{});
+  }
+}
+
+// ---- many rows a sequence: 64 keys a wave ---------------------------------------------------------------------------
+// A score costs its exponential (half the vector rate), a scaling and an addition.
+// kEven: a sequence's rows are whole tiles, and 32 rows on is the same head, so every tile lies as far from the one before.
+template <int D, bool kEven, typename Groups>
+__global__ __launch_bounds__(kWThreads, kEven ? 4 : 3) void key_weights_many_kernel(KeyWeightsParams p, Groups groups) {
+  constexpr int NT = kRowsTiles, NB = kRowsBuffers;
+  constexpr int CPR = D / 8, KCH = D / 16, ROWB = D * 2, LPR = 256 / ROWB, RPI = 1024 / ROWB;  // RPI: rows of a load instruction
+  constexpr int OPS = 32 / RPI / (kWThreads / 64);                                             // of a wave and tile
+  constexpr uint32_t TB = 32 * ROWB;
+  constexpr int kNoted = 32, kNotes = 2 * 32 * 4;  // tiles whose notes lie in LDS at a time; bytes of a tile's
+  __shared__ __attribute__((aligned(1024))) char smem_generic[NB * TB + kNoted * (kNotes + 4)];
+  lds_char *const smem = (lds_char *)smem_generic, *const notes_at = smem + NB * TB;
+  lds_i *const all_at = (lds_i *)(notes_at + kNoted * kNotes);
+  const WeightsItem item = weights_item<kWeightsManyKeys>(p, groups);
+  if (item.key0 >= item.key_end) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 31, hf = lane >> 5;
+  const int item_last = min(item.key_end, item.key0 + kWeightsManyKeys) - 1;
+  const int per_seq = (p.rows + 31) / 32, n_tiles = item.n_mem * per_seq;  // tiles of a sequence (the last one may end early), of all
+
+  // row r of sequence j: its token, its head
+  auto place = [&](int j, int r, int64_t &tok, int &head) __attribute__((always_inline)) {
+    const int i = (int)fast_div((uint32_t)r, p.group_div);
+    tok = (int64_t)(item.seq0 + j) * p.nq + i;
+    head = item.kvh * p.group + r - i * p.group;
+    return i;
+  };
+  const char *from_even[OPS];
+  const int64_t tile_step = 32 / p.group * p.q_st * 2;
+  // tile `at` of sequence j: rows at * 32 + (0 .. 31) of it, the last one again behind it (and masked)
+  auto where = [&](int u, int j, int at) __attribute__((always_inline)) {
+    const int row = (wave * OPS + u) * RPI + lane / CPR;
+    int64_t tok;
+    int head;
+    place(j, min(at * 32 + row, p.rows - 1), tok, head);
+    return (const char *)(p.q + tok * p.q_st + head * p.q_sh) + (((lane % CPR) ^ ((row / LPR) & (CPR - 1))) << 4);
+  };
+  if constexpr (kEven)
 #pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            const float total = sum[t] + other_half(sum[t]);
-            if (hf == 0) finish(t, j, total, len);
-            sum[t] = 0.f;
+    for (int u = 0; u < OPS; ++u) from_even[u] = where(u, 0, 0);
+  int j_in = 0, at_in = 0;  // the tile that is asked for next
+  auto issue = [&](uint32_t to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < OPS; ++u) {
+      const char *from;
+      if constexpr (kEven) from = from_even[u], from_even[u] += tile_step;
+      else from = where(u, j_in, at_in);
+      lds_dma16_lane(from, (uint32_t)(uintptr_t)smem + to + (wave * OPS + u) * 1024);
+    }
+    if (++at_in == per_seq) at_in = 0, ++j_in;
+  };
+  // what the rows of the next kNoted tiles have beside them: -lse in log2 units, the key that each ends before, whether a tile's rows see all keys
+  auto note = [&](int tile0) __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int n = threadIdx.x; n < min(kNoted, n_tiles - tile0) * 32; n += kWThreads) {
+      const int tile = tile0 + n / 32, j = tile / per_seq, r = (tile - j * per_seq) * 32 + n % 32;
+      int64_t tok;
+      int head;
+      const int i = place(j, min(r, p.rows - 1), tok, head);
+      const float lse = p.lse[tok * (p.n_kv_heads * p.group) + head];
+      const int limit = r < p.rows && lse != -INFINITY ? clamped_length(p.seq_len, p.cap, item.seq0 + j) - p.nq + i + 1 : 0;
+      lds_char *const to = notes_at + n / 32 * kNotes;
+      ((lds_f *)to)[n % 32] = -lse * 1.4426950408889634f;
+      ((lds_i *)to)[32 + n % 32] = limit;
+      const uint64_t see_all = __builtin_amdgcn_ballot_w64(limit > item_last);  // (two tiles to a wave)
+      if (n % 32 == 0) all_at[n / 32] = (uint32_t)(see_all >> (lane & 32)) == ~0u;
+    }
+  };
+  issue(0);
+  WaveKeys<D, NT> k;
+  k.load(p, item, item.key0 + wave * NT * 32, lane);
+  note(0);
+  if (n_tiles > 1) issue(TB);
+  lds_wait();
+
+  const uint32_t q_rd = col * ROWB + ((hf ^ ((col / LPR) & (CPR - 1))) << 4);  // (chunk pairs kk on are an exclusive or away)
+  float sum[NT] = {};
+  int j = 0, at = 0;
+  uint32_t buffer = 0;
+#pragma unroll 1
+  for (int tile = 0; tile < n_tiles; ++tile) {
+    if (tile + 1 < n_tiles) dma_wait<OPS>(); else dma_wait<0>();
+    wg_barrier();  // the tile is there, and its notes; nobody needs the one before
+    if (tile > 0 && tile % kNoted == 0) {
+      note(tile);
+      lds_wait();
+      wg_barrier();
+    }
+    const uint32_t from = q_rd + buffer;
+    buffer = buffer == (NB - 1) * TB ? 0 : buffer + TB;
+    if (tile + 2 < n_tiles) issue(buffer == (NB - 1) * TB ? 0 : buffer + TB);
+    lds_char *const beside = notes_at + tile % kNoted * kNotes;
+    f32x16_t s[NT];
+    auto q_frag = [&](int kk) __attribute__((always_inline)) { return *(lds_bf16x8 *)(smem + (from ^ (kk << 5))); };
+    constexpr int kWin = 2;  // fragments on their way from LDS
+    bf16x8_t qf[kWin];
+    qf[0] = q_frag(0);
+#pragma unroll
+    for (int kk = 0; kk < KCH; ++kk) {
+      const f32x16_t zero = {};
+      if (kk + 1 < KCH) qf[(kk + 1) % kWin] = q_frag(kk + 1);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[kk % kWin], k.frag[t][kk], kk ? s[t] : zero, 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    auto sums = [&](auto masked) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {  // this lane's rows: i * 8 + hf * 4 + (0 .. 3)
+        const f32x4_t nl = *(const lds_f32x4 *)(beside + (i * 8 + hf * 4) * 4);
+        i32x4_t lim = {0, 0, 0, 0};
+        if constexpr (decltype(masked)::value) lim = *(const lds_i32x4 *)(beside + (32 + i * 8 + hf * 4) * 4);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          float e[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            e[c] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i * 4 + c], p.scale_log2e, nl[c]));
+            if constexpr (decltype(masked)::value) e[c] = k.key[t] < lim[c] ? e[c] : 0.f;
           }
+          sum[t] += (e[0] + e[1]) + (e[2] + e[3]);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (as few of them on their way as the registers have room for)
+      }
+    };
+    if (__builtin_amdgcn_readfirstlane(all_at[tile % kNoted]) != 0) sums(std::false_type{});
+    else sums(std::true_type{});
+    if (++at == per_seq) {
+      const int len = clamped_length(p.seq_len, p.cap, item.seq0 + j);
+      const int64_t list = ((int64_t)(item.seq0 + j) * p.n_kv_heads + item.kvh) * p.w_stride;
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        const float total = sum[t] + other_half(sum[t]);
+        sum[t] = 0.f;
+        if (hf == 0 && k.key[t] <= item_last && k.key[t] < len) {
+          const float old = p.w_in && k.key[t] < len - p.nq ? p.w_in[list + k.key[t]] : 0.f;
+          p.w_out[list + k.key[t]] = __builtin_fmaf(p.decay, old, k.there[t] ? total : 0.f);
         }
       }
+      at = 0, ++j;
     }
-    if (tile + 1 < n_tiles) store_tile(tile + 1);
-    __syncthreads();
   }
 }
 
 template <int D, typename Groups>
-hipError_t launch_d(const KeyWeightsParams &p, const Groups &g, int tiles, hipStream_t stream) {
+hipError_t launch_d(const KeyWeightsParams &p, const Groups &g, bool many, hipStream_t stream) {
   const int64_t items = p.prefix_items + (int64_t)p.n_seqs * p.n_kv_heads * p.own_chunks;
   if (items < 1 || items > kMaxWorkgroups) return hipErrorInvalidValue;
-  if (tiles == 2) key_weights_kernel<D, 2, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
-  else key_weights_kernel<D, 1, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
+  if (many && p.rows % 32 == 0 && 32 % p.group == 0) key_weights_many_kernel<D, true, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
+  else if (many) key_weights_many_kernel<D, false, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
+  else {
+    auto launch = [&](auto four, auto even) {
+      key_weights_kernel<D, decltype(four)::value, decltype(even)::value, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
+    };
+    const bool even = p.rows == p.padded && 32 % p.group == 0;
+    if (p.padded == 4) even ? launch(std::true_type{}, std::true_type{}) : launch(std::true_type{}, std::false_type{});
+    else even ? launch(std::false_type{}, std::true_type{}) : launch(std::false_type{}, std::false_type{});
+  }
   return hipGetLastError();
 }
 
 }  // namespace
 
 template <typename Groups>
-hipError_t launch_key_weights(const KeyWeightsParams &p, const Groups &g, int head_dim, int tiles, hipStream_t stream) {
-  return head_dim == 128 ? launch_d<128>(p, g, tiles, stream) : launch_d<64>(p, g, tiles, stream);
+hipError_t launch_key_weights(const KeyWeightsParams &p, const Groups &g, int head_dim, bool many, hipStream_t stream) {
+  return head_dim == 128 ? launch_d<128>(p, g, many, stream) : launch_d<64>(p, g, many, stream);
 }
-template hipError_t launch_key_weights(const KeyWeightsParams &, const PagedGroups &, int, int, hipStream_t);
-template hipError_t launch_key_weights(const KeyWeightsParams &, const PagedGroupsSmall &, int, int, hipStream_t);
+template hipError_t launch_key_weights(const KeyWeightsParams &, const PagedGroups &, int, bool, hipStream_t);
+template hipError_t launch_key_weights(const KeyWeightsParams &, const PagedGroupsSmall &, int, bool, hipStream_t);
 
 }  // namespace ba
