@@ -219,7 +219,7 @@ int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const
   if (weights_out && stride_out < n_keep) return fail(BA_ERR_INVALID_ARG, "stride_out smaller than n_keep");
   const int64_t lists = (int64_t)n_seqs * hkv;
   if ((rc = check_lists(n_seqs, heads))) return rc;
-  if (lists * ((n_keep + kEvictCopyRows - 1) / kEvictCopyRows) > kMaxWorkgroups) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
+  if (n_seqs * evict_copy_chunks(n_keep, max_len, hkv) > kMaxWorkgroups || (int64_t)std::min(n_keep, max_len) * hkv > (1 << 30)) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
   // ---- where everything lies
   if (!apart(extent(&to->k, to->page_rows, hkv, D), extent(&to->v, to->page_rows, hkv, D)))
     return fail(BA_ERR_INVALID_ARG, "to: keys and values of a page overlap");
@@ -259,6 +259,9 @@ int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const
   set_rows(&p.k, &cache->k, cache->k_stride_page), set_rows(&p.v, &cache->v, cache->v_stride_page);
   set_rows(&p.to_k, &to->k, to->k_stride_page), set_rows(&p.to_v, &to->v, to->v_stride_page);
   set_table(&p.from, cache), set_table(&p.to, to);
+  p.heads_div = make_fast_div((uint32_t)hkv);
+  // (rows go by once, and are read next after all other layers' have gone by, too)
+  p.past_caches = lists * std::min(n_keep, max_len) * D * 8 > kCacheBytes * 3 / 4;
   hipError_t e;
   {
     ProfileScope ps(BA_PROFILE_COMBINE, stream);
@@ -342,7 +345,7 @@ int32_t ba_page_select(const ba_heads *heads, const ba_paged_cache *cache, const
   p.selected = selected_out, p.scores_out = scores_out;
   p.scores = (float *)ws;
   p.score_stride = ((int64_t)max_len + cache->page_rows - 1) / cache->page_rows;
-  if (lists * ((p.score_stride + kScorePages - 1) / kScorePages) > kMaxWorkgroups) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
+  if ((n_seqs * ((p.score_stride + kScorePages - 1) / kScorePages) + 8) * hkv > kMaxWorkgroups) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
   hipError_t e = hipSuccess;
   if (max_len > 0) {
     ProfileScope ps(BA_PROFILE_ATTENTION, stream);

@@ -56,9 +56,14 @@ struct EvictParams {
   int32_t *len_out;        // nullable
   PagedRowsParams k, v, to_k, to_v;
   PagedTableParams from, to;
+  FastDiv heads_div;       // by n_kv_heads
+  int32_t past_caches;     // rows are copied past the caches
 };
 constexpr int64_t kMaxPickWorkgroups = 0xffffffffll / 1024;
-constexpr int kEvictCopyRows = 64;  // kept rows that a workgroup copies
+constexpr int kEvictCopyRows = 64;  // rows of heads that a workgroup copies
+inline int64_t evict_copy_chunks(int64_t n_keep, int64_t cap, int64_t n_kv_heads) {
+  return ((n_keep < cap ? n_keep : cap) * n_kv_heads + kEvictCopyRows - 1) / kEvictCopyRows;
+}
 hipError_t launch_evict_pick(const EvictParams &p, hipStream_t stream);
 hipError_t launch_evict_copy(const EvictParams &p, hipStream_t stream);
 

@@ -5,7 +5,7 @@
 
 namespace ba {
 
-// Order of floats as unsigned numbers above 0 (0: not in the list); -0 as 0, a NaN below everything, kPickAlways above it.
+// Order of floats as unsigned numbers; -0 as 0, a NaN below everything.  0: not in the list, kPickAlways: taken ahead of all others.
 constexpr uint32_t kPickAlways = 0xffffffffu;
 __device__ __forceinline__ uint32_t pick_key(float x) {
   if (x != x) return 1u;
@@ -13,87 +13,230 @@ __device__ __forceinline__ uint32_t pick_key(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Digits of 11, 11 and 10 bits, from the highest: a histogram of those that share the digits found so far, in LDS, says in which bin the
-// n-th largest lies; then every wave counts and writes a run of places of its own.
-constexpr int kPickWaves = 16, kPickThreads = kPickWaves * 64, kPickBins = 2048;
+constexpr int kPickFew = 64;
+// W: waves of the workgroup, 4 or 16; two bins a thread
+template <int W>
 struct PickLds {
-  uint32_t hist[kPickBins];
-  uint32_t wave_sum[kPickWaves], wave_equal[kPickWaves];
-  uint32_t bin, left, total;
+  uint32_t hist[W * 128];
+  alignas(16) uint32_t a[W], b[W], least[W], most[W], above[W], equal[W];  // of each wave
+  uint32_t few[kPickFew];
+  uint32_t bin, left, in_bin, n_few;
 };
-// key(i), i in [0, n): its order, 0: not in the list.  emit(position, i) for the `want` largest (all, if there are no more).  Returns their number.
-template <typename Key, typename Emit>
-__device__ __forceinline__ int pick_largest(PickLds &l, int n, int want, Key &&key, Emit &&emit) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  uint32_t found = 0, left = (uint32_t)want, total = 0;
-  int bits = 32;
-  bool all = false;
-#pragma unroll 1
-  for (int pass = 0; pass < 3; ++pass) {
-    const int width = pass == 2 ? 10 : 11, shift = bits - width;
-    for (int b = tid; b < kPickBins; b += kPickThreads) l.hist[b] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += kPickThreads) {
-      const uint32_t u = key(i);
-      if (u != 0 && (bits == 32 || (u >> (bits & 31)) == found)) atomicAdd(&l.hist[(u >> shift) & ((1u << width) - 1)], 1u);
-    }
-    __syncthreads();
-    // two bins a thread, from the highest down
-    const int top = kPickBins - 1 - 2 * tid;
-    const uint32_t a = l.hist[top], b = l.hist[top - 1];
-    uint32_t upto = a + b;
+// Across the 64 lanes without a trip through LDS: the smallest, the largest (in all of them), sums up to each lane.
+template <typename Op>
+__device__ __forceinline__ uint32_t pick_reduce(uint32_t x, Op &&op) {
+  auto with = [&](auto ctrl) __attribute__((always_inline)) { x = op(x, (uint32_t)__builtin_amdgcn_mov_dpp((int)x, decltype(ctrl)::value, 0xf, 0xf, true)); };
+  with(std::integral_constant<int, 0xb1>{});   // (as sum_over_lanes)
+  with(std::integral_constant<int, 0x4e>{});
+  with(std::integral_constant<int, 0x141>{});
+  with(std::integral_constant<int, 0x140>{});
+  auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = op((uint32_t)r[0], (uint32_t)r[1]);
+  r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return op((uint32_t)r[0], (uint32_t)r[1]);
+}
+__device__ __forceinline__ uint32_t pick_sums_upto(uint32_t x) {
+  auto add = [&](auto ctrl, auto rows) __attribute__((always_inline)) {
+    x += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, decltype(ctrl)::value, decltype(rows)::value, 0xf, false);
+  };
+  using std::integral_constant;
+  add(integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});  // one, two, four, eight lanes on within sixteen
+  add(integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+  add(integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+  add(integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+  add(integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});  // a sixteen's last lane to the next sixteen, the second and the fourth
+  add(integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});  // the first half's last lane to the other half
+  return x;
+}
+// The sum of what the waves in front of this one have left in `of`.
+template <int W>
+__device__ __forceinline__ uint32_t pick_before(const uint32_t (&of)[W], int wave, int lane) {
+  const uint32_t x = lane < wave ? of[lane & (W - 1)] : 0;
+  return (uint32_t)__builtin_amdgcn_readfirstlane((int)pick_reduce(x, [](uint32_t a, uint32_t b) { return a + b; }));
+}
+
+// value(i), i in [0, n): a number; key(i, number): its order.  emit(position, i, number) for the `want` largest (all that are in the list, if there
+// are no more).  Returns their number.
+// E > 0: n is at most E times the threads, and every thread keeps its numbers and keys; E = 0: they are looked up again by every pass.
+//
+// Every wave has a run of places of its own.  The smallest and the largest key say how many bits they differ in; a histogram by the highest
+// nine or eleven of those says in which bin the last one that is taken lies, and so on with the next ones within it, until its bin is taken whole,
+// holds equal keys only, or few enough to be ranked one against the other.  Bound by latency, and with a list a compute unit by the
+// instructions of its waves, which share four SIMDs: what is the same in all waves is done by one of them.
+template <int W, int E, typename Value, typename Key, typename Emit>
+__device__ __forceinline__ int pick_largest(PickLds<W> &l, int n, int want, Value &&value, Key &&key, Emit &&emit) {
+  constexpr int kPickThreads = W * 64, kPickBins = 2 * kPickThreads, kDigit = W == 16 ? 11 : 9;
+  static_assert(1 << kDigit == kPickBins, "a bin for each digit");
+  auto uniform = [](uint32_t x) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)x); };
+  const int tid = threadIdx.x, lane = tid & 63, wave = (int)uniform(tid >> 6);
+  const int steps = (n + kPickThreads - 1) / kPickThreads, run = steps * 64, begin = wave * run;
+  float number[E > 0 ? E : 1];
+  uint32_t mine[E > 0 ? E : 1];
+  if constexpr (E > 0) {
+    constexpr int kTogether = E < 8 ? E : 8;  // (asked for together)
 #pragma unroll
-    for (int m = 1; m < 64; m *= 2) {
-      const uint32_t o = __shfl_up(upto, m);
-      if (lane >= m) upto += o;
-    }
-    if (lane == 63) l.wave_sum[wave] = upto;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) upto += l.wave_sum[w];
-    if (pass == 0) {
-      if (tid == kPickThreads - 1) l.total = upto;
-      __syncthreads();
-      total = l.total;
-      if (total <= left) {
-        all = true;
-        break;
+    for (int g = 0; g < E; g += kTogether) {
+#pragma unroll
+      for (int s = g; s < g + kTogether; ++s) mine[s] = 0, number[s] = 0.f;
+      if (g >= steps) continue;
+#pragma unroll
+      for (int s = g; s < g + kTogether; ++s) number[s] = value(min(begin + s * 64 + lane, n - 1));
+#pragma unroll
+      for (int s = g; s < g + kTogether; ++s) {
+        const int i = begin + s * 64 + lane;
+        mine[s] = s < steps && i < n ? key(i, number[s]) : 0;
       }
     }
-    const uint32_t before = upto - a - b;
-    if (before < left && left <= upto) {
-      const bool first = left <= before + a;
-      l.bin = (uint32_t)(first ? top : top - 1);
-      l.left = left - before - (first ? 0 : a);
+  }
+  // f(step, key, number): this lane's of every step, the same steps in all lanes
+  auto each = [&](auto &&f) __attribute__((always_inline)) {
+    if constexpr (E > 0) {
+#pragma unroll
+      for (int s = 0; s < E; ++s)
+        if (s < steps) f(s, mine[s], number[s]);
+    } else {
+#pragma unroll 1
+      for (int s = 0; s < steps; ++s) {
+        const int i = begin + s * 64 + lane;
+        const float x = i < n ? value(i) : 0.f;
+        f(s, i < n ? key(i, x) : 0u, x);
+      }
     }
-    __syncthreads();
-    found = (pass == 0 ? 0 : found << width) | l.bin;
-    left = l.left;
-    bits = shift;
+  };
+  auto ordinary = [](uint32_t u) { return u - 1 < kPickAlways - 1; };
+
+  // ---- how many there are, and between what
+  for (int b = tid; b < kPickBins; b += kPickThreads) l.hist[b] = 0;
+  if (tid == 0) l.n_few = 0;
+  uint32_t least = kPickAlways, most = 0, n_always = 0, n_ordinary = 0;
+  each([&](int, uint32_t u, float) {
+    n_always += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u == kPickAlways));
+    n_ordinary += __builtin_popcountll(__builtin_amdgcn_ballot_w64(ordinary(u)));
+    least = min(least, ordinary(u) ? u : kPickAlways);
+    most = max(most, ordinary(u) ? u : 0);
+  });
+  least = pick_reduce(least, [](uint32_t a, uint32_t b) { return min(a, b); });
+  most = pick_reduce(most, [](uint32_t a, uint32_t b) { return max(a, b); });
+  if (lane == 0) l.a[wave] = n_always, l.b[wave] = n_ordinary, l.least[wave] = least, l.most[wave] = most;
+  __syncthreads();
+  {  // a lane for each wave's
+    const int w = lane & (W - 1);
+    n_always = lane < W ? l.a[w] : 0, n_ordinary = lane < W ? l.b[w] : 0;
+    least = uniform(pick_reduce(l.least[w], [](uint32_t a, uint32_t b) { return min(a, b); }));
+    most = uniform(pick_reduce(l.most[w], [](uint32_t a, uint32_t b) { return max(a, b); }));
+    const auto add = [](uint32_t a, uint32_t b) { return a + b; };
+    n_always = uniform(pick_reduce(n_always, add)), n_ordinary = uniform(pick_reduce(n_ordinary, add));
   }
-  // those above the last one, and the first `left` of its equals
-  if (all || want <= 0) found = all ? 0 : kPickAlways, left = 0;
-  const int run = ((n + kPickThreads - 1) / kPickThreads) * 64, begin = wave * run, end = min(n, begin + run);
+  const uint32_t total = min(n_always + n_ordinary, (uint32_t)max(want, 0));
+  uint32_t left = total - min(total, n_always);  // ordinary ones that are taken
+
+  // ---- the last one that is taken: those above `found`, and the first `left` of its equals
+  uint32_t found = 0;
+  if (left == 0) {
+    found = kPickAlways - 1;  // (no ordinary key is above it)
+  } else if (left == n_ordinary) {
+    left = 0;
+  } else {
+    uint32_t base = least;
+    int bits = 32 - __builtin_clz((most - least) | 1);
+    while (true) {  // (the same in all threads)
+      const int shift = max(0, bits - kDigit);
+      each([&](int, uint32_t u, float) {
+        if (ordinary(u) && u >= base && (bits == 32 || (u - base) >> (bits & 31) == 0)) atomicAdd(&l.hist[(u - base) >> shift], 1u);
+      });
+      __syncthreads();
+      // two bins a thread, from the highest down
+      const int top = kPickBins - 1 - 2 * tid;
+      const uint32_t first = l.hist[top], second = l.hist[top - 1];
+      uint32_t upto = pick_sums_upto(first + second);
+      if (lane == 63) l.a[wave] = upto;
+      __syncthreads();
+      upto += pick_before(l.a, wave, lane);
+      const uint32_t before = upto - first - second;
+      if (before < left && left <= upto) {
+        const bool in_first = left <= before + first;
+        l.bin = (uint32_t)(in_first ? top : top - 1);
+        l.left = left - before - (in_first ? 0 : first);
+        l.in_bin = in_first ? first : second;
+      }
+      __syncthreads();
+      base += uniform(l.bin) << shift;
+      left = uniform(l.left);
+      bits = shift;
+      const uint32_t in_bin = uniform(l.in_bin);
+      if (left == in_bin) {  // all of them
+        found = base - 1;
+        left = 0;
+        break;
+      }
+      if (shift == 0) {  // equal keys
+        found = base;
+        break;
+      }
+      if (in_bin <= kPickFew) {
+        each([&](int, uint32_t u, float) {
+          if (ordinary(u) && u >= base && (u - base) >> bits == 0) l.few[atomicAdd(&l.n_few, 1u)] = u;
+        });
+        __syncthreads();
+        if (wave == 0) {
+          // how many are above this lane's, and how many are its equals
+          const uint32_t my = lane < (int)in_bin ? l.few[lane] : 0;
+          uint32_t above = 0, equals = 0;
+          for (int o = 0; o < (int)in_bin; ++o) {
+            const uint32_t u = (uint32_t)__builtin_amdgcn_readlane((int)my, o);
+            above += u > my;
+            equals += u == my;
+          }
+          if (lane < (int)in_bin && above < left && left <= above + equals) l.bin = my, l.left = left - above;  // (its equals write the same)
+        }
+        __syncthreads();
+        found = uniform(l.bin);
+        left = uniform(l.left);
+        break;
+      }
+      for (int b = tid; b < kPickBins; b += kPickThreads) l.hist[b] = 0;
+      __syncthreads();
+    }
+  }
+
+  // ---- their places, in order
   uint32_t above = 0, equal = 0;
-  for (int i = begin + lane; i < begin + run; i += 64) {
-    const uint32_t u = i < end ? key(i) : 0;
-    above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u > found));
-    equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u == found && u != 0));
-  }
+  each([&](int, uint32_t u, float) { above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u > found)); });
+  if (left > 0) each([&](int, uint32_t u, float) { equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u == found)); });
+  if (lane == 0) l.above[wave] = above, l.equal[wave] = equal;
   __syncthreads();
-  if (lane == 0) l.wave_sum[wave] = above, l.wave_equal[wave] = equal;
-  __syncthreads();
-  above = equal = 0;
-  for (int w = 0; w < wave; ++w) above += l.wave_sum[w], equal += l.wave_equal[w];
-  const uint64_t below_me = (1ull << lane) - 1;
-  for (int i = begin + lane; i < begin + run; i += 64) {
-    const uint32_t u = i < end ? key(i) : 0;
-    const uint64_t gt = __builtin_amdgcn_ballot_w64(u > found), eq = __builtin_amdgcn_ballot_w64(u == found && u != 0);
-    const uint32_t g = above + __builtin_popcountll(gt & below_me), e = equal + __builtin_popcountll(eq & below_me);
-    if (u > found || (u == found && u != 0 && e < left)) emit((int)(g + min(e, left)), i);
+  above = pick_before(l.above, wave, lane);
+  if (left > 0) equal = pick_before(l.equal, wave, lane);
+  auto lanes_before = [&](uint64_t mask, uint32_t from) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, from)); };
+  each([&](int s, uint32_t u, float x) {
+    const uint64_t gt = __builtin_amdgcn_ballot_w64(u > found);
+    uint32_t at = lanes_before(gt, above);
+    bool taken = u > found;
+    if (left > 0) {
+      const uint64_t eq = __builtin_amdgcn_ballot_w64(u == found);
+      const uint32_t e = lanes_before(eq, equal);
+      at += min(e, left);
+      taken = taken || (u == found && e < left);
+      equal += __builtin_popcountll(eq);
+    }
+    if (taken) emit((int)at, begin + s * 64 + lane, x);
     above += __builtin_popcountll(gt);
-    equal += __builtin_popcountll(eq);
-  }
-  return (int)min(total, (uint32_t)max(want, 0));
+  });
+  return (int)total;
+}
+// Calls f with the waves and the number of keys that a thread has to keep for lists of up to n.
+// us a call of eight lists, 4 / 8 / 16 waves: selection out of 2,000 pages 11.8 / 10.9 / 9.7, eviction out of 2,064 tokens 11.6 / 12.0 / 11.5; of 512 lists:
+// selection out of up to 1,000 pages, 4 / 16 waves 8 / 12 (the kernel alone).
+template <typename F>
+auto with_pick_shape(int64_t n, F &&f) {
+  using std::integral_constant;
+  constexpr integral_constant<int, 4> four{};
+  constexpr integral_constant<int, 16> sixteen{};
+  if (n <= 1024) return f(four, integral_constant<int, 4>{});
+  if (n <= 4 * 1024) return f(sixteen, integral_constant<int, 4>{});
+  if (n <= 8 * 1024) return f(sixteen, integral_constant<int, 8>{});
+  if (n <= 32 * 1024) return f(sixteen, integral_constant<int, 32>{});
+  return f(sixteen, integral_constant<int, 0>{});
 }
 
 }  // namespace ba

@@ -8,8 +8,9 @@
 namespace ba {
 namespace {
 
-__global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictParams p) {
-  __shared__ PickLds lds;
+template <int W, int E>
+__global__ __launch_bounds__(W * 64) void evict_pick_kernel(EvictParams p) {
+  __shared__ PickLds<W> lds;
   const int kvh = blockIdx.x % p.n_kv_heads, seq = blockIdx.x / p.n_kv_heads;
   const int len = max(0, min(p.seq_len[seq], p.cap));
   const int64_t list = (int64_t)seq * p.n_kv_heads + kvh;
@@ -17,53 +18,56 @@ __global__ __launch_bounds__(kPickThreads) void evict_pick_kernel(EvictParams p)
   int32_t *kept = p.kept + list * p.n_keep;
   float *w_out = p.w_out ? p.w_out + list * p.w_out_stride : nullptr;
   const int last0 = len - p.n_last;
-  const int n = pick_largest(
-      lds, len, p.n_keep, [&](int i) { return i < p.n_first || i >= last0 ? kPickAlways : pick_key(w[i]); },
-      [&](int at, int i) {
+  const int n = pick_largest<W, E>(
+      lds, len, p.n_keep, [&](int i) { return w[i]; }, [&](int i, float x) { return i < p.n_first || i >= last0 ? kPickAlways : pick_key(x); },
+      [&](int at, int i, float x) {
         kept[at] = i;
-        if (w_out) w_out[at] = w[i];
+        if (w_out) w_out[at] = x;
       });
-  for (int j = n + threadIdx.x; j < p.n_keep; j += kPickThreads) kept[j] = -1;
+  for (int j = n + threadIdx.x; j < p.n_keep; j += W * 64) kept[j] = -1;
   if (kvh == 0 && threadIdx.x == 0 && p.len_out) p.len_out[seq] = n;
 }
 
 constexpr int kCopyThreads = 256, kCopyRows = kEvictCopyRows;
-__device__ __forceinline__ int page_of(const PagedTableParams &t, int seq, int at, int &row) {
-  const int i = (int)fast_div((uint32_t)at, t.page_div);
-  row = at - i * t.page_rows;
-  const int page = i < t.max_pages ? t.table[seq * t.stride + i] : -1;
-  return page >= 0 && page < t.n_pages ? page : -1;
+__device__ __forceinline__ char *row_at(const PagedRowsParams &r, int kvh, int page, int row) {
+  return (char *)(r.base + kvh * r.sh) + ((uint64_t)(uint32_t)page * r.page_b16 << 4) + (uint64_t)(uint32_t)row * r.rb;
 }
-__device__ __forceinline__ const char *row_at(const PagedRowsParams &r, int kvh, int page, int row) {
-  return (const char *)(r.base + kvh * r.sh) + ((uint64_t)(uint32_t)page * r.page_b16 << 4) + (uint64_t)(uint32_t)row * r.rb;
-}
-template <int D>
+// A workgroup takes kCopyRows new rows of heads, a token's heads one after the other: what it writes lies together.  A row's place comes out of three
+// loads one behind the other; all rows' go together.
+template <int D, bool kPast>
 __global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictParams p, int chunks) {
   constexpr int CPR = D / 8, RPP = kCopyThreads / CPR, N = kCopyRows / RPP;
-  const int kvh = blockIdx.x % p.n_kv_heads, rest = blockIdx.x / p.n_kv_heads, chunk = rest % chunks, seq = rest / chunks;
-  const int32_t *kept = p.kept + ((int64_t)seq * p.n_kv_heads + kvh) * p.n_keep;
+  const int chunk = blockIdx.x % chunks, seq = blockIdx.x / chunks;
   const int c = threadIdx.x % CPR * 16;
-  u32x4_t x[N][2];
-  char *to[N][2];
+  int kvh[N], at[N], of[N], page[N], to_page[N];
 #pragma unroll
   for (int u = 0; u < N; ++u) {
-    const int j = chunk * kCopyRows + u * RPP + threadIdx.x / CPR;
-    const int of = j < p.n_keep ? kept[j] : -1;
-    to[u][0] = to[u][1] = nullptr;
-    if (of < 0) continue;
-    int row, to_row;
-    const int page = page_of(p.from, seq, of, row), to_page = page_of(p.to, seq, j, to_row);
-    if (page < 0 || to_page < 0) continue;
-    x[u][0] = *reinterpret_cast<const u32x4_t *>(row_at(p.k, kvh, page, row) + c);
-    x[u][1] = *reinterpret_cast<const u32x4_t *>(row_at(p.v, kvh, page, row) + c);
-    to[u][0] = (char *)row_at(p.to_k, kvh, to_page, to_row) + c;
-    to[u][1] = (char *)row_at(p.to_v, kvh, to_page, to_row) + c;
+    const uint32_t r = (uint32_t)chunk * kCopyRows + u * RPP + threadIdx.x / CPR;
+    at[u] = (int)fast_div(r, p.heads_div), kvh[u] = (int)r - at[u] * p.n_kv_heads;
+    of[u] = p.kept[((int64_t)seq * p.n_kv_heads + kvh[u]) * p.n_keep + min(at[u], p.n_keep - 1)];
+    if (at[u] >= p.n_keep) of[u] = -1;
+  }
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int i = (int)fast_div((uint32_t)max(of[u], 0), p.from.page_div), to_i = (int)fast_div((uint32_t)at[u], p.to.page_div);
+    page[u] = p.from.table[seq * p.from.stride + min(i, p.from.max_pages - 1)];
+    to_page[u] = p.to.table[seq * p.to.stride + min(to_i, p.to.max_pages - 1)];
+    if (of[u] < 0 || i >= p.from.max_pages || to_i >= p.to.max_pages || page[u] < 0 || page[u] >= p.from.n_pages || to_page[u] < 0 || to_page[u] >= p.to.n_pages)
+      page[u] = -1;  // (not copied)
+    of[u] -= i * p.from.page_rows, at[u] -= to_i * p.to.page_rows;
+  }
+  u32x4_t x[N][2];
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int row = page[u] < 0 ? 0 : of[u];
+    x[u][0] = load_row_piece<kPast>(row_at(p.k, kvh[u], max(page[u], 0), row) + c);
+    x[u][1] = load_row_piece<kPast>(row_at(p.v, kvh[u], max(page[u], 0), row) + c);
   }
 #pragma unroll
   for (int u = 0; u < N; ++u)
-    if (to[u][0]) {
-      *reinterpret_cast<u32x4_t *>(to[u][0]) = x[u][0];
-      *reinterpret_cast<u32x4_t *>(to[u][1]) = x[u][1];
+    if (page[u] >= 0) {
+      store_row_piece<kPast>(row_at(p.to_k, kvh[u], to_page[u], at[u]) + c, x[u][0]);
+      store_row_piece<kPast>(row_at(p.to_v, kvh[u], to_page[u], at[u]) + c, x[u][1]);
     }
 }
 
@@ -72,15 +76,23 @@ __global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictParams p,
 hipError_t launch_evict_pick(const EvictParams &p, hipStream_t stream) {
   const int64_t wgs = (int64_t)p.n_seqs * p.n_kv_heads;
   if (wgs < 1 || wgs > kMaxPickWorkgroups) return hipErrorInvalidValue;
-  evict_pick_kernel<<<(unsigned)wgs, kPickThreads, 0, stream>>>(p);
-  return hipGetLastError();
+  return with_pick_shape(p.cap, [&](auto w, auto e) {
+    evict_pick_kernel<decltype(w)::value, decltype(e)::value><<<(unsigned)wgs, decltype(w)::value * 64, 0, stream>>>(p);
+    return hipGetLastError();
+  });
 }
 hipError_t launch_evict_copy(const EvictParams &p, hipStream_t stream) {
-  const int64_t chunks = (p.n_keep + kCopyRows - 1) / kCopyRows, wgs = (int64_t)p.n_seqs * p.n_kv_heads * chunks;
-  if (wgs < 1 || wgs > kMaxWorkgroups) return hipErrorInvalidValue;
-  if (p.head_dim == 128) evict_copy_kernel<128><<<(unsigned)wgs, kCopyThreads, 0, stream>>>(p, (int)chunks);
-  else evict_copy_kernel<64><<<(unsigned)wgs, kCopyThreads, 0, stream>>>(p, (int)chunks);
-  return hipGetLastError();
+  const int64_t chunks = evict_copy_chunks(p.n_keep, p.cap, p.n_kv_heads), wgs = (int64_t)p.n_seqs * chunks;
+  if (wgs > kMaxWorkgroups) return hipErrorInvalidValue;
+  if (wgs == 0) return hipSuccess;
+  auto launch = [&](auto d, auto past) {
+    evict_copy_kernel<decltype(d)::value, decltype(past)::value><<<(unsigned)wgs, kCopyThreads, 0, stream>>>(p, (int)chunks);
+    return hipGetLastError();
+  };
+  using D128 = std::integral_constant<int, 128>;
+  using D64 = std::integral_constant<int, 64>;
+  if (p.past_caches) return p.head_dim == 128 ? launch(D128{}, std::true_type{}) : launch(D64{}, std::true_type{});
+  return p.head_dim == 128 ? launch(D128{}, std::false_type{}) : launch(D64{}, std::false_type{});
 }
 
 }  // namespace ba
