@@ -55,10 +55,13 @@ void set_table(PagedTableParams *p, const ba_paged_cache *c) {
   p->page_div = make_fast_div((uint32_t)c->page_rows);
 }
 
+constexpr int64_t kWeightsSlots = 4;  // workgroups of the kernel for many rows to a compute unit
+
 // ---- weights of cached keys --------------------------------------------------------------------------------
 struct WeightsPlan {
   int32_t seq0, n_seqs, group_end;
   int32_t prefix_items, own_chunks;
+  int32_t part_tiles, row_parts;  // (see KeyWeightsParams)
   bool many;
   int64_t items;
   PagedGroups groups;
@@ -104,7 +107,21 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
   }
   pl->groups.item0[pl->groups.n] = pl->prefix_items = (int32_t)std::min<int64_t>(items, INT32_MAX);
   pl->own_chunks = (int32_t)(((int64_t)max_len - least_prefix + keys - 1) / keys);
-  pl->items = items + (int64_t)pl->n_seqs * h->n_kv_heads * pl->own_chunks;
+  const int64_t own_items = (int64_t)pl->n_seqs * h->n_kv_heads * pl->own_chunks;
+  // Many rows over keys that do not fill the chip: in up to eight parts of two tiles at least, where the merge (3 us, a tile 0.9) costs less than they save.
+  // us, in one part and in several: 1,024 rows over 2,000 keys 36 / 15, over 500 32 / 12.
+  pl->row_parts = 1;
+  if (pl->many && n_groups == 0 && own_items > 0) {
+    const int64_t tiles = ((int64_t)nq * (h->n_q_heads / h->n_kv_heads) + 31) / 32, parts = std::min<int64_t>({tiles / 2, 8, kWeightsSlots * num_cus() / own_items});
+    if (tiles >= 8 && parts > 1) {
+      pl->part_tiles = (int32_t)((tiles + parts - 1) / parts);
+      pl->row_parts = (int32_t)((tiles + pl->part_tiles - 1) / pl->part_tiles);
+    }
+  }
+  pl->items = items + own_items * pl->row_parts;
+}
+size_t weights_bytes(const WeightsPlan &pl, const ba_heads *h, int32_t max_len) {
+  return pl.part_tiles ? align256((size_t)pl.row_parts * pl.n_seqs * h->n_kv_heads * max_len * 4) : 0;
 }
 
 }  // namespace
@@ -118,7 +135,11 @@ extern "C" {
 
 size_t ba_paged_key_weights_workspace_bytes(const ba_heads *heads, int32_t n_seqs, int32_t q_per_seq, int32_t max_len, int32_t n_groups,
                                             const int32_t *cu_group, const int32_t *prefix_len) {
-  return 0;
+  if (check_paged_sizes(heads, n_seqs, q_per_seq, max_len) != BA_OK || check_groups(n_seqs, max_len, n_groups, cu_group, prefix_len) != BA_OK || n_groups > 0)
+    return 0;
+  WeightsPlan pl;
+  plan_weights(heads, n_seqs, q_per_seq, max_len, 0, nullptr, nullptr, 0, &pl);
+  return weights_bytes(pl, heads, max_len);
 }
 
 int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache, const ba_tensor *q, const float *lse, const float *weights_in,
@@ -147,6 +168,9 @@ int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache,
   do {  // (whether every launch can be made, ahead of the first)
     plan_weights(heads, n_seqs, q_per_seq, max_len, n_groups, cu_group, prefix_len, g, &pl);
     if (pl.items > kMaxWorkgroups) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
+    const size_t need = weights_bytes(pl, heads, max_len);
+    if (need > 0 && (!ws || ((uintptr_t)ws & 255) || ws_bytes < need))
+      return fail(BA_ERR_WORKSPACE, "workspace missing, not 256-byte aligned or smaller than %zu bytes", need);
     if (pl.groups.n > 0 && (int64_t)padded_rows(heads, q_per_seq) * pl.n_seqs > (1 << 30)) return fail(BA_ERR_UNSUPPORTED, "2^30 query rows and more");
     g = pl.group_end;
   } while (g < n_groups);
@@ -177,6 +201,8 @@ int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache,
     p.w_out = weights_out + at;
     p.w_stride = stride_weights;
     p.prefix_items = pl.prefix_items, p.own_chunks = pl.own_chunks;
+    p.part_tiles = pl.part_tiles, p.row_parts = pl.row_parts;
+    p.part = (float *)ws;
     ProfileScope ps(BA_PROFILE_ATTENTION, (hipStream_t)stream);
     hipError_t e;
     if (pl.groups.n <= PagedGroupsSmall::kGroups) {  // (a small table: many large argument blocks in flight hold up the queue)
@@ -190,6 +216,7 @@ int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache,
     } else {
       e = launch_key_weights(p, pl.groups, D, pl.many, (hipStream_t)stream);
     }
+    if (e == hipSuccess && pl.part_tiles) e = launch_key_weights_merge(p, (hipStream_t)stream);
     if (e != hipSuccess) return device_fail(e, "key weights launch");
   } while (g < n_groups);
   return BA_OK;

@@ -291,18 +291,33 @@ size_t plan_bytes(const PagedPlan &pl, const ba_heads *h, int32_t nq) {
   return align256(rows * pl.parts * h->head_dim * 2) + align256(rows * pl.parts * 16);
 }
 
-// The plan of a call over listed pages of `keys` keys at most: as without groups, in parts whose lists fit a workgroup.
-void plan_selected(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t keys, int cus, PagedPlan *pl) {
-  plan_paged(h, n_seqs, nq, keys, 0, nullptr, nullptr, 0, cus, pl);
-  pl->own_chunk = std::min(pl->own_chunk, kSelectedMaxChunk / 64 * 64);
-  pl->parts = pl->own_splits = std::max(1, (keys + pl->own_chunk - 1) / pl->own_chunk);
-  pl->items = (int64_t)n_seqs * h->n_kv_heads * pl->own_row_tiles * pl->own_splits;
+// The plan of a call over listed pages of `keys` keys at most.  Their number is a bound that most sequences reach, so the parts are as many as cost
+// least: rounds of items on the slots, an item as much as its keys and 100 more (see plan_paged), the merge as much as 70 and what it
+// writes and reads.
+void plan_selected(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t page_rows, int32_t keys, int cus, PagedPlan *pl) {
+  memset(pl, 0, sizeof(*pl));
+  const int64_t rows = (int64_t)nq * (h->n_q_heads / h->n_kv_heads), slots = 2 * cus, D = h->head_dim;
+  pl->n_seqs = n_seqs;
+  pl->own_row_tiles = (int32_t)((rows + paged_tile_rows((int)rows) - 1) / paged_tile_rows((int)rows));
+  pl->keys = (int64_t)n_seqs * keys;
+  const int64_t walks = (int64_t)n_seqs * h->n_kv_heads * pl->own_row_tiles, all_rows = (int64_t)n_seqs * h->n_kv_heads * rows;
+  const int32_t most = selected_max_chunk(page_rows);
+  int64_t least_cost = INT64_MAX;
+  for (int64_t parts = 1; parts == 1 || parts <= std::min(256, (keys + 63) / 64); ++parts) {
+    const int64_t chunk = std::max<int64_t>(64, (keys + parts * 64 - 1) / (parts * 64) * 64);
+    if (chunk > most && parts < 256) continue;
+    const int64_t taken = std::min<int64_t>(chunk, most), really = std::max<int64_t>(1, (keys + taken - 1) / taken);
+    const int64_t cost = (walks * really + slots - 1) / slots * (taken + 100) + (really > 1 ? 70 + all_rows * really * (4 * D + 32) / (4 * D * slots) : 0);
+    if (cost < least_cost) least_cost = cost, pl->own_chunk = (int32_t)taken, pl->own_splits = (int32_t)really;
+  }
+  pl->parts = pl->own_splits;
+  pl->items = walks * pl->own_splits;
 }
 int32_t selected_keys(int32_t page_rows, int32_t max_len, int32_t n_select) {
   return (int32_t)std::min<int64_t>((int64_t)n_select * page_rows, max_len);
 }
 int32_t check_selected_plan(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t page_rows, int32_t max_len, int32_t n_select, PagedPlan *pl, size_t *bytes) {
-  plan_selected(h, n_seqs, nq, selected_keys(page_rows, max_len, n_select), num_cus(), pl);
+  plan_selected(h, n_seqs, nq, page_rows, selected_keys(page_rows, max_len, n_select), num_cus(), pl);
   if (pl->items > kMaxWorkgroups) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
   *bytes = plan_bytes(*pl, h, nq);
   if (*bytes > 0 && ((int64_t)n_seqs * nq * h->n_q_heads + kPagedMergeRows - 1) / kPagedMergeRows > kMaxWorkgroups)

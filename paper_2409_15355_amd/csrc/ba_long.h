@@ -38,7 +38,11 @@ struct KeyWeightsParams {
   float *w_out;
   int64_t w_stride;
   int32_t prefix_items, own_chunks;
+  // many rows without groups, in parts: tiles of 32 rows of a part (0: one part), its sums [part][sequence][KV head][cap]
+  int32_t part_tiles, row_parts;
+  float *part;
 };
+hipError_t launch_key_weights_merge(const KeyWeightsParams &p, hipStream_t stream);
 constexpr int kWeightsFewKeys = 128, kWeightsManyKeys = 256;  // keys of a work item of the kernels for few and for many rows a sequence
 template <typename Groups>
 hipError_t launch_key_weights(const KeyWeightsParams &p, const Groups &g, int head_dim, bool many, hipStream_t stream);

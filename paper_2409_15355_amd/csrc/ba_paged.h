@@ -109,7 +109,12 @@ struct PagedSelection {
   int32_t n, max_pages;
   int32_t keys;          // of the listed pages at most: min(n * page_rows, cap)
 };
-constexpr int kSelectedMaxChunk = 1152;  // keys of a work item at most: its part of the list lies in LDS as well
+// Keys of a work item at most: its part of the list lies in LDS as well.
+constexpr int kSelectedMaxPages = 1154;
+inline int32_t selected_max_chunk(int32_t page_rows) {
+  const int64_t keys = (int64_t)(kSelectedMaxPages - 2) * page_rows / 64 * 64;
+  return keys < 4096 ? (int32_t)keys : 4096;
+}
 
 template <typename Groups>
 hipError_t launch_paged_attention(const PagedAttnParams &p, const Groups &g, int head_dim, hipStream_t stream);

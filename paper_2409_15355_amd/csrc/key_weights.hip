@@ -28,10 +28,12 @@ struct WeightsItem {
   int seq0, n_mem;    // the sequences whose rows it takes
   int kvh;
   int key0, key_end;  // keys from key0 on, below key_end
+  int part;
 };
 template <int KEYS, typename Groups>
 __device__ __forceinline__ WeightsItem weights_item(const KeyWeightsParams &p, const Groups &groups) {
   WeightsItem it;
+  it.part = 0;
   if ((int)blockIdx.x < p.prefix_items) {
     const int id = (int)blockIdx.x;
     int lo = 0, hi = groups.n;
@@ -50,7 +52,9 @@ __device__ __forceinline__ WeightsItem weights_item(const KeyWeightsParams &p, c
     it.kvh = rel % p.n_kv_heads;
     rel /= p.n_kv_heads;
     const int chunk = rel % p.own_chunks;
-    it.seq0 = rel / p.own_chunks;
+    rel /= p.own_chunks;
+    it.seq0 = rel % p.n_seqs;
+    it.part = rel / p.n_seqs;
     it.n_mem = 1;
     int lo = 0, hi = groups.n;  // its group
     while (hi - lo > 1) {
@@ -266,7 +270,9 @@ __global__ __launch_bounds__(kWThreads, kEven ? 4 : 3) void key_weights_many_ker
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 31, hf = lane >> 5;
   const int item_last = min(item.key_end, item.key0 + kWeightsManyKeys) - 1;
-  const int per_seq = (p.rows + 31) / 32, n_tiles = item.n_mem * per_seq;  // tiles of a sequence (the last one may end early), of all
+  const int per_seq = (p.rows + 31) / 32;  // tiles of a sequence (the last one may end early)
+  const int tile_first = item.part * p.part_tiles;
+  const int n_tiles = p.part_tiles ? min(p.part_tiles, per_seq - tile_first) : item.n_mem * per_seq;
 
   // row r of sequence j: its token, its head
   auto place = [&](int j, int r, int64_t &tok, int &head) __attribute__((always_inline)) {
@@ -275,8 +281,10 @@ __global__ __launch_bounds__(kWThreads, kEven ? 4 : 3) void key_weights_many_ker
     head = item.kvh * p.group + r - i * p.group;
     return i;
   };
-  const char *from_even[OPS];
+  // (kEven: a tile's first row, the same in all lanes, and how far behind it a lane's piece lies)
   const int64_t tile_step = 32 / p.group * p.q_st * 2;
+  const char *from_even = (const char *)(p.q + (int64_t)item.seq0 * p.nq * p.q_st + (int64_t)item.kvh * p.group * p.q_sh) + tile_first * tile_step;
+  uint32_t behind[OPS];
   // tile `at` of sequence j: rows at * 32 + (0 .. 31) of it, the last one again behind it (and masked)
   auto where = [&](int u, int j, int at) __attribute__((always_inline)) {
     const int row = (wave * OPS + u) * RPI + lane / CPR;
@@ -287,23 +295,26 @@ __global__ __launch_bounds__(kWThreads, kEven ? 4 : 3) void key_weights_many_ker
   };
   if constexpr (kEven)
 #pragma unroll
-    for (int u = 0; u < OPS; ++u) from_even[u] = where(u, 0, 0);
-  int j_in = 0, at_in = 0;  // the tile that is asked for next
+    for (int u = 0; u < OPS; ++u) {
+      const int row = (wave * OPS + u) * RPI + lane / CPR, i = (int)fast_div((uint32_t)row, p.group_div);
+      behind[u] = (uint32_t)(i * p.q_st + (row - i * p.group) * p.q_sh) * 2 + (((lane % CPR) ^ ((row / LPR) & (CPR - 1))) << 4);
+    }
+  int j_in = 0, at_in = tile_first;  // the tile that is asked for next
   auto issue = [&](uint32_t to) __attribute__((always_inline)) {
 #pragma unroll
     for (int u = 0; u < OPS; ++u) {
-      const char *from;
-      if constexpr (kEven) from = from_even[u], from_even[u] += tile_step;
-      else from = where(u, j_in, at_in);
-      lds_dma16_lane(from, (uint32_t)(uintptr_t)smem + to + (wave * OPS + u) * 1024);
+      const uint32_t lds = (uint32_t)(uintptr_t)smem + to + (wave * OPS + u) * 1024;
+      if constexpr (kEven) lds_dma16(from_even, behind[u], lds);
+      else lds_dma16_lane(where(u, j_in, at_in), lds);
     }
+    if constexpr (kEven) from_even += tile_step;
     if (++at_in == per_seq) at_in = 0, ++j_in;
   };
   // what the rows of the next kNoted tiles have beside them: -lse in log2 units, the key that each ends before, whether a tile's rows see all keys
   auto note = [&](int tile0) __attribute__((always_inline)) {
 #pragma unroll 1
     for (int n = threadIdx.x; n < min(kNoted, n_tiles - tile0) * 32; n += kWThreads) {
-      const int tile = tile0 + n / 32, j = tile / per_seq, r = (tile - j * per_seq) * 32 + n % 32;
+      const int tile = tile_first + tile0 + n / 32, j = tile / per_seq, r = (tile - j * per_seq) * 32 + n % 32;
       int64_t tok;
       int head;
       const int i = place(j, min(r, p.rows - 1), tok, head);
@@ -319,13 +330,15 @@ __global__ __launch_bounds__(kWThreads, kEven ? 4 : 3) void key_weights_many_ker
   issue(0);
   WaveKeys<D, NT> k;
   k.load(p, item, item.key0 + wave * NT * 32, lane);
+  const int my_key = item.key0 + wave * NT * 32 + col;
+  auto key = [&](int t) __attribute__((always_inline)) { return my_key + t * 32; };
   note(0);
   if (n_tiles > 1) issue(TB);
   lds_wait();
 
   const uint32_t q_rd = col * ROWB + ((hf ^ ((col / LPR) & (CPR - 1))) << 4);  // (chunk pairs kk on are an exclusive or away)
   float sum[NT] = {};
-  int j = 0, at = 0;
+  int j = 0, at = tile_first;
   uint32_t buffer = 0;
 #pragma unroll 1
   for (int tile = 0; tile < n_tiles; ++tile) {
@@ -365,7 +378,7 @@ __global__ __launch_bounds__(kWThreads, kEven ? 4 : 3) void key_weights_many_ker
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             e[c] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i * 4 + c], p.scale_log2e, nl[c]));
-            if constexpr (decltype(masked)::value) e[c] = k.key[t] < lim[c] ? e[c] : 0.f;
+            if constexpr (decltype(masked)::value) e[c] = key(t) < lim[c] ? e[c] : 0.f;
           }
           sum[t] += (e[0] + e[1]) + (e[2] + e[3]);
         }
@@ -374,28 +387,52 @@ __global__ __launch_bounds__(kWThreads, kEven ? 4 : 3) void key_weights_many_ker
     };
     if (__builtin_amdgcn_readfirstlane(all_at[tile % kNoted]) != 0) sums(std::false_type{});
     else sums(std::true_type{});
-    if (++at == per_seq) {
+    if (++at == per_seq && !p.part_tiles) {
       const int len = clamped_length(p.seq_len, p.cap, item.seq0 + j);
       const int64_t list = ((int64_t)(item.seq0 + j) * p.n_kv_heads + item.kvh) * p.w_stride;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
         const float total = sum[t] + other_half(sum[t]);
         sum[t] = 0.f;
-        if (hf == 0 && k.key[t] <= item_last && k.key[t] < len) {
-          const float old = p.w_in && k.key[t] < len - p.nq ? p.w_in[list + k.key[t]] : 0.f;
-          p.w_out[list + k.key[t]] = __builtin_fmaf(p.decay, old, k.there[t] ? total : 0.f);
+        if (hf == 0 && key(t) <= item_last && key(t) < len) {
+          const float old = p.w_in && key(t) < len - p.nq ? p.w_in[list + key(t)] : 0.f;
+          p.w_out[list + key(t)] = __builtin_fmaf(p.decay, old, k.there[t] ? total : 0.f);
         }
       }
       at = 0, ++j;
     }
   }
+  if (p.part_tiles) {
+    const int64_t list = (((int64_t)item.part * p.n_seqs + item.seq0) * p.n_kv_heads + item.kvh) * p.cap;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const float total = sum[t] + other_half(sum[t]);
+      if (hf == 0 && key(t) <= item_last) p.part[list + key(t)] = k.there[t] ? total : 0.f;
+    }
+  }
+}
+
+// A sequence's parts, added up in their order.
+__global__ __launch_bounds__(kWThreads) void key_weights_merge_kernel(KeyWeightsParams p, int chunks) {
+  const int list = blockIdx.x / chunks, seq = list / p.n_kv_heads, key = blockIdx.x % chunks * kWThreads + threadIdx.x;
+  const int len = clamped_length(p.seq_len, p.cap, seq);
+  if (key >= len) return;
+  const int64_t at = (int64_t)list * p.w_stride + key, step = (int64_t)p.n_seqs * p.n_kv_heads * p.cap;
+  const float old = p.w_in && key < len - p.nq ? p.w_in[at] : 0.f;
+  const float *from = p.part + (int64_t)list * p.cap + key;
+  float sum = 0.f;
+#pragma unroll 8
+  for (int i = 0; i < p.row_parts; ++i) sum += from[i * step];
+  p.w_out[at] = __builtin_fmaf(p.decay, old, sum);
 }
 
 template <int D, typename Groups>
 hipError_t launch_d(const KeyWeightsParams &p, const Groups &g, bool many, hipStream_t stream) {
-  const int64_t items = p.prefix_items + (int64_t)p.n_seqs * p.n_kv_heads * p.own_chunks;
+  const int64_t items = p.prefix_items + (int64_t)p.n_seqs * p.n_kv_heads * p.own_chunks * p.row_parts;
   if (items < 1 || items > kMaxWorkgroups) return hipErrorInvalidValue;
-  if (many && p.rows % 32 == 0 && 32 % p.group == 0) key_weights_many_kernel<D, true, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
+  // (a tile's rows in 32 bits behind the first)
+  const bool near = (32 / p.group + 1) * p.q_st + p.group * p.q_sh < ((int64_t)1 << 30);
+  if (many && p.rows % 32 == 0 && 32 % p.group == 0 && near) key_weights_many_kernel<D, true, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
   else if (many) key_weights_many_kernel<D, false, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
   else {
     auto launch = [&](auto four, auto even) {
@@ -413,6 +450,12 @@ hipError_t launch_d(const KeyWeightsParams &p, const Groups &g, bool many, hipSt
 template <typename Groups>
 hipError_t launch_key_weights(const KeyWeightsParams &p, const Groups &g, int head_dim, bool many, hipStream_t stream) {
   return head_dim == 128 ? launch_d<128>(p, g, many, stream) : launch_d<64>(p, g, many, stream);
+}
+hipError_t launch_key_weights_merge(const KeyWeightsParams &p, hipStream_t stream) {
+  const int64_t chunks = ((int64_t)p.cap + kWThreads - 1) / kWThreads, wgs = (int64_t)p.n_seqs * p.n_kv_heads * chunks;
+  if (wgs < 1 || wgs > kMaxWorkgroups) return hipErrorInvalidValue;
+  key_weights_merge_kernel<<<(unsigned)wgs, kWThreads, 0, stream>>>(p, (int)chunks);
+  return hipGetLastError();
 }
 template hipError_t launch_key_weights(const KeyWeightsParams &, const PagedGroups &, int, bool, hipStream_t);
 template hipError_t launch_key_weights(const KeyWeightsParams &, const PagedGroupsSmall &, int, bool, hipStream_t);

@@ -949,13 +949,13 @@ __global__ __launch_bounds__(kMergeThreads) void paged_merge_kernel(PagedAttnPar
 // LDS behind the tiles: entries of the page table for `pages` pages
 template <int D, bool kAligned, typename Groups>
 struct AttnKernel {
-  static constexpr int kMaxChunk = kPagedMaxChunk;
+  static constexpr int kMaxPages = kPagedMaxChunk + 2;
   static constexpr size_t table_bytes(int pages) { return (size_t)pages * 4; }
   static constexpr auto *kernel = &paged_attn_kernel<D, kAligned, Groups>;
 };
 template <int D, bool kAligned>
 struct AttnKernel<D, kAligned, PagedSelection> {
-  static constexpr int kMaxChunk = kSelectedMaxChunk;
+  static constexpr int kMaxPages = kSelectedMaxPages;
   static constexpr size_t table_bytes(int pages) { return (size_t)pages * 8 + kPWaves * 4; }
   static constexpr auto *kernel = &paged_selected_kernel<D, kAligned>;
 };
@@ -968,7 +968,7 @@ hipError_t launch_attn_a(const PagedAttnParams &p, const Groups &g, unsigned ite
   if (e != hipSuccess) return e;
   if (dev >= 16 || !told[dev].load(std::memory_order_acquire)) {
     e = hipFuncSetAttribute(reinterpret_cast<const void *>(AttnKernel<D, kAligned, Groups>::kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                            kTilesB + (int)AttnKernel<D, kAligned, Groups>::table_bytes(AttnKernel<D, kAligned, Groups>::kMaxChunk + 2));
+                            kTilesB + (int)AttnKernel<D, kAligned, Groups>::table_bytes(AttnKernel<D, kAligned, Groups>::kMaxPages));
     if (e != hipSuccess) return e;
     if (dev < 16) told[dev].store(true, std::memory_order_release);
   }
@@ -980,9 +980,9 @@ hipError_t launch_attn_d(const PagedAttnParams &p, const Groups &g, hipStream_t 
   const int64_t items = p.prefix_items + (int64_t)p.n_seqs * p.n_kv_heads * p.own_row_tiles * p.own_splits;
   const int32_t chunk = std::max(p.chunk, p.own_chunk);
   using Kernel = AttnKernel<D, true, Groups>;
-  if (items < 1 || items > kMaxWorkgroups || chunk > Kernel::kMaxChunk) return hipErrorInvalidValue;
+  if (items < 1 || items > kMaxWorkgroups || chunk / p.page_rows + 2 > Kernel::kMaxPages) return hipErrorInvalidValue;
   const size_t lds = kTilesB + Kernel::table_bytes(chunk / p.page_rows + 2);  // (a range may begin and end inside a page)
-  static_assert(2 * (kTilesB + Kernel::table_bytes(Kernel::kMaxChunk + 2)) <= 160 * 1024, "two workgroups a compute unit");
+  static_assert(2 * (kTilesB + Kernel::table_bytes(Kernel::kMaxPages)) <= 160 * 1024, "two workgroups a compute unit");
   return p.page_rows % 16 == 0 ? launch_attn_a<D, true>(p, g, (unsigned)items, lds, stream) : launch_attn_a<D, false>(p, g, (unsigned)items, lds, stream);
 }
 template <int D, int kWays, typename Groups>

@@ -123,7 +123,7 @@ def weights64(pool, q, lse, nq, scale, holes=()):
 # ---- weights of cached keys -----------------------------------------------------------------------------------------
 @pytest.mark.parametrize("hq,hkv,d,rows,lens,nq", [
     (4, 4, 64, 16, [1], 1), (32, 8, 128, 16, [2064], 1), (8, 2, 64, 7, [0, 1, 130, 129, 33], 1), (6, 2, 128, 64, [300, 5], 1), (16, 2, 64, 32, [257, 100, 3], 1),
-    (8, 2, 128, 16, [70, 3, 0, 40], 5), (5, 1, 64, 1, [90, 31], 3), (8, 8, 64, 128, [200, 130], 33), (32, 8, 128, 16, [400], 64), (4, 1, 128, 100, [513, 1], 16)])
+    (8, 2, 128, 16, [70, 3, 0, 40], 5), (5, 1, 64, 1, [90, 31], 3), (8, 8, 64, 128, [200, 130], 33), (32, 8, 128, 16, [400], 64), (4, 1, 128, 100, [513, 1], 16), (16, 2, 128, 16, [300, 150], 100), (12, 2, 64, 16, [290], 150)])
 @pytest.mark.parametrize("decay", [0.0, 1.0, 0.75])
 def test_key_weights(ba, hq, hkv, d, rows, lens, nq, decay):
     import torch
