@@ -289,12 +289,15 @@ int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const
   p.heads_div = make_fast_div((uint32_t)hkv);
   // (rows go by once, and are read next after all other layers' have gone by, too)
   p.past_caches = lists * std::min(n_keep, max_len) * D * 8 > kCacheBytes * 3 / 4;
+  // us, eight lists of 2,064 tokens, in one launch and in two: 64 rows of 128 kept 8.2 / 9.3, 128 8.8 / 10.1, 256 9.9 / 10.5, 512 12.9 / 10.9; 512 lists of
+  // up to 8,000, 1,024 kept 123 / 117.
+  p.copies = std::min(n_keep, max_len) * (int64_t)D <= 256 * 128;
   hipError_t e;
   {
     ProfileScope ps(BA_PROFILE_COMBINE, stream);
     e = launch_evict_pick(p, stream);
   }
-  if (e == hipSuccess) {
+  if (e == hipSuccess && !p.copies) {
     ProfileScope ps(BA_PROFILE_REENCODE, stream);
     e = launch_evict_copy(p, stream);
   }
@@ -374,6 +377,11 @@ int32_t ba_page_select(const ba_heads *heads, const ba_paged_cache *cache, const
   p.score_stride = ((int64_t)max_len + cache->page_rows - 1) / cache->page_rows;
   if ((n_seqs * ((p.score_stride + kScorePages - 1) / kScorePages) + 8) * hkv > kMaxWorkgroups) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
   hipError_t e = hipSuccess;
+  if (p.score_stride <= kSelectOneLaunch) {
+    ProfileScope ps(BA_PROFILE_ATTENTION, stream);
+    e = launch_page_select(p, D, stream);
+    return e == hipSuccess ? BA_OK : device_fail(e, "page selection launch");
+  }
   if (max_len > 0) {
     ProfileScope ps(BA_PROFILE_ATTENTION, stream);
     e = launch_page_scores(p, D, stream);

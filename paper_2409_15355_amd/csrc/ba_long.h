@@ -62,6 +62,7 @@ struct EvictParams {
   PagedTableParams from, to;
   FastDiv heads_div;       // by n_kv_heads
   int32_t past_caches;     // rows are copied past the caches
+  int32_t copies;          // a list's workgroup copies its rows
 };
 constexpr int64_t kMaxPickWorkgroups = 0xffffffffll / 1024;
 constexpr int kEvictCopyRows = 64;  // rows of heads that a workgroup copies
@@ -98,6 +99,10 @@ struct PageSelectParams {
   int64_t score_stride;
 };
 hipError_t launch_page_scores(const PageSelectParams &p, int head_dim, hipStream_t stream);
+// Pages of a sequence up to which one launch does both.  us, eight lists, in one launch (4 waves / 16) and in two: 63 pages 5.7 / 6.7 and 8.3, 500 pages
+// 10.0 / 9.4 and 9.5, 1,000 pages 15 / 13 and 9.8; 512 lists of up to 1,000 pages 24.7 / 26 and 21.7.
+constexpr int kSelectOneLaunch = 256;
+hipError_t launch_page_select(const PageSelectParams &p, int head_dim, hipStream_t stream);
 hipError_t launch_page_pick(const PageSelectParams &p, hipStream_t stream);
 
 }  // namespace ba

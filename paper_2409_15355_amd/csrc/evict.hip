@@ -8,45 +8,17 @@
 namespace ba {
 namespace {
 
-template <int W, int E>
-__global__ __launch_bounds__(W * 64) void evict_pick_kernel(EvictParams p) {
-  __shared__ PickLds<W> lds;
-  const int kvh = blockIdx.x % p.n_kv_heads, seq = blockIdx.x / p.n_kv_heads;
-  const int len = max(0, min(p.seq_len[seq], p.cap));
-  const int64_t list = (int64_t)seq * p.n_kv_heads + kvh;
-  const float *w = p.weights + list * p.w_stride;
-  int32_t *kept = p.kept + list * p.n_keep;
-  float *w_out = p.w_out ? p.w_out + list * p.w_out_stride : nullptr;
-  const int last0 = len - p.n_last;
-  const int n = pick_largest<W, E>(
-      lds, len, p.n_keep, [&](int i) { return w[i]; }, [&](int i, float x) { return i < p.n_first || i >= last0 ? kPickAlways : pick_key(x); },
-      [&](int at, int i, float x) {
-        kept[at] = i;
-        if (w_out) w_out[at] = x;
-      });
-  for (int j = n + threadIdx.x; j < p.n_keep; j += W * 64) kept[j] = -1;
-  if (kvh == 0 && threadIdx.x == 0 && p.len_out) p.len_out[seq] = n;
-}
-
-constexpr int kCopyThreads = 256, kCopyRows = kEvictCopyRows;
 __device__ __forceinline__ char *row_at(const PagedRowsParams &r, int kvh, int page, int row) {
   return (char *)(r.base + kvh * r.sh) + ((uint64_t)(uint32_t)page * r.page_b16 << 4) + (uint64_t)(uint32_t)row * r.rb;
 }
-// A workgroup takes kCopyRows new rows of heads, a token's heads one after the other: what it writes lies together.  A row's place comes out of three
-// loads one behind the other; all rows' go together.
-template <int D, bool kPast>
-__global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictParams p, int chunks) {
-  constexpr int CPR = D / 8, RPP = kCopyThreads / CPR, N = kCopyRows / RPP;
-  const int chunk = blockIdx.x % chunks, seq = blockIdx.x / chunks;
-  const int c = threadIdx.x % CPR * 16;
+// Rows of one sequence by what `which` says of the n-th: its head, its place among the kept ones, its token (-1: none).  A row's place comes out of three
+// loads one behind the other; N rows' go together.
+template <int D, int N, bool kPast, typename Which>
+__device__ __forceinline__ void copy_rows(const EvictParams &p, int seq, int first, int apart, Which &&which) {
+  const int c = threadIdx.x % (D / 8) * 16;
   int kvh[N], at[N], of[N], page[N], to_page[N];
 #pragma unroll
-  for (int u = 0; u < N; ++u) {
-    const uint32_t r = (uint32_t)chunk * kCopyRows + u * RPP + threadIdx.x / CPR;
-    at[u] = (int)fast_div(r, p.heads_div), kvh[u] = (int)r - at[u] * p.n_kv_heads;
-    of[u] = p.kept[((int64_t)seq * p.n_kv_heads + kvh[u]) * p.n_keep + min(at[u], p.n_keep - 1)];
-    if (at[u] >= p.n_keep) of[u] = -1;
-  }
+  for (int u = 0; u < N; ++u) which(first + u * apart, kvh[u], at[u], of[u]);
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     const int i = (int)fast_div((uint32_t)max(of[u], 0), p.from.page_div), to_i = (int)fast_div((uint32_t)at[u], p.to.page_div);
@@ -71,14 +43,64 @@ __global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictParams p,
     }
 }
 
+// kRows: head_dim, and the workgroup copies its list's rows, too; 0: it does not.
+template <int W, int E, int kRows>
+__global__ __launch_bounds__(W * 64) void evict_pick_kernel(EvictParams p) {
+  __shared__ PickLds<W> lds;
+  const int kvh = blockIdx.x % p.n_kv_heads, seq = blockIdx.x / p.n_kv_heads;
+  const int len = max(0, min(p.seq_len[seq], p.cap));
+  const int64_t list = (int64_t)seq * p.n_kv_heads + kvh;
+  const float *w = p.weights + list * p.w_stride;
+  int32_t *kept = p.kept + list * p.n_keep;
+  float *w_out = p.w_out ? p.w_out + list * p.w_out_stride : nullptr;
+  const int last0 = len - p.n_last;
+  const int n = pick_largest<W, E>(
+      lds, len, p.n_keep, [&](int i) { return w[i]; }, [&](int i, float x) { return i < p.n_first || i >= last0 ? kPickAlways : pick_key(x); },
+      [&](int at, int i, float x) {
+        kept[at] = i;
+        if (w_out) w_out[at] = x;
+      });
+  for (int j = n + threadIdx.x; j < p.n_keep; j += W * 64) kept[j] = -1;
+  if (kvh == 0 && threadIdx.x == 0 && p.len_out) p.len_out[seq] = n;
+  if constexpr (kRows > 0) {
+    constexpr int RPP = W * 64 / (kRows / 8), N = 4;  // rows of a pass of the threads, passes together
+    __syncthreads();
+#pragma unroll 1
+    for (int j0 = 0; j0 < n; j0 += N * RPP)
+      copy_rows<kRows, N, false>(p, seq, j0 + threadIdx.x / (kRows / 8), RPP, [&](int j, int &head, int &at, int &of) {
+        head = kvh, at = min(j, n - 1);
+        of = kept[at];
+        if (j >= n) of = -1;
+      });
+  }
+}
+
+// The copies apart from the lists: a workgroup takes kCopyRows new rows of heads, a token's heads one after the other, so what it writes lies together.
+constexpr int kCopyThreads = 256, kCopyRows = kEvictCopyRows;
+template <int D, bool kPast>
+__global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictParams p, int chunks) {
+  constexpr int RPP = kCopyThreads / (D / 8);
+  const int chunk = blockIdx.x % chunks, seq = blockIdx.x / chunks;
+  copy_rows<D, kCopyRows / RPP, kPast>(p, seq, chunk * kCopyRows + threadIdx.x / (D / 8), RPP, [&](int r, int &head, int &at, int &of) {
+    at = (int)fast_div((uint32_t)r, p.heads_div), head = r - at * p.n_kv_heads;
+    of = p.kept[((int64_t)seq * p.n_kv_heads + head) * p.n_keep + min(at, p.n_keep - 1)];
+    if (at >= p.n_keep) of = -1;
+  });
+}
+
 }  // namespace
 
 hipError_t launch_evict_pick(const EvictParams &p, hipStream_t stream) {
   const int64_t wgs = (int64_t)p.n_seqs * p.n_kv_heads;
   if (wgs < 1 || wgs > kMaxPickWorkgroups) return hipErrorInvalidValue;
   return with_pick_shape(p.cap, [&](auto w, auto e) {
-    evict_pick_kernel<decltype(w)::value, decltype(e)::value><<<(unsigned)wgs, decltype(w)::value * 64, 0, stream>>>(p);
-    return hipGetLastError();
+    auto launch = [&](auto rows) {
+      evict_pick_kernel<decltype(w)::value, decltype(e)::value, decltype(rows)::value><<<(unsigned)wgs, decltype(w)::value * 64, 0, stream>>>(p);
+      return hipGetLastError();
+    };
+    using std::integral_constant;
+    if (!p.copies) return launch(integral_constant<int, 0>{});
+    return p.head_dim == 128 ? launch(integral_constant<int, 128>{}) : launch(integral_constant<int, 64>{});
   });
 }
 hipError_t launch_evict_copy(const EvictParams &p, hipStream_t stream) {

@@ -229,104 +229,117 @@ typedef __attribute__((address_space(3))) int32_t lds_i;
 // one of 2,000 pages 4.1.  The same: 32 pages to a product (lanes that take 32 bytes a row); fewer workgroups that walk on, the next pages' codes ahead.
 constexpr int kScoreThreads = 256, kScoreRows = 16;
 static_assert(kScorePages == kScoreThreads / 64 * 32, "32 pages a wave");
+// A tile of query rows in 8 bits into LDS.
+template <int D, int kThreads>
+__device__ __forceinline__ void stage_queries(const PageSelectParams &p, int seq, int kvh, int row0, lds_char *smem, lds_i *exps) {
+  constexpr int CPR = D / 8, RPP = kThreads / CPR, ROWB = 2 * D + 16;  // (off the last row's banks)
+  const int n_rows = p.nq * p.group;
+#pragma unroll 1
+  for (int r = threadIdx.x / CPR; r < kScoreRows; r += RPP) {  // (the last row more than once changes nothing)
+    const int of = min(row0 + r, n_rows - 1), i = (int)fast_div((uint32_t)of, p.group_div), c = threadIdx.x % CPR;
+    const u32x4_t x = *reinterpret_cast<const u32x4_t *>(p.q + ((int64_t)seq * p.nq + i) * p.q_st + (kvh * p.group + of - i * p.group) * p.q_sh + c * 8);
+    float f[8], top = 0.f;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+      f[d] = d & 1 ? bf16_hi(x[d / 2]) : bf16_lo(x[d / 2]);
+      f[d] = f[d] != f[d] ? 0.f : f[d];
+      top = fmaxf(top, fabsf(f[d]));
+    }
+    const int e = bound_exponent(max_over_lanes<CPR>(top));
+    u32x2_t up = {0, 0}, down = {0, 0};
+#pragma unroll
+    for (int d = 0; d < 8; ++d) {
+      const int code = clamp_code(__builtin_rintf(__builtin_ldexpf(f[d], -e)));
+      up[d / 4] |= (uint32_t)(max(code, 0) & 0xff) << (d % 4 * 8);
+      down[d / 4] |= (uint32_t)(min(code, 0) & 0xff) << (d % 4 * 8);
+    }
+    *(lds_u32x2 *)(smem + r * ROWB + c * 8) = up;
+    *(lds_u32x2 *)(smem + r * ROWB + D + c * 8) = down;
+    if (c == 0) exps[r] = e;
+  }
+}
+// Pages of a wave, 16 to a lane's `col`: their codes, and their scores for a tile of query rows.
+template <int D>
+struct WavePages {
+  static constexpr int K2 = 2 * D, CH = K2 / 64, ROWB = K2 + 16;
+  int e[2];
+  bool there[2];
+  i32x4_t codes[2][CH];
+  __device__ __forceinline__ void load(const PageSelectParams &p, int seq, int kvh, int first, int held, int lane) {
+    int page[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) page[g] = p.pages.table[seq * p.pages.stride + min(first + g * 16 + (lane & 15), held - 1)];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      there[g] = page[g] >= 0 && page[g] < p.pages.n_pages;
+      const int64_t where = (int64_t)(there[g] ? page[g] : 0) * p.n_kv_heads + kvh;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) codes[g][i] = *reinterpret_cast<const i32x4_t *>(p.codes + where * K2 + i * 64 + (lane >> 4) * 16);
+      e[g] = p.exps[where];
+    }
+  }
+  __device__ __forceinline__ void score(lds_char *smem, lds_i *exps, int lane, float (&best)[2]) const {
+    i32x4_t s[2] = {};
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const i32x4_t qc = *(lds_i32x4 *)(smem + (lane & 15) * ROWB + i * 64 + (lane >> 4) * 16);
+#pragma unroll
+      for (int g = 0; g < 2; ++g) s[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qc, codes[g][i], s[g], 0, 0, 0);
+    }
+    const i32x4_t qe = *(lds_i32x4 *)(exps + (lane >> 4) * 4);
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) best[g] = fmaxf(best[g], __builtin_ldexpf((float)s[g][v], qe[v]));
+  }
+  // the largest of all rows, in the page's own units; -infinity: it is not there
+  __device__ __forceinline__ float result(int g, float best) const {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(best), __float_as_uint(best), false, false);
+    best = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    best = fmaxf(best, other_half(best));
+    return there[g] ? __builtin_ldexpf(best, e[g]) : -INFINITY;
+  }
+};
 template <int D>
 __global__ __launch_bounds__(kScoreThreads) void page_scores_kernel(PageSelectParams p, int chunks) {
-  constexpr int K2 = 2 * D, CH = K2 / 64, CPR = D / 8, RPP = kScoreThreads / CPR;
-  constexpr int ROWB = K2 + 16;  // (off the last row's banks)
-  __shared__ __attribute__((aligned(16))) char smem_generic[kScoreRows * ROWB + kScoreRows * 4];
+  __shared__ __attribute__((aligned(16))) char smem_generic[kScoreRows * (2 * D + 16) + kScoreRows * 4];
   lds_char *const smem = (lds_char *)smem_generic;
-  lds_i *const exps = (lds_i *)(smem + kScoreRows * ROWB);
+  lds_i *const exps = (lds_i *)(smem + kScoreRows * (2 * D + 16));
   // The heads of a sequence's pages one after the other on one XCD (ids go round the eight): the exponents of a page are one piece of memory.
   const int kvh = blockIdx.x / 8 % p.n_kv_heads, unit = blockIdx.x / 8 / p.n_kv_heads * 8 + blockIdx.x % 8, seq = unit / chunks;
   const int first = (unit + seq) % chunks * kScorePages;  // (turned on from sequence to sequence, so that no XCD gets all the beginnings)
   if (seq >= p.n_seqs) return;
-  const int len = max(0, min(p.seq_len[seq], p.cap));
-  const int held = pages_held(p.pages, len);
+  const int len = max(0, min(p.seq_len[seq], p.cap)), held = pages_held(p.pages, len);
   if (first >= held) return;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
-  int at[2], page[2], page_e[2];
-  bool there[2];
-  i32x4_t codes[2][CH];
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    at[g] = first + wave * 32 + g * 16 + col;
-    page[g] = p.pages.table[seq * p.pages.stride + min(at[g], held - 1)];
-  }
-#pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    there[g] = page[g] >= 0 && page[g] < p.pages.n_pages;
-    const int64_t where = (int64_t)(there[g] ? page[g] : 0) * p.n_kv_heads + kvh;
-#pragma unroll
-    for (int i = 0; i < CH; ++i) codes[g][i] = *reinterpret_cast<const i32x4_t *>(p.codes + where * K2 + i * 64 + quad * 16);
-    page_e[g] = p.exps[where];
-  }
-  const int n_rows = p.nq * p.group;
+  const int lane = threadIdx.x & 63, mine = first + (threadIdx.x >> 6) * 32;
+  WavePages<D> pages;
+  pages.load(p, seq, kvh, mine, held, lane);
   float best[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
-  for (int row0 = 0; row0 < n_rows; row0 += kScoreRows) {
+  for (int row0 = 0; row0 < p.nq * p.group; row0 += kScoreRows) {
     if (row0 > 0) __syncthreads();
-#pragma unroll 1
-    for (int r = threadIdx.x / CPR; r < kScoreRows; r += RPP) {  // (the last row more than once changes nothing)
-      const int of = min(row0 + r, n_rows - 1), i = (int)fast_div((uint32_t)of, p.group_div), c = threadIdx.x % CPR;
-      const u32x4_t x = *reinterpret_cast<const u32x4_t *>(p.q + ((int64_t)seq * p.nq + i) * p.q_st + (kvh * p.group + of - i * p.group) * p.q_sh + c * 8);
-      float f[8], top = 0.f;
-#pragma unroll
-      for (int d = 0; d < 8; ++d) {
-        f[d] = d & 1 ? bf16_hi(x[d / 2]) : bf16_lo(x[d / 2]);
-        f[d] = f[d] != f[d] ? 0.f : f[d];
-        top = fmaxf(top, fabsf(f[d]));
-      }
-      const int e = bound_exponent(max_over_lanes<CPR>(top));
-      u32x2_t up = {0, 0}, down = {0, 0};
-#pragma unroll
-      for (int d = 0; d < 8; ++d) {
-        const int code = clamp_code(__builtin_rintf(__builtin_ldexpf(f[d], -e)));
-        up[d / 4] |= (uint32_t)(max(code, 0) & 0xff) << (d % 4 * 8);
-        down[d / 4] |= (uint32_t)(min(code, 0) & 0xff) << (d % 4 * 8);
-      }
-      *(lds_u32x2 *)(smem + r * ROWB + c * 8) = up;
-      *(lds_u32x2 *)(smem + r * ROWB + D + c * 8) = down;
-      if (c == 0) exps[r] = e;
-    }
+    stage_queries<D, kScoreThreads>(p, seq, kvh, row0, smem, exps);
     __syncthreads();
-    i32x4_t s[2] = {};
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const i32x4_t qc = *(lds_i32x4 *)(smem + col * ROWB + i * 64 + quad * 16);
-#pragma unroll
-      for (int g = 0; g < 2; ++g) s[g] = __builtin_amdgcn_mfma_i32_16x16x64_i8(qc, codes[g][i], s[g], 0, 0, 0);
-    }
-    const i32x4_t e = *(lds_i32x4 *)(exps + quad * 4);
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int v = 0; v < 4; ++v) best[g] = fmaxf(best[g], __builtin_ldexpf((float)s[g][v], e[v]));
+    pages.score(smem, exps, lane, best);
   }
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
-    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(best[g]), __float_as_uint(best[g]), false, false);
-    best[g] = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-    best[g] = fmaxf(best[g], other_half(best[g]));
-    if (quad == g && at[g] < held)
-      p.scores[((int64_t)seq * p.n_kv_heads + kvh) * p.score_stride + at[g]] = there[g] ? __builtin_ldexpf(best[g], page_e[g]) : -INFINITY;
+    const float x = pages.result(g, best[g]);
+    const int at = mine + g * 16 + (lane & 15);
+    if (lane >> 4 == g && at < held) p.scores[((int64_t)seq * p.n_kv_heads + kvh) * p.score_stride + at] = x;
   }
 }
 
 // ---- pick -------------------------------------------------------------------------------------------------------
-template <int W, int E>
-__global__ __launch_bounds__(W * 64) void page_pick_kernel(PageSelectParams p) {
-  __shared__ PickLds<W> lds;
-  const int kvh = blockIdx.x % p.n_kv_heads, seq = blockIdx.x / p.n_kv_heads;
-  const int len = max(0, min(p.seq_len[seq], p.cap));
-  const int held = pages_held(p.pages, len);
+template <int W, int E, typename Value>
+__device__ __forceinline__ void pick_pages(const PageSelectParams &p, PickLds<W> &lds, int seq, int kvh, int len, int held, Value &&value) {
   const int newest = len > p.nq ? (int)fast_div((uint32_t)(len - p.nq), p.pages.page_div) : 0;
   const int last0 = min(held - p.n_last, newest);
   const int64_t list = (int64_t)seq * p.n_kv_heads + kvh;
-  const float *scores = p.scores + list * p.score_stride;
   int32_t *selected = p.selected + list * p.n_select;
   float *scores_out = p.scores_out ? p.scores_out + list * p.n_select : nullptr;
   const int n = pick_largest<W, E>(
-      lds, held, p.n_select, [&](int i) { return scores[i]; },
+      lds, held, p.n_select, value,
       [&](int i, float x) { return x == -INFINITY ? 0u : i < p.n_first || i >= last0 ? kPickAlways : pick_key(x); },  // (-infinity: not there)
       [&](int at, int i, float x) {
         selected[at] = i;
@@ -336,6 +349,57 @@ __global__ __launch_bounds__(W * 64) void page_pick_kernel(PageSelectParams p) {
     selected[j] = -1;
     if (scores_out) scores_out[j] = -INFINITY;
   }
+}
+template <int W, int E>
+__global__ __launch_bounds__(W * 64) void page_pick_kernel(PageSelectParams p) {
+  __shared__ PickLds<W> lds;
+  const int kvh = blockIdx.x % p.n_kv_heads, seq = blockIdx.x / p.n_kv_heads;
+  const int len = max(0, min(p.seq_len[seq], p.cap)), held = pages_held(p.pages, len);
+  const float *scores = p.scores + ((int64_t)seq * p.n_kv_heads + kvh) * p.score_stride;
+  pick_pages<W, E>(p, lds, seq, kvh, len, held, [&](int i) { return scores[i]; });
+}
+// Both in one launch, where a list's pages are few: scores stay in LDS.
+constexpr int kSelectOneWaves = 4;
+template <int D, int W>
+__global__ __launch_bounds__(W * 64) void page_select_kernel(PageSelectParams p) {
+  __shared__ PickLds<W> lds;
+  __shared__ float scores[kSelectOneLaunch];
+  __shared__ __attribute__((aligned(16))) char smem_generic[kScoreRows * (2 * D + 16) + kScoreRows * 4];
+  lds_char *const smem = (lds_char *)smem_generic;
+  lds_i *const exps = (lds_i *)(smem + kScoreRows * (2 * D + 16));
+  const int kvh = blockIdx.x % p.n_kv_heads, seq = blockIdx.x / p.n_kv_heads;
+  const int len = max(0, min(p.seq_len[seq], p.cap)), held = pages_held(p.pages, len);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n_rows = p.nq * p.group;
+  if (n_rows <= kScoreRows) {
+    stage_queries<D, W * 64>(p, seq, kvh, 0, smem, exps);
+    __syncthreads();
+  }
+#pragma unroll 1
+  for (int first = 0; first < held; first += W * 32) {  // (the same in all waves)
+    const int mine = first + wave * 32;
+    WavePages<D> pages;
+    pages.load(p, seq, kvh, mine, held, lane);
+    float best[2] = {-INFINITY, -INFINITY};
+    if (n_rows <= kScoreRows) {
+      pages.score(smem, exps, lane, best);
+    } else {
+#pragma unroll 1
+      for (int row0 = 0; row0 < n_rows; row0 += kScoreRows) {
+        __syncthreads();
+        stage_queries<D, W * 64>(p, seq, kvh, row0, smem, exps);
+        __syncthreads();
+        pages.score(smem, exps, lane, best);
+      }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const float x = pages.result(g, best[g]);
+      const int at = mine + g * 16 + (lane & 15);
+      if (lane >> 4 == g && at < held) scores[at] = x;
+    }
+  }
+  __syncthreads();
+  pick_pages<W, kSelectOneLaunch / (W * 64)>(p, lds, seq, kvh, len, held, [&](int i) { return scores[i]; });
 }
 
 }  // namespace
@@ -354,6 +418,13 @@ hipError_t launch_page_scores(const PageSelectParams &p, int head_dim, hipStream
   if (wgs < 1 || wgs > kMaxWorkgroups) return hipErrorInvalidValue;
   if (head_dim == 128) page_scores_kernel<128><<<(unsigned)wgs, kScoreThreads, 0, stream>>>(p, (int)chunks);
   else page_scores_kernel<64><<<(unsigned)wgs, kScoreThreads, 0, stream>>>(p, (int)chunks);
+  return hipGetLastError();
+}
+hipError_t launch_page_select(const PageSelectParams &p, int head_dim, hipStream_t stream) {
+  const int64_t wgs = (int64_t)p.n_seqs * p.n_kv_heads;
+  if (wgs < 1 || wgs > kMaxPickWorkgroups || p.score_stride > kSelectOneLaunch) return hipErrorInvalidValue;
+  if (head_dim == 128) page_select_kernel<128, kSelectOneWaves><<<(unsigned)wgs, kSelectOneWaves * 64, 0, stream>>>(p);
+  else page_select_kernel<64, kSelectOneWaves><<<(unsigned)wgs, kSelectOneWaves * 64, 0, stream>>>(p);
   return hipGetLastError();
 }
 hipError_t launch_page_pick(const PageSelectParams &p, hipStream_t stream) {
