@@ -152,7 +152,7 @@ __global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsPar
     }
   };
   // what the rows of the next kNoted tiles have beside them: -lse in log2 units, the key that each ends before, the sequence's length; whether all
-  // of a tile see all keys
+  // keys are old ones, seen by all rows of a tile
   auto note = [&](int tile0) __attribute__((always_inline)) {
 #pragma unroll 1
     for (int n = threadIdx.x; n < min(kNoted, n_tiles - tile0) * 32; n += kWThreads) {
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsPar
       ((lds_f *)to)[n % 32] = -lse * 1.4426950408889634f;
       ((lds_i *)to)[32 + n % 32] = limit;
       ((lds_i *)to)[64 + n % 32] = len;
-      const uint64_t see_all = __builtin_amdgcn_ballot_w64(limit > item_last);  // (two tiles to a wave)
+      const uint64_t see_all = __builtin_amdgcn_ballot_w64(limit > item_last && len - p.nq > item_last);  // (two tiles to a wave)
       if (n % 32 == 0) all_at[n / 32] = (uint32_t)(see_all >> (lane & 32)) == ~0u;
     }
   };
@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsPar
     auto sums = [&](auto masked) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {  // this lane's rows: tile * 32 + i * 8 + hf * 4 + (0 .. 3)
-        if (tile * 32 + i * 8 >= n_rows) break;
+        if (decltype(masked)::value && tile * 32 + i * 8 >= n_rows) break;  // (a tile with rows behind the last is masked)
         const f32x4_t nl = *(const lds_f32x4 *)(beside + (i * 8 + hf * 4) * 4);
         i32x4_t limit = {0, 0, 0, 0};
         if constexpr (decltype(masked)::value) limit = *(const lds_i32x4 *)(beside + (32 + i * 8 + hf * 4) * 4);
@@ -241,9 +241,14 @@ __global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsPar
           float total = sum;
           if constexpr (!kFour) total += other_half(total);
           sum = 0.f;
-          const int len = ((const lds_i *)beside)[64 + i * 8 + (kFour ? hf * 4 : 0)];
-          if (stores && key < len && (!kFour || tile * 32 + i * 8 + hf * 4 < n_rows))
-            (p.w_out + mine)[at[i]] = __builtin_fmaf(p.decay, key < len - p.nq ? old[i] : 0.f, k.there[0] ? total : 0.f);
+          total = k.there[0] ? total : 0.f;
+          if constexpr (decltype(masked)::value) {
+            const int len = ((const lds_i *)beside)[64 + i * 8 + (kFour ? hf * 4 : 0)];
+            if (stores && key < len && (!kFour || tile * 32 + i * 8 + hf * 4 < n_rows))
+              (p.w_out + mine)[at[i]] = __builtin_fmaf(p.decay, key < len - p.nq ? old[i] : 0.f, total);
+          } else {
+            if (stores) (p.w_out + mine)[at[i]] = __builtin_fmaf(p.decay, old[i], total);
+          }
         }
       }
     };
