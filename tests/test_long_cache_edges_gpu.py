@@ -343,3 +343,35 @@ def test_a_padded_batch(ba):
     ba.ba_paged_attention_selected(heads, cache, q, o, l, ints(lens), max_len, sel, 1, room(ba.ba_paged_attention_selected_workspace_bytes(heads, 5, 1, 16, max_len, 3)))
     assert not o[[1, 3]].any() and (l[[1, 3]] == -math.inf).all()
     close_attention(o, l, *attend64(pool, f64(q), 1, sel.cpu().numpy(), 0.125, pool.table))
+
+
+@pytest.mark.parametrize("keep,pages", [(0, 0), (48, 0), (0, 6), (64, 3)])
+def test_the_example(keep, pages):
+    """examples/long_answers.py at a small size: what its last step leaves against 64 bits."""
+    import importlib.util
+    import os
+
+    from paper_2409_15355_amd import binding
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "long_answers.py")
+    spec = importlib.util.spec_from_file_location("long_answers", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    run = example.LongAnswers(binding.Heads(8, 2, 64, 10000.0), 3, 200, 9, 5, 16, keep, pages, seed=4)
+    for _ in range(4):
+        o = run.step()
+    n = (keep or 209) + 4
+    assert run.len.tolist() == [n] * 3 and run.position.tolist() == [213] * 3
+
+    class Now:
+        pass
+    table = run.cache.page_table.cpu().numpy()
+    Now.lens, Now.rows, Now.hkv, Now.d, Now.kp, Now.max_len = [n] * 3, 16, 2, 64, run.cache.k_pages, n
+    Now.k, Now.v = (np.nan_to_num(np.stack([f64(pool)[table[s]].reshape(-1, 2, 64) for s in range(3)])) for pool in (run.cache.k_pages, run.cache.v_pages))
+    held = -(-n // 16)
+    sel = run.selected.cpu().numpy() if pages else np.tile(np.arange(held), (3, 2, 1))
+    if pages:
+        sel64, _ = select64(Now, run.bounds.codes.cpu().numpy(), run.bounds.exponents.cpu().numpy(), f64(run.q_rot), 1, pages, 1, 1, table)
+        assert np.array_equal(sel, sel64)
+    out, _, size, off = attend64(Now, f64(run.q_rot), 1, sel, 0.125, table)
+    tol = (BF16_STEP + 2.0 ** -11 + 2 * off[..., None]) * size + BF16_STEP * (np.abs(out) + (BF16_STEP + 2.0 ** -11) * size) + 1e-30
+    assert (np.abs(f64(o) - out) <= tol).all()
