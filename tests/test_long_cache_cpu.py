@@ -33,6 +33,7 @@ def test_key_weights_refusals(lib):  # noqa: F811
     assert weights(lib, w_in=0x20000004) == -1 and b"overlap" in lib.ba_last_error()
     assert weights(lib, w_in=0x20000000 + 6 * 64 * 4 - 4) == -1
     assert weights(lib, w_out=0x1000000) == -1 and weights(lib, w_out=0x500000 - 256) == -1      # q, lse
+    assert weights(lib, lens=0x20000000 + 64) == -1 and b"seq_len" in lib.ba_last_error()
     assert weights(lib, w_out=0x10000000 + 9 * 16 * 2048) == -1 and weights(lib, w_out=0x11000000) == -1  # pages
     # groups
     assert weights(lib, cu=[0, 2], pre=[5]) == -1 and weights(lib, cu=[0, 3], pre=[65]) == -1 and weights(lib, cu=[0, 3, 2, 3], pre=[5, 5, 5]) == -1

@@ -1,0 +1,52 @@
+"""Long paged caches on the paths that only larger calls take: pages scored apart from the choice among them by more query rows than a product has; groups and
+questions of more rows than a workgroup notes at a time; eviction past the caches.  Checks and tolerances are those of test_long_cache_gpu.py."""
+import pytest
+
+import test_long_cache_gpu as forms
+from test_long_cache_gpu import ba, ints  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("hq,hkv,d,rows,lens,nq,n_select,first,last", [
+    (16, 2, 64, 16, [5000, 4200], 5, 40, 1, 2), (6, 2, 128, 4, [5000], 7, 100, 3, 1), (8, 1, 64, 1, [300, 0, 290], 1, 20, 0, 0), (17, 1, 128, 2, [600, 9], 1, 70, 0, 5)])
+def test_selection_out_of_many_pages(ba, hq, hkv, d, rows, lens, nq, n_select, first, last):  # noqa: F811
+    forms.test_page_select(ba, hq, hkv, d, rows, lens, nq, n_select, first, last)
+
+
+@pytest.mark.parametrize("hq,hkv,d,rows,nq,members,prefix,behind", [
+    (8, 2, 64, 16, 1, [140], [130], [1 + i % 7 for i in range(140)]), (8, 1, 128, 16, 3, [30], [200], [3 + i % 9 for i in range(30)]),
+    (5, 1, 64, 7, 1, [2, 70], [20, 90], [1 + i % 11 for i in range(72)]),                                                                # few rows a sequence
+    (16, 2, 64, 16, 40, [5], [300], [40, 41, 70, 2, 300]), (12, 2, 128, 16, 50, [4], [100], [50, 60, 55, 300])])                         # many
+def test_key_weights_of_large_groups(ba, hq, hkv, d, rows, nq, members, prefix, behind):  # noqa: F811
+    forms.test_key_weights_over_shared_prefixes(ba, hq, hkv, d, rows, nq, members, prefix, behind)
+
+
+@pytest.mark.parametrize("hq,hkv,d,rows,lens,nq", [(16, 2, 64, 16, [1100], 1040), (9, 3, 64, 16, [900, 40], 700)])
+def test_key_weights_of_long_questions(ba, hq, hkv, d, rows, lens, nq):  # noqa: F811
+    forms.test_key_weights(ba, hq, hkv, d, rows, lens, nq, 0.5)
+
+
+@pytest.mark.parametrize("d,keep", [(128, 512), (64, 1024)])
+def test_eviction_past_the_caches(ba, d, keep):  # noqa: F811
+    """Half a gigabyte that goes by once: every row at its place, and none beside."""
+    import torch
+    n_seqs, hkv, rows, to_rows = 64, 8, 16, 32
+    lens = [keep + 1 + s % 50 for s in range(n_seqs)]
+    n, pages, to_pages = max(lens), -(-max(lens) // rows), keep // to_rows
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    kp, vp = (torch.randn((n_seqs * pages, rows, hkv, d), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    to_k, to_v = (torch.full((n_seqs * to_pages + 1, to_rows, hkv, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    old, new = torch.randperm(n_seqs * pages, generator=gen, device="cuda").view(n_seqs, pages), torch.randperm(n_seqs * to_pages, generator=gen, device="cuda").view(n_seqs, to_pages)
+    w = torch.randperm(n_seqs * hkv * n, generator=gen, device="cuda").float().view(n_seqs, hkv, n)  # (below 2^24: no two alike)
+    kept = torch.empty((n_seqs, hkv, keep), dtype=torch.int32, device="cuda")
+    ba.ba_paged_evict(ba.Heads(hkv, hkv, d), ba.PagedCache(kp, vp, old.int()), ba.PagedCache(to_k, to_v, new.int()), w, ints(lens), n, keep, 0, 0, kept)
+    for s, m in enumerate(lens):
+        w[s, :, m:] = -1.0
+    want = w.topk(keep).indices.sort().values
+    assert torch.equal(kept.long(), want)
+    j, head = torch.arange(keep, device="cuda"), torch.arange(hkv, device="cuda")[:, None]
+    for s in range(n_seqs):
+        for pool, to in ((kp, to_k), (vp, to_v)):
+            assert torch.equal(to[new[s][j // to_rows], j % to_rows].transpose(0, 1), pool[old[s][want[s] // rows], want[s] % rows, head]), s
+    assert bool((to_k[-1] == 7).all()) and bool((to_v[-1] == 7).all())
