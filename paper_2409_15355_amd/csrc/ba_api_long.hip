@@ -291,15 +291,22 @@ int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const
   // Rows go by once, and are read next after all other layers' have gone by, too.  us a call with / without the hint, 1,024 rows of eight heads of 128 for 8 sequences (67 MB read
   // and written) 22.3 / 21.5, 16 36.1 / 39.7, 24 50.0 / 54.0, 64 118 / 124.
   p.past_caches = lists * std::min(n_keep, max_len) * D * 8 > kCacheBytes * 3 / 8;
-  // us, eight lists of 2,064 tokens, in one launch and in two: 64 rows of 128 kept 8.2 / 9.3, 128 8.8 / 10.1, 256 9.9 / 10.5, 512 12.9 / 10.9; 512 lists of
-  // up to 8,000, 1,024 kept 123 / 117.
-  p.copies = std::min(n_keep, max_len) * (int64_t)D <= 256 * 128;
+  // Up to a list a compute unit: one launch, in which as many workgroups as there is room for make a list's choice, each of them for 32 rows of 128 at least.  us, in one launch and in two,
+  // 8 lists of 2,064 tokens, 64 rows of 128 kept 7.1 / 10.7, 512 7.5 / 10.6 (for 16, 64, 128 rows at least 7.4, 7.6, 9.1); 64 lists, 512 12.3 / 14.5; 256 lists, 256 19.1 / 20.5;
+  // 8 lists of 8,000, 2,048 13.4 / 15.6; 512 lists of 8,000, 128 35 / 30.
+  const int64_t rows = std::max<int64_t>(1, std::min(n_keep, max_len));
+  if (lists <= num_cus()) {
+    p.parts = (int32_t)std::min<int64_t>(num_cus() / lists, (rows * D + kEvictPartLeast - 1) / kEvictPartLeast);
+    p.part_rows = (int32_t)((rows + p.parts - 1) / p.parts);
+    p.parts = (int32_t)((rows + p.part_rows - 1) / p.part_rows);
+    if ((int64_t)p.part_rows * D > kEvictPartMost) p.parts = p.part_rows = 0;
+  }
   hipError_t e;
   {
     ProfileScope ps(BA_PROFILE_COMBINE, stream);
     e = launch_evict_pick(p, stream);
   }
-  if (e == hipSuccess && !p.copies) {
+  if (e == hipSuccess && p.parts == 0) {
     ProfileScope ps(BA_PROFILE_REENCODE, stream);
     e = launch_evict_copy(p, stream);
   }

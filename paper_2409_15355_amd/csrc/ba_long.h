@@ -62,9 +62,11 @@ struct EvictParams {
   PagedTableParams from, to;
   FastDiv heads_div;       // by n_kv_heads
   int32_t past_caches;     // rows are copied past the caches
-  int32_t copies;          // a list's workgroup copies its rows
+  // workgroups of a list (0: one, and the rows go in a launch of their own), rows that each of them writes and copies
+  int32_t parts, part_rows;
 };
 constexpr int64_t kMaxPickWorkgroups = 0xffffffffll / 1024;
+constexpr int kEvictPartLeast = 32 * 128, kEvictPartMost = 256 * 128;  // elements of the rows that a list's workgroup copies
 constexpr int kEvictCopyRows = 64;  // rows of heads that a workgroup copies
 inline int64_t evict_copy_chunks(int64_t n_keep, int64_t cap, int64_t n_kv_heads) {
   return ((n_keep < cap ? n_keep : cap) * n_kv_heads + kEvictCopyRows - 1) / kEvictCopyRows;

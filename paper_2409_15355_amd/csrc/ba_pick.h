@@ -95,11 +95,17 @@ __device__ __forceinline__ int pick_largest(PickLds<W> &l, int n, int want, Valu
       for (int s = 0; s < E; ++s)
         if (s < steps) f(s, mine[s], number[s]);
     } else {
+      constexpr int kTogether = 8;  // (eight lists of 100,000, 4,096 kept: one by one 153 to 182 us, so 143)
 #pragma unroll 1
-      for (int s = 0; s < steps; ++s) {
-        const int i = begin + s * 64 + lane;
-        const float x = i < n ? value(i) : 0.f;
-        f(s, i < n ? key(i, x) : 0u, x);
+      for (int s0 = 0; s0 < steps; s0 += kTogether) {
+        float x[kTogether];
+#pragma unroll
+        for (int s = 0; s < kTogether; ++s) x[s] = value(min(begin + (s0 + s) * 64 + lane, n - 1));
+#pragma unroll
+        for (int s = 0; s < kTogether; ++s) {
+          const int i = begin + (s0 + s) * 64 + lane;
+          if (s0 + s < steps) f(s0 + s, i < n ? key(i, x[s]) : 0u, x[s]);
+        }
       }
     }
   };

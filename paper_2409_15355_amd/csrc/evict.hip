@@ -1,7 +1,10 @@
 // Eviction from a paged cache by the weights of its keys (arXiv 2409.15355, Section 2.5: a cache that answers go on from): of every sequence
 // and KV head the first, the last and the heaviest tokens stay, in order, and move to other pages.
-//   pick: a workgroup a (sequence, KV head) finds the n_keep largest weights (ba_pick.h) and writes their places, their weights and the new length;
+//   pick: a workgroup a (sequence, KV head) finds the n_keep largest weights (ba_pick.h) and writes their places, their weights and the new length; of few lists
+//     several workgroups each, which copy the rows as well;
 //   copy: rows of keys and values by those places, sixteen bytes a lane.
+#include <algorithm>
+
 #include "ba_long.h"
 #include "ba_pick.h"
 
@@ -45,35 +48,47 @@ __device__ __forceinline__ void copy_rows(const EvictParams &p, int seq, int fir
 
 // Bound by latency for a few lists (eight of 2,064 tokens 7.2 us), by the instructions of sixteen waves a list for many (512 of up to 8,000 tokens 14.8 us: 47 % of
 // the vector units' cycles; 9 MB).
-// kRows: head_dim, and the workgroup copies its list's rows, too; 0: it does not.
+// kRows: head_dim, and rows are copied, too.  Then a list may have several workgroups: each of them makes the same choice, and writes and copies its part
+// of the rows, so nothing is handed on.  0: one workgroup a list, and no copies.
 template <int W, int E, int kRows>
 __global__ __launch_bounds__(W * 64) void evict_pick_kernel(EvictParams p) {
   __shared__ PickLds<W> lds;
-  const int kvh = blockIdx.x % p.n_kv_heads, seq = blockIdx.x / p.n_kv_heads;
+  __shared__ int32_t place_of[kRows > 0 ? kEvictPartMost / kRows : 1];
+  const int lists = p.n_seqs * p.n_kv_heads, part = kRows > 0 ? (int)blockIdx.x / lists : 0, of_list = kRows > 0 ? (int)blockIdx.x % lists : (int)blockIdx.x;
+  const int kvh = of_list % p.n_kv_heads, seq = of_list / p.n_kv_heads;
   const int len = max(0, min(p.seq_len[seq], p.cap));
   const int64_t list = (int64_t)seq * p.n_kv_heads + kvh;
   const float *w = p.weights + list * p.w_stride;
   int32_t *kept = p.kept + list * p.n_keep;
   float *w_out = p.w_out ? p.w_out + list * p.w_out_stride : nullptr;
   const int last0 = len - p.n_last;
+  const int lo = kRows > 0 ? part * p.part_rows : 0, hi = kRows > 0 && part + 1 < p.parts ? lo + p.part_rows : p.n_keep;
   const int n = pick_largest<W, E>(
       lds, len, p.n_keep, [&](int i) { return w[i]; }, [&](int i, float x) { return i < p.n_first || i >= last0 ? kPickAlways : pick_key(x); },
       [&](int at, int i, float x) {
+        if (kRows > 0 && (at < lo || at >= hi)) return;
         kept[at] = i;
         if (w_out) w_out[at] = x;
+        if constexpr (kRows > 0) place_of[at - lo] = i;
       });
-  for (int j = n + threadIdx.x; j < p.n_keep; j += W * 64) kept[j] = -1;
-  if (kvh == 0 && threadIdx.x == 0 && p.len_out) p.len_out[seq] = n;
+  for (int j = max(n, lo) + threadIdx.x; j < hi; j += W * 64) kept[j] = -1;
+  if (kvh == 0 && part == 0 && threadIdx.x == 0 && p.len_out) p.len_out[seq] = n;
   if constexpr (kRows > 0) {
-    constexpr int RPP = W * 64 / (kRows / 8), N = 4;  // rows of a pass of the threads, passes together
+    constexpr int RPP = W * 64 / (kRows / 8);  // rows of a pass of the threads
+    const int end = min(n, hi);
+    auto which = [&](int j, int &head, int &at, int &of) __attribute__((always_inline)) {
+      head = kvh, at = min(j, end - 1);
+      of = j < end ? place_of[at - lo] : -1;
+    };
+    if (lo >= end) return;
     __syncthreads();
+    const int first = lo + threadIdx.x / (kRows / 8);
+    if (p.part_rows <= RPP) {
+      copy_rows<kRows, 1, false>(p, seq, first, RPP, which);
+    } else {
 #pragma unroll 1
-    for (int j0 = 0; j0 < n; j0 += N * RPP)
-      copy_rows<kRows, N, false>(p, seq, j0 + threadIdx.x / (kRows / 8), RPP, [&](int j, int &head, int &at, int &of) {
-        head = kvh, at = min(j, n - 1);
-        of = kept[at];
-        if (j >= n) of = -1;
-      });
+      for (int j0 = 0; lo + j0 < end; j0 += 4 * RPP) copy_rows<kRows, 4, false>(p, seq, first + j0, RPP, which);
+    }
   }
 }
 
@@ -95,15 +110,15 @@ __global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictParams p,
 }  // namespace
 
 hipError_t launch_evict_pick(const EvictParams &p, hipStream_t stream) {
-  const int64_t wgs = (int64_t)p.n_seqs * p.n_kv_heads;
-  if (wgs < 1 || wgs > kMaxPickWorkgroups) return hipErrorInvalidValue;
+  const int64_t wgs = (int64_t)p.n_seqs * p.n_kv_heads * std::max(p.parts, 1);
+  if (wgs < 1 || wgs > kMaxPickWorkgroups || (p.parts > 0 && (int64_t)p.part_rows * p.head_dim > kEvictPartMost)) return hipErrorInvalidValue;
   return with_pick_shape(p.cap, [&](auto w, auto e) {
     auto launch = [&](auto rows) {
       evict_pick_kernel<decltype(w)::value, decltype(e)::value, decltype(rows)::value><<<(unsigned)wgs, decltype(w)::value * 64, 0, stream>>>(p);
       return hipGetLastError();
     };
     using std::integral_constant;
-    if (!p.copies) return launch(integral_constant<int, 0>{});
+    if (p.parts == 0) return launch(integral_constant<int, 0>{});
     return p.head_dim == 128 ? launch(integral_constant<int, 128>{}) : launch(integral_constant<int, 64>{});
   });
 }
