@@ -108,8 +108,8 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
   pl->groups.item0[pl->groups.n] = pl->prefix_items = (int32_t)std::min<int64_t>(items, INT32_MAX);
   pl->own_chunks = (int32_t)(((int64_t)max_len - least_prefix + keys - 1) / keys);
   const int64_t own_items = (int64_t)pl->n_seqs * h->n_kv_heads * pl->own_chunks;
-  // Many rows over keys that do not fill the chip: in up to eight parts of two tiles at least, where the merge (3 us, a tile 0.9) costs less than they save.
-  // us, in one part and in several: 1,024 rows over 2,000 keys 36 / 15, over 500 32 / 12.
+  // Many rows over keys that do not fill the chip: in up to eight parts of two tiles at least, where the merge (3 us, a tile 0.9) costs less than
+  // they save.  us, in one part and in several: 1,024 rows over 2,000 keys 36 / 15, over 500 32 / 12.
   pl->row_parts = 1;
   if (pl->many && n_groups == 0 && own_items > 0) {
     const int64_t tiles = ((int64_t)nq * (h->n_q_heads / h->n_kv_heads) + 31) / 32, parts = std::min<int64_t>({tiles / 2, 8, kWeightsSlots * num_cus() / own_items});
@@ -247,7 +247,8 @@ int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const
   if (weights_out && stride_out < n_keep) return fail(BA_ERR_INVALID_ARG, "stride_out smaller than n_keep");
   const int64_t lists = (int64_t)n_seqs * hkv;
   if ((rc = check_lists(n_seqs, heads))) return rc;
-  if (n_seqs * evict_copy_chunks(n_keep, max_len, hkv) > kMaxWorkgroups || (int64_t)std::min(n_keep, max_len) * hkv > (1 << 30)) return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
+  if (n_seqs * evict_copy_chunks(n_keep, max_len, hkv) > kMaxWorkgroups || (int64_t)std::min(n_keep, max_len) * hkv > (1 << 30))
+    return fail(BA_ERR_UNSUPPORTED, "2^24 work items and more in one launch");
   // ---- where everything lies
   if (!apart(extent(&to->k, to->page_rows, hkv, D), extent(&to->v, to->page_rows, hkv, D)))
     return fail(BA_ERR_INVALID_ARG, "to: keys and values of a page overlap");
@@ -288,12 +289,12 @@ int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const
   set_rows(&p.to_k, &to->k, to->k_stride_page), set_rows(&p.to_v, &to->v, to->v_stride_page);
   set_table(&p.from, cache), set_table(&p.to, to);
   p.heads_div = make_fast_div((uint32_t)hkv);
-  // Rows go by once, and are read next after all other layers' have gone by, too.  us a call with / without the hint, 1,024 rows of eight heads of 128 for 8 sequences (67 MB read
-  // and written) 22.3 / 21.5, 16 36.1 / 39.7, 24 50.0 / 54.0, 64 118 / 124.
+  // Rows go by once, and are read next after all other layers' have gone by, too.  us a call with / without the hint, 1,024 rows of eight heads of
+  // 128 for 8 sequences (67 MB read and written) 22.3 / 21.5, 16 36.1 / 39.7, 24 50.0 / 54.0, 64 118 / 124.
   p.past_caches = lists * std::min(n_keep, max_len) * D * 8 > kCacheBytes * 3 / 8;
-  // Up to a list a compute unit: one launch, in which as many workgroups as there is room for make a list's choice, each of them for 32 rows of 128 at least.  us, in one launch and in two,
-  // 8 lists of 2,064 tokens, 64 rows of 128 kept 7.1 / 10.7, 512 7.5 / 10.6 (for 16, 64, 128 rows at least 7.4, 7.6, 9.1); 64 lists, 512 12.3 / 14.5; 256 lists, 256 19.1 / 20.5;
-  // 8 lists of 8,000, 2,048 13.4 / 15.6; 512 lists of 8,000, 128 35 / 30.
+  // Up to a list a compute unit: one launch, in which as many workgroups as there is room for make a list's choice, each of them for 32 rows of 128
+  // at least.  us, in one launch and in two, 8 lists of 2,064 tokens, 64 rows of 128 kept 7.1 / 10.7, 512 7.5 / 10.6 (for 16, 64, 128 rows at least
+  // 7.4, 7.6, 9.1); 64 lists, 512 12.3 / 14.5; 256 lists, 256 19.1 / 20.5; 8 lists of 8,000, 2,048 13.4 / 15.6; 512 lists of 8,000, 128 35 / 30.
   const int64_t rows = std::max<int64_t>(1, std::min(n_keep, max_len));
   if (lists <= num_cus()) {
     p.parts = (int32_t)std::min<int64_t>(num_cus() / lists, (rows * D + kEvictPartLeast - 1) / kEvictPartLeast);

@@ -1,7 +1,7 @@
 // Eviction from a paged cache by the weights of its keys (arXiv 2409.15355, Section 2.5: a cache that answers go on from): of every sequence
 // and KV head the first, the last and the heaviest tokens stay, in order, and move to other pages.
-//   pick: a workgroup a (sequence, KV head) finds the n_keep largest weights (ba_pick.h) and writes their places, their weights and the new length; of few lists
-//     several workgroups each, which copy the rows as well;
+//   pick: a workgroup a (sequence, KV head) finds the n_keep largest weights (ba_pick.h) and writes their places, their weights and the new
+//     length; of few lists several workgroups each, which copy the rows as well;
 //   copy: rows of keys and values by those places, sixteen bytes a lane.
 #include <algorithm>
 
@@ -46,8 +46,8 @@ __device__ __forceinline__ void copy_rows(const EvictParams &p, int seq, int fir
     }
 }
 
-// Bound by latency for a few lists (eight of 2,064 tokens 7.2 us), by the instructions of sixteen waves a list for many (512 of up to 8,000 tokens 14.8 us: 47 % of
-// the vector units' cycles; 9 MB).
+// Bound by latency for a few lists (eight of 2,064 tokens, 512 rows of 128 each copied: a call 7.4 us), by the instructions of sixteen waves a list
+// for many (512 of up to 8,000 tokens 14.8 us: 47 % of the vector units' cycles; 9 MB).
 // kRows: head_dim, and rows are copied, too.  Then a list may have several workgroups: each of them makes the same choice, and writes and copies its part
 // of the rows, so nothing is handed on.  0: one workgroup a list, and no copies.
 template <int W, int E, int kRows>
@@ -93,8 +93,7 @@ __global__ __launch_bounds__(W * 64) void evict_pick_kernel(EvictParams p) {
 }
 
 // The copies apart from the lists: a workgroup takes kCopyRows new rows of heads, a token's heads one after the other, so what it writes lies together.
-// Bound by HBM: 64 sequences, 1,024 rows of eight heads of 128, 271 MB in and 261 out, 104 us, 5.1 TB/s.  For one
-// sequence's 512 rows (4 MB, 3.9 us) by the loads in front of a row.
+// Bound by HBM: 64 sequences, 1,024 rows of eight heads of 128, 271 MB in and 261 out, 104 us, 5.1 TB/s.
 constexpr int kCopyThreads = 256, kCopyRows = kEvictCopyRows;
 template <int D, bool kPast>
 __global__ __launch_bounds__(kCopyThreads) void evict_copy_kernel(EvictParams p, int chunks) {

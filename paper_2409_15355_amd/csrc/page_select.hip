@@ -71,8 +71,8 @@ __device__ __forceinline__ float max_over_lanes(float x) {
 }
 
 // ---- bounds -----------------------------------------------------------------------------------------------------
-// A wave a (page, KV head), D / 8 lanes a row; nothing is computed twice, each key is read once.  Bound by HBM where much is new (31,744 tokens, 8 heads of 128: 16 us,
-// 65 MB in and 4 out), by the launch in a decoding step (128 sequences 4.6 us).
+// A wave a (page, KV head), D / 8 lanes a row; nothing is computed twice, each key is read once.  Bound by HBM where much is new (31,744 tokens, 8
+// heads of 128: 16 us, 65 MB in and 4 out), by the launch in a decoding step (128 sequences 4.6 us).
 // Waves of a launch.  us, 2,048 / 4,096 / 8,192: 128 sequences that take one token more 4.7 / 5.6 / 8.0, all of 31,744 tokens 16.0 / 15.3 / 15.4.
 constexpr int kBoundTarget = 2048;
 constexpr int kBoundThreads = 256, kBoundWaves = kBoundThreads / 64;
