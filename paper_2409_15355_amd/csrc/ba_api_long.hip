@@ -60,7 +60,7 @@ constexpr int64_t kWeightsSlots = 4;  // workgroups of the kernel for many rows 
 // ---- weights of cached keys --------------------------------------------------------------------------------
 struct WeightsPlan {
   int32_t seq0, n_seqs, group_end;
-  int32_t prefix_items, own_chunks;
+  int32_t prefix_items, own_chunks, item_members;
   int32_t part_tiles, row_parts;  // (see KeyWeightsParams)
   bool many;
   int64_t items;
@@ -100,10 +100,21 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
   // 64 19.9 / 15.3, 128 28.2 / 20.2, 1,024 139 / 84; of 2,000, 32 rows 5.0 / 5.5, 64 5.9 / 6.8, 256 15.1 / 11.9, 1,024 52 / 36.
   pl->many = nq * (h->n_q_heads / h->n_kv_heads) >= 32;
   const int32_t keys = pl->many ? kWeightsManyKeys : kWeightsFewKeys;
-  int64_t items = 0;
+  int64_t items = 0, most_members = 1;
+  for (int i = 0; i < pl->groups.n; ++i) {
+    items += ((int64_t)pl->groups.prefix[i] + keys - 1) / keys * h->n_kv_heads;
+    most_members = std::max<int64_t>(most_members, pl->groups.members[i]);
+  }
+  // A group's sequences in parts (nothing has to be added up: their weights are their own) where its keys do not fill the chip, of 64 rows at least.
+  // us, in one part and in several (of 32 / 64 / 128 rows at least): 46 answers of 4 rows on 1,141 keys 11.2 and 7.0 / 7.3 / 9.3; two groups of 28 of 16 rows on
+  // 1,096 keys 19.5 and 13.1 / 13.1 / 11.5; 16 of 32 rows on 2,000 keys 24.4 and 14.4 / 11.1 / 11.2.
+  constexpr int64_t kRowsLeast = 64;
+  const int64_t parts = items > 0 ? std::max<int64_t>(1, kWeightsSlots * num_cus() / items) : 1, padded = padded_rows(h, nq);
+  pl->item_members = (int32_t)std::min(most_members, std::max((kRowsLeast + padded - 1) / padded, (most_members + parts - 1) / parts));
+  items = 0;
   for (int i = 0; i < pl->groups.n; ++i) {
     pl->groups.item0[i] = (int32_t)std::min<int64_t>(items, INT32_MAX);
-    items += ((int64_t)pl->groups.prefix[i] + keys - 1) / keys * h->n_kv_heads;
+    items += ((int64_t)pl->groups.prefix[i] + keys - 1) / keys * h->n_kv_heads * ((pl->groups.members[i] + pl->item_members - 1) / pl->item_members);
   }
   pl->groups.item0[pl->groups.n] = pl->prefix_items = (int32_t)std::min<int64_t>(items, INT32_MAX);
   pl->own_chunks = (int32_t)(((int64_t)max_len - least_prefix + keys - 1) / keys);
@@ -111,7 +122,7 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
   // Many rows over keys that do not fill the chip: in up to eight parts of two tiles at least, where the merge (3 us, a tile 0.9) costs less than
   // they save.  us, in one part and in several: 1,024 rows over 2,000 keys 36 / 15, over 500 32 / 12.
   pl->row_parts = 1;
-  if (pl->many && n_groups == 0 && own_items > 0) {
+  if (pl->many && pl->groups.n == 0 && own_items > 0) {
     const int64_t tiles = ((int64_t)nq * (h->n_q_heads / h->n_kv_heads) + 31) / 32, parts = std::min<int64_t>({tiles / 2, 8, kWeightsSlots * num_cus() / own_items});
     if (tiles >= 8 && parts > 1) {
       pl->part_tiles = (int32_t)((tiles + parts - 1) / parts);
@@ -135,11 +146,16 @@ extern "C" {
 
 size_t ba_paged_key_weights_workspace_bytes(const ba_heads *heads, int32_t n_seqs, int32_t q_per_seq, int32_t max_len, int32_t n_groups,
                                             const int32_t *cu_group, const int32_t *prefix_len) {
-  if (check_paged_sizes(heads, n_seqs, q_per_seq, max_len) != BA_OK || check_groups(n_seqs, max_len, n_groups, cu_group, prefix_len) != BA_OK || n_groups > 0)
-    return 0;
+  if (check_paged_sizes(heads, n_seqs, q_per_seq, max_len) != BA_OK || check_groups(n_seqs, max_len, n_groups, cu_group, prefix_len) != BA_OK) return 0;
+  size_t bytes = 0;
   WeightsPlan pl;
-  plan_weights(heads, n_seqs, q_per_seq, max_len, 0, nullptr, nullptr, 0, &pl);
-  return weights_bytes(pl, heads, max_len);
+  int g = 0;
+  do {
+    plan_weights(heads, n_seqs, q_per_seq, max_len, n_groups, cu_group, prefix_len, g, &pl);
+    bytes = std::max(bytes, weights_bytes(pl, heads, max_len));
+    g = pl.group_end;
+  } while (g < n_groups);
+  return bytes;
 }
 
 int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache, const ba_tensor *q, const float *lse, const float *weights_in,
@@ -201,7 +217,7 @@ int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache,
     p.w_in = weights_in && decay != 0.f ? weights_in + at : nullptr;
     p.w_out = weights_out + at;
     p.w_stride = stride_weights;
-    p.prefix_items = pl.prefix_items, p.own_chunks = pl.own_chunks;
+    p.prefix_items = pl.prefix_items, p.own_chunks = pl.own_chunks, p.item_members = pl.item_members;
     p.part_tiles = pl.part_tiles, p.row_parts = pl.row_parts;
     p.part = (float *)ws;
     ProfileScope ps(BA_PROFILE_ATTENTION, (hipStream_t)stream);

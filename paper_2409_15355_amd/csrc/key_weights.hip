@@ -2,7 +2,7 @@
 // sequence's query rows (token i, head h of the KV head) and its key t <= p(i)
 //   w_t = decay w_t + sum_rows exp(scale <q_row, k_t> - lse_row).
 //
-// A work item is a range of keys of one KV head, of a group's prefix (for the rows of all its sequences, whose weights lie apart)
+// A work item is a range of keys of one KV head, of a group's prefix (for the rows of its sequences, or of some of them, whose weights lie apart)
 // or of what a sequence has behind it.  S = Q K^T by v_mfma_f32_32x32x16_bf16 with the keys as columns: a lane owns a key, its
 // registers run over the rows, so the sum over rows is a lane's own and is stored as 128 consecutive bytes a half-wave.  A wave's
 // keys come straight from the pages into its registers, once; the query rows go round through LDS in tiles of 32, for all waves.
@@ -26,6 +26,7 @@ __device__ __forceinline__ int clamped_length(const int32_t *seq_len, int cap, i
 
 struct WeightsItem {
   int seq0, n_mem;    // the sequences whose rows it takes
+  int table_seq;      // the one whose pages it reads
   int kvh;
   int key0, key_end;  // keys from key0 on, below key_end
   int part;
@@ -42,10 +43,17 @@ __device__ __forceinline__ WeightsItem weights_item(const KeyWeightsParams &p, c
       if (groups.item0[mid] <= id) lo = mid; else hi = mid;
     }
     const int rel = id - groups.item0[lo];
-    it.seq0 = groups.seq0[lo];
+    it.seq0 = it.table_seq = groups.seq0[lo];
     it.n_mem = groups.members[lo];
     it.kvh = rel % p.n_kv_heads;
-    it.key0 = rel / p.n_kv_heads * KEYS;
+    int chunk = rel / p.n_kv_heads;
+    if (it.n_mem > p.item_members) {
+      const int parts = (it.n_mem + p.item_members - 1) / p.item_members, first = chunk % parts * p.item_members;
+      chunk /= parts;
+      it.seq0 += first;
+      it.n_mem = min(p.item_members, it.n_mem - first);
+    }
+    it.key0 = chunk * KEYS;
     it.key_end = groups.prefix[lo];
   } else {
     int rel = (int)blockIdx.x - p.prefix_items;
@@ -53,7 +61,7 @@ __device__ __forceinline__ WeightsItem weights_item(const KeyWeightsParams &p, c
     rel /= p.n_kv_heads;
     const int chunk = rel % p.own_chunks;
     rel /= p.own_chunks;
-    it.seq0 = rel % p.n_seqs;
+    it.seq0 = it.table_seq = rel % p.n_seqs;
     it.part = rel / p.n_seqs;
     it.n_mem = 1;
     int lo = 0, hi = groups.n;  // its group
@@ -78,7 +86,7 @@ struct WaveKeys {
     for (int t = 0; t < NT; ++t) {
       key[t] = key0 + t * 32 + (lane & 31);
       const int k = min(key[t], it.key_end - 1), page_at = (int)fast_div((uint32_t)k, p.pages.page_div);
-      int page = page_at < p.pages.max_pages ? p.pages.table[it.seq0 * p.pages.stride + page_at] : -1;
+      int page = page_at < p.pages.max_pages ? p.pages.table[it.table_seq * p.pages.stride + page_at] : -1;
       there[t] = page >= 0 && page < p.pages.n_pages;
       page = there[t] ? page : 0;  // (some row that is there: its sums are dropped)
       const char *row = (const char *)(p.k.base + it.kvh * p.k.sh) + ((uint64_t)(uint32_t)page * p.k.page_b16 << 4) +

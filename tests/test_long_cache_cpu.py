@@ -50,7 +50,7 @@ def test_key_weights_workspace(lib):  # noqa: F811
     size = lambda n, nq, m, cu=None, pre=None, h=HEADS: lib.ba_paged_key_weights_workspace_bytes(ref(h.c), n, nq, m, 0 if pre is None else len(pre), ip(cu), ip(pre))  # noqa: E731
     assert size(3, 1, 64) == 0 and size(0, 1, 64) == 0 and size(3, 1, -1) == 0 and size(3, 0, 64) == 0
     assert size(1, 256, 400) > 0                 # many rows over few keys: in parts
-    assert size(1, 256, 400, [0, 1], [100]) == 0
+    assert size(2, 256, 400, [0, 2], [100]) == 0 and size(2, 256, 400, [0, 2], [0]) == size(2, 256, 400)
     q = fake(FAR)
     need = size(3, 256, 64)
     assert need > 0 and weights(lib, q=q, nq=256, wsb=need - 1) == -4 and weights(lib, q=q, nq=256, ws=None, wsb=0) == -4

@@ -27,6 +27,50 @@ def test_key_weights_of_long_questions(ba, hq, hkv, d, rows, lens, nq):  # noqa:
     forms.test_key_weights(ba, hq, hkv, d, rows, lens, nq, 0.5)
 
 
+@pytest.mark.parametrize("hq,d,members,prefix", [(32, 64, 140, 8400), (24, 128, 70, 8321), (32, 64, 9, 1000)])
+def test_key_weights_of_many_answers_on_a_long_prefix(ba, hq, d, members, prefix):  # noqa: F811
+    """More rows than a workgroup notes at a time; with old weights, and in parts of a group's sequences."""
+    import torch
+    hkv, rows = 8, 16
+    g, pages = hq // hkv, -(-prefix // rows)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    kp = torch.randn((pages + members, rows, hkv, d), generator=gen, device="cuda").bfloat16()
+    order = torch.randperm(pages + members, generator=gen, device="cuda")
+    table = order[:pages].expand(members, pages).clone()
+    table = torch.cat([table, order[pages:, None]], 1)
+    lens = [pages * rows + 1 + s % rows for s in range(members)]
+    n = pages * rows + rows
+    q = (torch.randn((members, hq, d), generator=gen, device="cuda") * 2).bfloat16()
+    old = torch.rand((members, hkv, n), generator=gen, device="cuda")
+    shared, own = kp[order[:pages]].double().view(-1, hkv, d), kp[order[pages:]].double()
+    lse = torch.empty((members, hq), device="cuda")
+    want, off = torch.zeros((2, members, hkv, n), dtype=torch.float64, device="cuda")
+    scale, u = d ** -0.5, forms.U
+    for h in range(hkv):
+        qh = q[:, h * g:(h + 1) * g].double()
+        sizes, scores = [], []
+        for f in (lambda x: x, torch.abs):
+            first = (f(qh).reshape(-1, d) @ f(shared[:, h]).T).view(members, g, -1)
+            last = (f(qh)[:, :, None] * f(own[:, None, :, h])).sum(-1)
+            (sizes if f is torch.abs else scores).append(torch.cat([first, last], 2) * scale)
+        s, size = scores[0], sizes[0]
+        for m, x in enumerate(lens):
+            s[m, :, x:] = -float("inf")
+        lse[:, h * g:(h + 1) * g] = s.logsumexp(-1).float()
+        l = lse[:, h * g:(h + 1) * g, None].double()
+        p = (s - l).exp()
+        want[:, h] = p.sum(1)
+        off[:, h] = (p * (d * u * size + (s.abs().nan_to_num(posinf=0.0) + l.abs() + 4 + g) * u)).sum(1)
+    out = torch.full((members, hkv, n), -7.0, device="cuda")
+    heads, cache = ba.Heads(hq, hkv, d), ba.PagedCache(kp, kp, table.int())
+    ba.ba_paged_key_weights(heads, cache, q, lse, old, out, 0.5, ints(lens), n, [0, members], [prefix], 1)
+    for m, x in enumerate(lens):
+        want[m, :, : x - 1] += 0.5 * old[m, :, : x - 1].double()
+        off[m, :, : x - 1] += 2 * u * want[m, :, : x - 1]
+        assert bool((out[m, :, x:] == -7).all()), m
+        assert bool(((out[m, :, :x].double() - want[m, :, :x]).abs() <= off[m, :, :x] + 1e-37).all()), m
+
+
 @pytest.mark.parametrize("d,keep", [(128, 512), (64, 1024)])
 def test_eviction_past_the_caches(ba, d, keep):  # noqa: F811
     """Half a gigabyte that goes by once: every row at its place, and none beside."""
