@@ -308,12 +308,13 @@ int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const
   // Rows go by once, and are read next after all other layers' have gone by, too.  us a call with / without the hint, 1,024 rows of eight heads of
   // 128 for 8 sequences (67 MB read and written) 22.3 / 21.5, 16 36.1 / 39.7, 24 50.0 / 54.0, 64 118 / 124.
   p.past_caches = lists * std::min(n_keep, max_len) * D * 8 > kCacheBytes * 3 / 8;
-  // Up to a list a compute unit: one launch, in which as many workgroups as there is room for make a list's choice, each of them for 32 rows of 128
-  // at least.  us, in one launch and in two, 8 lists of 2,064 tokens, 64 rows of 128 kept 7.1 / 10.7, 512 7.5 / 10.6 (for 16, 64, 128 rows at least
-  // 7.4, 7.6, 9.1); 64 lists, 512 12.3 / 14.5; 256 lists, 256 19.1 / 20.5; 8 lists of 8,000, 2,048 13.4 / 15.6; 512 lists of 8,000, 128 35 / 30.
+  // Up to a list a compute unit, and lists short enough for four waves: one launch, in which as many workgroups as there is room for make a list's
+  // choice, each of them for 32 rows of 128 at least.  us, in one launch and in two, 8 lists of 2,064 tokens, 64 rows of 128 kept 7.1 / 10.7, 512 7.5 / 10.6
+  // (for 16, 64, 128 rows at least 7.4, 7.6, 9.1); 64 lists, 512 12.3 / 14.5; 256 lists, 256 19.1 / 20.5; 8 lists of 8,000, 2,048 13.4 / 15.6; 512 lists of
+  // 100 tokens, 50 8.8 / 12.0; of 1,000, 64 11.8 / 14.8; of 2,000, 128 23.6 / 22.3; of 8,000, 128 35 / 30.
   const int64_t rows = std::max<int64_t>(1, std::min(n_keep, max_len));
-  if (lists <= num_cus()) {
-    p.parts = (int32_t)std::min<int64_t>(num_cus() / lists, (rows * D + kEvictPartLeast - 1) / kEvictPartLeast);
+  if (lists <= num_cus() || max_len <= kPickFourWaves) {
+    p.parts = (int32_t)std::min<int64_t>(std::max<int64_t>(1, num_cus() / lists), (rows * D + kEvictPartLeast - 1) / kEvictPartLeast);
     p.part_rows = (int32_t)((rows + p.parts - 1) / p.parts);
     p.parts = (int32_t)((rows + p.part_rows - 1) / p.part_rows);
     if ((int64_t)p.part_rows * D > kEvictPartMost) p.parts = p.part_rows = 0;

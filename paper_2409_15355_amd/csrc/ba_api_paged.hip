@@ -292,11 +292,14 @@ size_t plan_bytes(const PagedPlan &pl, const ba_heads *h, int32_t nq) {
 }
 
 // The plan of a call over listed pages of `keys` keys at most.  Their number is a bound that most sequences reach, so the parts are as many as cost
-// least: rounds of items on the slots, an item as much as its keys and 100 more (see plan_paged), the merge as much as 70 and what it
-// writes and reads.
+// least: rounds of items on the compute units, an item as much as its keys (twice, with more than 16 rows) and 150 more, the merge as much as 400 and
+// what it writes and reads.  A key more is 0.011 us where an item has a compute unit to itself; two that share one take as long as one after the other.
+// us, 8 key heads of 128 and 4 rows, in 1 / 2 / 4 / 8 / 16 parts: 1 sequence of 256 keys 8.3 / 10.7 / 10.3, of 512 10.8 / 12.0 / 11.3 / 10.3, of 1,024
+// 16.1 / 14.3 / 12.4 / 10.7 / 10.4; 4 of 1,536 22.0 / 17.9 / 13.9 / 13.1 / 13.8; 12 of 1,536 22.7 / 20.9 / 21.5 / 22.8; 24 29.6 / 35.0 / 33.1 / 36.4 / 41.9;
+// 80 87 / 88 / 92 / 105; 64 of 384 21.3 / 28.5; 32 rows, 1 of 256 13.1 / 14.8, of 512 17.7 / 16.7 / 16.0 / 14.7.
 void plan_selected(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t page_rows, int32_t keys, int cus, PagedPlan *pl) {
   memset(pl, 0, sizeof(*pl));
-  const int64_t rows = (int64_t)nq * (h->n_q_heads / h->n_kv_heads), slots = 2 * cus, D = h->head_dim;
+  const int64_t rows = (int64_t)nq * (h->n_q_heads / h->n_kv_heads), D = h->head_dim;
   pl->n_seqs = n_seqs;
   pl->own_row_tiles = (int32_t)((rows + paged_tile_rows((int)rows) - 1) / paged_tile_rows((int)rows));
   pl->keys = (int64_t)n_seqs * keys;
@@ -307,7 +310,8 @@ void plan_selected(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t page_r
     const int64_t chunk = std::max<int64_t>(64, (keys + parts * 64 - 1) / (parts * 64) * 64);
     if (chunk > most && parts < 256) continue;
     const int64_t taken = std::min<int64_t>(chunk, most), really = std::max<int64_t>(1, (keys + taken - 1) / taken);
-    const int64_t cost = (walks * really + slots - 1) / slots * (taken + 100) + (really > 1 ? 70 + all_rows * really * (4 * D + 32) / (4 * D * slots) : 0);
+    const int64_t cost = (walks * really + cus - 1) / cus * (taken * (rows > 16 ? 2 : 1) + 150) +
+                         (really > 1 ? 400 + all_rows * really * (4 * D + 32) / (8 * D * cus) : 0);
     if (cost < least_cost) least_cost = cost, pl->own_chunk = (int32_t)taken, pl->own_splits = (int32_t)really;
   }
   pl->parts = pl->own_splits;

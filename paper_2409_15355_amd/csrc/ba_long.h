@@ -67,6 +67,7 @@ struct EvictParams {
   int32_t parts, part_rows;
 };
 constexpr int64_t kMaxPickWorkgroups = 0xffffffffll / 1024;
+constexpr int kPickFourWaves = 1024;  // of lists up to here a choice takes four waves, of longer ones sixteen
 constexpr int kEvictPartLeast = 32 * 128, kEvictPartMost = 256 * 128;  // elements of the rows that a list's workgroup copies
 constexpr int kEvictCopyRows = 64;  // rows of heads that a workgroup copies
 inline int64_t evict_copy_chunks(int64_t n_keep, int64_t cap, int64_t n_kv_heads) {

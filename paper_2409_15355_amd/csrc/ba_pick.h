@@ -2,6 +2,7 @@
 #pragma once
 
 #include "ba_lds.h"
+#include "ba_long.h"
 
 namespace ba {
 
@@ -238,7 +239,7 @@ auto with_pick_shape(int64_t n, F &&f) {
   using std::integral_constant;
   constexpr integral_constant<int, 4> four{};
   constexpr integral_constant<int, 16> sixteen{};
-  if (n <= 1024) return f(four, integral_constant<int, 4>{});
+  if (n <= kPickFourWaves) return f(four, integral_constant<int, 4>{});
   if (n <= 4 * 1024) return f(sixteen, integral_constant<int, 4>{});
   if (n <= 8 * 1024) return f(sixteen, integral_constant<int, 8>{});
   if (n <= 32 * 1024) return f(sixteen, integral_constant<int, 32>{});
