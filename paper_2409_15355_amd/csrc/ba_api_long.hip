@@ -55,7 +55,7 @@ void set_table(PagedTableParams *p, const ba_paged_cache *c) {
   p->page_div = make_fast_div((uint32_t)c->page_rows);
 }
 
-constexpr int64_t kWeightsSlots = 4;  // workgroups of the kernel for many rows to a compute unit
+constexpr int64_t kWeightsSlots = 4;  // workgroups to a compute unit
 
 // ---- weights of cached keys --------------------------------------------------------------------------------
 struct WeightsPlan {
@@ -119,14 +119,18 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
   pl->groups.item0[pl->groups.n] = pl->prefix_items = (int32_t)std::min<int64_t>(items, INT32_MAX);
   pl->own_chunks = (int32_t)(((int64_t)max_len - least_prefix + keys - 1) / keys);
   const int64_t own_items = (int64_t)pl->n_seqs * h->n_kv_heads * pl->own_chunks;
-  // Many rows over keys that do not fill the chip: in up to eight parts of two tiles at least, where the merge (3 us, a tile 0.9) costs less than
-  // they save.  us, in one part and in several: 1,024 rows over 2,000 keys 36 / 15, over 500 32 / 12.
+  // Many rows in up to eight parts: what costs least, in tenths of the time that a tile takes a compute unit's workgroups together: 12 for one of them, 20
+  // for two, 10 each for more; the merge (a launch) 50 and its bytes.  us, in 1 / 2 / 4 / 8 parts, 8 heads of 128: 1 sequence, 1,024 rows over 500 keys
+  // 36 / 23 / 16 / 13, over 8,000 38 / 31 / 31 / 35, over 20,000 63 / 58 / 58 / 72, 256 rows over 2,000 12.5 / 12.5 / 11.0 / 11.1, over 8,000
+  // 14.8 / 15.6 / 18.1 / 24.5; 8 of 3,000 keys, 1,024 rows 66 / 73 / 71 / 83, 400 rows 36 / 39 / 49 / 54; 23 of 698, 920 rows 63 / 58 / 56 / 66.
   pl->row_parts = 1;
   if (pl->many && pl->groups.n == 0 && own_items > 0) {
-    const int64_t tiles = ((int64_t)nq * (h->n_q_heads / h->n_kv_heads) + 31) / 32, parts = std::min<int64_t>({tiles / 2, 8, kWeightsSlots * num_cus() / own_items});
-    if (tiles >= 8 && parts > 1) {
-      pl->part_tiles = (int32_t)((tiles + parts - 1) / parts);
-      pl->row_parts = (int32_t)((tiles + pl->part_tiles - 1) / pl->part_tiles);
+    const int64_t tiles = ((int64_t)nq * (h->n_q_heads / h->n_kv_heads) + 31) / 32, cus = num_cus();
+    int64_t least_cost = INT64_MAX;
+    for (int64_t p = 1; p <= std::min<int64_t>(tiles, 8); ++p) {
+      const int64_t taken = (tiles + p - 1) / p, parts = (tiles + taken - 1) / taken, together = (own_items * parts + cus - 1) / cus;
+      const int64_t cost = taken * (together == 1 ? 12 : 10 * together) + (parts > 1 ? 50 + (int64_t)pl->n_seqs * h->n_kv_heads * max_len * parts / 10000 : 0);
+      if (cost < least_cost) least_cost = cost, pl->part_tiles = parts > 1 ? (int32_t)taken : 0, pl->row_parts = (int32_t)parts;
     }
   }
   pl->items = items + own_items * pl->row_parts;
