@@ -14,13 +14,13 @@ __device__ __forceinline__ uint32_t pick_key(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-constexpr int kPickFew = 64;
+constexpr int kPickFew = 128;  // (no more than threads)
 // W: waves of the workgroup, 4 or 16; two bins a thread
 template <int W>
 struct PickLds {
   uint32_t hist[W * 128];
   alignas(16) uint32_t a[W], b[W], least[W], most[W], above[W], equal[W];  // of each wave
-  uint32_t few[kPickFew];
+  alignas(16) uint32_t few[kPickFew];
   uint32_t bin, left, in_bin, n_few;
 };
 // Across the 64 lanes without a trip through LDS: the smallest, the largest (in all of them), sums up to each lane.
@@ -115,6 +115,7 @@ __device__ __forceinline__ int pick_largest(PickLds<W> &l, int n, int want, Valu
   // ---- how many there are, and between what
   for (int b = tid; b < kPickBins; b += kPickThreads) l.hist[b] = 0;
   if (tid == 0) l.n_few = 0;
+  if (tid < kPickFew) l.few[tid] = 0;
   uint32_t least = kPickAlways, most = 0, n_always = 0, n_ordinary = 0;
   each([&](int, uint32_t u, float) {
     n_always += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u == kPickAlways));
@@ -185,16 +186,17 @@ __device__ __forceinline__ int pick_largest(PickLds<W> &l, int n, int want, Valu
           if (ordinary(u) && u >= base && (u - base) >> bits == 0) l.few[atomicAdd(&l.n_few, 1u)] = u;
         });
         __syncthreads();
-        if (wave == 0) {
-          // how many are above this lane's, and how many are its equals
-          const uint32_t my = lane < (int)in_bin ? l.few[lane] : 0;
+        if (tid < (int)in_bin) {  // how many are above this thread's, and how many are its equals
+          typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+          const uint32_t my = l.few[tid];
           uint32_t above = 0, equals = 0;
-          for (int o = 0; o < (int)in_bin; ++o) {
-            const uint32_t u = (uint32_t)__builtin_amdgcn_readlane((int)my, o);
-            above += u > my;
-            equals += u == my;
+#pragma unroll 4
+          for (int o = 0; o < (int)in_bin; o += 4) {  // (behind the last one there are zeros)
+            const u32x4 u = *reinterpret_cast<const u32x4 *>(l.few + o);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) above += u[c] > my, equals += u[c] == my;
           }
-          if (lane < (int)in_bin && above < left && left <= above + equals) l.bin = my, l.left = left - above;  // (its equals write the same)
+          if (above < left && left <= above + equals) l.bin = my, l.left = left - above;  // (its equals write the same)
         }
         __syncthreads();
         found = uniform(l.bin);
