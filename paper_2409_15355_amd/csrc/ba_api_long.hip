@@ -55,14 +55,14 @@ void set_table(PagedTableParams *p, const ba_paged_cache *c) {
   p->page_div = make_fast_div((uint32_t)c->page_rows);
 }
 
-constexpr int64_t kWeightsSlots = 4;  // workgroups to a compute unit
+constexpr int64_t kWeightsSlots = 4, kWeightsOwn = 8;  // workgroups to a compute unit
 
 // ---- weights of cached keys --------------------------------------------------------------------------------
 struct WeightsPlan {
   int32_t seq0, n_seqs, group_end;
   int32_t prefix_items, own_chunks, item_members;
   int32_t part_tiles, row_parts;  // (see KeyWeightsParams)
-  bool many;
+  bool many, own_go_on;
   int64_t items;
   PagedGroups groups;
 };
@@ -74,7 +74,7 @@ int32_t padded_rows(const ba_heads *h, int32_t nq) {
 void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len, int32_t n_groups, const int32_t *cu_group, const int32_t *prefix_len,
                   int g0, WeightsPlan *pl) {
   memset(pl, 0, sizeof(*pl));
-  int32_t least_prefix = 0;
+  int32_t least_prefix = 0, most_prefix = 0;
   if (n_groups == 0) {
     pl->n_seqs = n_seqs;
   } else {
@@ -92,6 +92,7 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
         pl->groups.prefix[i] = prefix_len[g];
       }
       if (members > 0) least_prefix = std::min(least_prefix, shares ? prefix_len[g] : 0);
+      if (shares) most_prefix = std::max(most_prefix, prefix_len[g]);
     }
     pl->group_end = g;
     pl->n_seqs = cu_group[g] - pl->seq0;
@@ -118,7 +119,15 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
   }
   pl->groups.item0[pl->groups.n] = pl->prefix_items = (int32_t)std::min<int64_t>(items, INT32_MAX);
   pl->own_chunks = (int32_t)(((int64_t)max_len - least_prefix + keys - 1) / keys);
-  const int64_t own_items = (int64_t)pl->n_seqs * h->n_kv_heads * pl->own_chunks;
+  const int64_t lists = (int64_t)pl->n_seqs * h->n_kv_heads;
+  // What a sequence has of its own is max_len less the shortest prefix at most, and mostly no more than max_len less the longest: with few rows there are workgroups
+  // for that, and they go on where there is more; a workgroup without keys costs its way to seq_len.  us, with workgroups for all and so: eight groups of 25 on 1,796 to
+  // 3,590 keys, up to 12 of their own 41.9 / 25.2; five of 40, 16 rows, on 481 to 963, up to 124 37.2 / 21.7.  (Two workgroups a sequence where 39 are needed: 130 / 165.)
+  if (!pl->many && pl->groups.n > 0 && lists > 0) {
+    const int64_t mostly = std::max<int64_t>({((int64_t)max_len - most_prefix + keys - 1) / keys, 1, kWeightsOwn * num_cus() / lists});
+    if (mostly < pl->own_chunks) pl->own_chunks = (int32_t)mostly, pl->own_go_on = true;
+  }
+  const int64_t own_items = lists * pl->own_chunks;
   // Many rows in up to eight parts: what costs least, in tenths of the time that a tile takes a compute unit's workgroups together: 12 for one of them, 20
   // for two, 10 each for more; the merge (a launch) 50 and its bytes.  us, in 1 / 2 / 4 / 8 parts, 8 heads of 128: 1 sequence, 1,024 rows over 500 keys
   // 36 / 23 / 16 / 13, over 8,000 38 / 31 / 31 / 35, over 20,000 63 / 58 / 58 / 72, 256 rows over 2,000 12.5 / 12.5 / 11.0 / 11.1, over 8,000
@@ -129,7 +138,7 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
     int64_t least_cost = INT64_MAX;
     for (int64_t p = 1; p <= std::min<int64_t>(tiles, 8); ++p) {
       const int64_t taken = (tiles + p - 1) / p, parts = (tiles + taken - 1) / taken, together = (own_items * parts + cus - 1) / cus;
-      const int64_t cost = taken * (together == 1 ? 12 : 10 * together) + (parts > 1 ? 50 + (int64_t)pl->n_seqs * h->n_kv_heads * max_len * parts / 10000 : 0);
+      const int64_t cost = taken * (together == 1 ? 12 : 10 * together) + (parts > 1 ? 50 + lists * max_len * parts / 10000 : 0);
       if (cost < least_cost) least_cost = cost, pl->part_tiles = parts > 1 ? (int32_t)taken : 0, pl->row_parts = (int32_t)parts;
     }
   }
@@ -222,6 +231,7 @@ int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache,
     p.w_out = weights_out + at;
     p.w_stride = stride_weights;
     p.prefix_items = pl.prefix_items, p.own_chunks = pl.own_chunks, p.item_members = pl.item_members;
+    p.own_go_on = pl.own_go_on;
     p.part_tiles = pl.part_tiles, p.row_parts = pl.row_parts;
     p.part = (float *)ws;
     ProfileScope ps(BA_PROFILE_ATTENTION, (hipStream_t)stream);

@@ -38,6 +38,7 @@ struct KeyWeightsParams {
   float *w_out;
   int64_t w_stride;
   int32_t prefix_items, own_chunks;
+  int32_t own_go_on;       // a sequence may have more than own_chunks ranges of keys of its own: their workgroups go on
   int32_t item_members;    // sequences of a group that a work item takes
   // many rows without groups, in parts: tiles of 32 rows of a part (0: one part), its sums [part][sequence][KV head][cap]
   int32_t part_tiles, row_parts;

@@ -29,6 +29,7 @@ struct WeightsItem {
   int table_seq;      // the one whose pages it reads
   int kvh;
   int key0, key_end;  // keys from key0 on, below key_end
+  int step;           // how much further on it goes on, if it does
   int part;
 };
 template <int KEYS, typename Groups>
@@ -55,6 +56,7 @@ __device__ __forceinline__ WeightsItem weights_item(const KeyWeightsParams &p, c
     }
     it.key0 = chunk * KEYS;
     it.key_end = groups.prefix[lo];
+    it.step = 1 << 30;
   } else {
     int rel = (int)blockIdx.x - p.prefix_items;
     it.kvh = rel % p.n_kv_heads;
@@ -72,6 +74,7 @@ __device__ __forceinline__ WeightsItem weights_item(const KeyWeightsParams &p, c
     const bool in = groups.n > 0 && groups.seq0[lo] <= it.seq0 && it.seq0 < groups.seq0[lo] + groups.members[lo];
     it.key0 = (in ? groups.prefix[lo] : 0) + chunk * KEYS;
     it.key_end = clamped_length(p.seq_len, p.cap, it.seq0);
+    it.step = p.own_chunks * KEYS;
   }
   return it;
 }
@@ -114,19 +117,21 @@ __device__ __forceinline__ void lds_dma16_lane(const char *from, uint32_t lds_ba
 // 31,744 keys, 8 heads of 128, 64 keys a wave 88 us, 32 keys 60 (149 MB in, 66 out; vector units 39 %, matrix units 14 % of the cycles).  One token
 // of one sequence (2,064 keys): a launch, 4.7 us.
 // kEven: without padding, and 32 rows on is the same head, so every tile lies as far from the one before.
-template <int D, bool kFour, bool kEven, typename Groups>
-__global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsParams p, Groups groups) {
+template <int D>
+struct FewLds {
+  static constexpr int kNoted = 16, kNotes = 3 * 32 * 4;  // tiles whose notes lie in LDS at a time; bytes of a tile's
+  static constexpr int kBytes = kRowsBuffers * 32 * D * 2 + kNoted * (kNotes + 4);
+};
+template <int D, bool kFour, bool kEven>
+__device__ __forceinline__ void key_weights_few(const KeyWeightsParams &p, const WeightsItem &item, lds_char *const smem, int tid) {
   constexpr int NB = kRowsBuffers;
   constexpr int CPR = D / 8, KCH = D / 16, ROWB = D * 2, LPR = 256 / ROWB, RPI = 1024 / ROWB;  // RPI: rows of a load instruction
   constexpr int OPS = 32 / RPI / (kWThreads / 64);                                             // of a wave and tile
   constexpr uint32_t TB = 32 * ROWB;
-  constexpr int kNoted = 16, kNotes = 3 * 32 * 4;  // tiles whose notes lie in LDS at a time; bytes of a tile's
-  __shared__ __attribute__((aligned(1024))) char smem_generic[NB * TB + kNoted * (kNotes + 4)];
-  lds_char *const smem = (lds_char *)smem_generic, *const notes_at = smem + NB * TB;
+  constexpr int kNoted = FewLds<D>::kNoted, kNotes = FewLds<D>::kNotes;
+  lds_char *const notes_at = smem + NB * TB;
   lds_i *const all_at = (lds_i *)(notes_at + kNoted * kNotes);
-  const WeightsItem item = weights_item<kWeightsFewKeys>(p, groups);
-  if (item.key0 >= item.key_end) return;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int col = lane & 31, hf = lane >> 5;
   const int item_last = min(item.key_end, item.key0 + kWeightsFewKeys) - 1;
   const int n_rows = item.n_mem * p.padded, n_tiles = (n_rows + 31) / 32;
@@ -168,7 +173,7 @@ __global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsPar
   // keys are old ones, seen by all rows of a tile
   auto note = [&](int tile0) __attribute__((always_inline)) {
 #pragma unroll 1
-    for (int n = threadIdx.x; n < min(kNoted, n_tiles - tile0) * 32; n += kWThreads) {
+    for (int n = tid; n < min(kNoted, n_tiles - tile0) * 32; n += kWThreads) {
       int j, i, head;
       int64_t tok;
       const bool there = place(tile0 * 32 + n, j, i, tok, head);
@@ -267,6 +272,26 @@ __global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsPar
     };
     if (__builtin_amdgcn_readfirstlane(all_at[tile % kNoted]) != 0) sums(std::false_type{});
     else sums(std::true_type{});
+  }
+}
+// kOn: a workgroup goes on with further keys of its sequence.
+template <int D, bool kFour, bool kEven, bool kOn, typename Groups>
+__global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsParams p, Groups groups) {
+  __shared__ __attribute__((aligned(1024))) char smem[FewLds<D>::kBytes];
+  WeightsItem item = weights_item<kWeightsFewKeys>(p, groups);
+  if (item.key0 >= item.key_end) return;
+  if constexpr (!kOn) {
+    key_weights_few<D, kFour, kEven>(p, item, (lds_char *)smem, threadIdx.x);
+  } else {
+#pragma unroll 1
+    while (true) {
+      int tid = threadIdx.x;  // (all is computed again by every pass: kept, it would cost a wave a SIMD)
+      asm volatile("" : "+v"(tid), "+s"(item.seq0), "+s"(item.n_mem), "+s"(item.table_seq), "+s"(item.kvh), "+s"(item.key0), "+s"(item.key_end));
+      key_weights_few<D, kFour, kEven>(p, item, (lds_char *)smem, tid);
+      item.key0 += item.step;
+      if (item.key0 >= item.key_end) return;
+      wg_barrier();  // (what lies in LDS has been read)
+    }
   }
 }
 
@@ -457,7 +482,8 @@ hipError_t launch_d(const KeyWeightsParams &p, const Groups &g, bool many, hipSt
   else if (many) key_weights_many_kernel<D, false, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
   else {
     auto launch = [&](auto four, auto even) {
-      key_weights_kernel<D, decltype(four)::value, decltype(even)::value, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
+      if (p.own_go_on) key_weights_kernel<D, decltype(four)::value, decltype(even)::value, true, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
+      else key_weights_kernel<D, decltype(four)::value, decltype(even)::value, false, Groups><<<(unsigned)items, kWThreads, 0, stream>>>(p, g);
     };
     const bool even = p.rows == p.padded && 32 % p.group == 0;
     if (p.padded == 4) even ? launch(std::true_type{}, std::true_type{}) : launch(std::true_type{}, std::false_type{});

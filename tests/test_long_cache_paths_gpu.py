@@ -71,6 +71,43 @@ def test_key_weights_of_many_answers_on_a_long_prefix(ba, hq, d, members, prefix
         assert bool(((out[m, :, :x].double() - want[m, :, :x]).abs() <= off[m, :, :x] + 1e-37).all()), m
 
 
+@pytest.mark.parametrize("hq,hkv,d,nq", [(32, 8, 64, 1), (40, 8, 64, 1), (16, 8, 128, 7)])
+def test_key_weights_of_groups_of_unequal_prefixes(ba, hq, hkv, d, nq):  # noqa: F811
+    """Sequences that go on far behind a short prefix beside others that end behind a long one."""
+    import torch
+    members, prefix, rows = [32, 34], [1200, 90], 16
+    g, n_seqs, scale, u = hq // hkv, sum(members), d ** -0.5, forms.U
+    lens = [1200 + nq + s % 40 for s in range(32)] + [90 + nq + (s * 331) % 1100 for s in range(34)]
+    n, pages = max(lens), -(-max(lens) // rows)
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    kp = torch.randn((n_seqs * pages, rows, hkv, d), generator=gen, device="cuda").bfloat16()
+    table = torch.randperm(n_seqs * pages, generator=gen, device="cuda").view(n_seqs, pages)
+    table[:32, : 1200 // rows] = table[0, : 1200 // rows].clone()
+    table[32:, : 90 // rows] = table[32, : 90 // rows].clone()
+    for s in range(33, n_seqs):  # (the page that the prefix ends in: a copy of its part)
+        kp[table[s, 5], :10] = kp[table[32, 5], :10]
+    q = (torch.randn((n_seqs * nq, hq, d), generator=gen, device="cuda") * 2).bfloat16()
+    old = torch.rand((n_seqs, hkv, n), generator=gen, device="cuda")
+    lse, out = torch.empty((n_seqs * nq, hq), device="cuda"), torch.full((n_seqs, hkv, n), -7.0, device="cuda")
+    want, off = [], []
+    for s, m in enumerate(lens):
+        k = kp[table[s]].double().view(-1, hkv, d)[:m].permute(1, 2, 0).contiguous()  # [heads, D, keys]
+        r = q[s * nq:(s + 1) * nq].double().view(nq, hkv, g, d).transpose(0, 1).reshape(hkv, nq * g, d)
+        x, size = torch.stack([r[h] @ k[h] for h in range(hkv)]) * scale, torch.stack([r[h].abs() @ k[h].abs() for h in range(hkv)]) * scale
+        seen = torch.arange(m, device="cuda") <= (m - nq + torch.arange(nq, device="cuda"))[:, None]
+        x = x.masked_fill(~seen.repeat_interleave(g, 0), -float("inf"))
+        l = x.logsumexp(-1).float()
+        lse[s * nq:(s + 1) * nq] = l.view(hkv, nq, g).transpose(0, 1).reshape(nq, hq)
+        p = (x - l.double()[..., None]).exp()
+        w, e = p.sum(1), (p * (d * u * size + (x.abs().nan_to_num(posinf=0.0) + l.abs().double()[..., None] + 4 + nq * g) * u)).sum(1)
+        w[:, : m - nq] += 0.5 * old[s, :, : m - nq].double()
+        want.append(w), off.append(e + 2 * u * w)
+    cache = ba.PagedCache(kp, kp, table.int())
+    ba.ba_paged_key_weights(ba.Heads(hq, hkv, d), cache, q, lse, old, out, 0.5, ints(lens), n, [0, 32, 66], prefix, nq)
+    for s, m in enumerate(lens):
+        assert bool((out[s, :, m:] == -7).all()) and bool(((out[s, :, :m].double() - want[s]).abs() <= off[s] + 1e-37).all()), s
+
+
 @pytest.mark.parametrize("d,keep", [(128, 512), (64, 1024)])
 def test_eviction_past_the_caches(ba, d, keep):  # noqa: F811
     """Half a gigabyte that goes by once: every row at its place, and none beside."""
