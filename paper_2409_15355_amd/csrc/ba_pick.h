@@ -11,7 +11,7 @@ constexpr uint32_t kPickAlways = 0xffffffffu;
 __device__ __forceinline__ uint32_t pick_key(float x) {
   if (x != x) return 1u;
   const uint32_t u = __float_as_uint(x + 0.f);
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
+  return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 constexpr int kPickFew = 128;  // (no more than threads)
@@ -120,11 +120,12 @@ __device__ __forceinline__ int pick_largest(PickLds<W> &l, int n, int want, Valu
   each([&](int, uint32_t u, float) {
     n_always += __builtin_popcountll(__builtin_amdgcn_ballot_w64(u == kPickAlways));
     n_ordinary += __builtin_popcountll(__builtin_amdgcn_ballot_w64(ordinary(u)));
-    least = min(least, ordinary(u) ? u : kPickAlways);
-    most = max(most, ordinary(u) ? u : 0);
+    least = min(least, u - 1);  // (0 comes out above all)
+    most = max(most, u == kPickAlways ? 0 : u);
   });
   least = pick_reduce(least, [](uint32_t a, uint32_t b) { return min(a, b); });
   most = pick_reduce(most, [](uint32_t a, uint32_t b) { return max(a, b); });
+  least += least != kPickAlways;  // (of the ordinary ones, if there is one)
   if (lane == 0) l.a[wave] = n_always, l.b[wave] = n_ordinary, l.least[wave] = least, l.most[wave] = most;
   __syncthreads();
   {  // a lane for each wave's
@@ -149,8 +150,9 @@ __device__ __forceinline__ int pick_largest(PickLds<W> &l, int n, int want, Valu
     int bits = 32 - __builtin_clz((most - least) | 1);
     while (true) {  // (the same in all threads)
       const int shift = max(0, bits - kDigit);
+      const uint32_t reach = bits < 32 ? min((1u << bits) - 1, most - base) : most - base;  // (0 and kPickAlways lie further on)
       each([&](int, uint32_t u, float) {
-        if (ordinary(u) && u >= base && (bits == 32 || (u - base) >> (bits & 31) == 0)) atomicAdd(&l.hist[(u - base) >> shift], 1u);
+        if (u - base <= reach) atomicAdd(&l.hist[(u - base) >> shift], 1u);
       });
       __syncthreads();
       // two bins a thread, from the highest down
@@ -183,7 +185,7 @@ __device__ __forceinline__ int pick_largest(PickLds<W> &l, int n, int want, Valu
       }
       if (in_bin <= kPickFew) {
         each([&](int, uint32_t u, float) {
-          if (ordinary(u) && u >= base && (u - base) >> bits == 0) l.few[atomicAdd(&l.n_few, 1u)] = u;
+          if (u - base <= min((1u << bits) - 1, most - base)) l.few[atomicAdd(&l.n_few, 1u)] = u;
         });
         __syncthreads();
         if (tid < (int)in_bin) {  // how many are above this thread's, and how many are its equals
@@ -219,17 +221,13 @@ __device__ __forceinline__ int pick_largest(PickLds<W> &l, int n, int want, Valu
   auto lanes_before = [&](uint64_t mask, uint32_t from) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, from)); };
   each([&](int s, uint32_t u, float x) {
     const uint64_t gt = __builtin_amdgcn_ballot_w64(u > found);
-    uint32_t at = lanes_before(gt, above);
-    bool taken = u > found;
-    if (left > 0) {
-      const uint64_t eq = __builtin_amdgcn_ballot_w64(u == found);
-      const uint32_t e = lanes_before(eq, equal);
-      at += min(e, left);
-      taken = taken || (u == found && e < left);
-      equal += __builtin_popcountll(eq);
-    }
-    if (taken) emit((int)at, begin + s * 64 + lane, x);
+    uint64_t eq = 0;
+    if (left > 0) eq = __builtin_amdgcn_ballot_w64(u == found);
+    if ((gt | eq) == 0) return;
+    const uint32_t e = lanes_before(eq, equal), at = lanes_before(gt, above) + min(e, left);
+    if (u > found || (u == found && e < left)) emit((int)at, begin + s * 64 + lane, x);
     above += __builtin_popcountll(gt);
+    equal += __builtin_popcountll(eq);
   });
   return (int)total;
 }

@@ -61,10 +61,10 @@ __global__ __launch_bounds__(W * 64) void evict_pick_kernel(EvictParams p) {
   const float *w = p.weights + list * p.w_stride;
   int32_t *kept = p.kept + list * p.n_keep;
   float *w_out = p.w_out ? p.w_out + list * p.w_out_stride : nullptr;
-  const int last0 = len - p.n_last;
+  const uint32_t between = (uint32_t)max(0, len - p.n_last - p.n_first);  // tokens that are neither of the first nor of the last
   const int lo = kRows > 0 ? part * p.part_rows : 0, hi = kRows > 0 && part + 1 < p.parts ? lo + p.part_rows : p.n_keep;
   const int n = pick_largest<W, E>(
-      lds, len, p.n_keep, [&](int i) { return w[i]; }, [&](int i, float x) { return i < p.n_first || i >= last0 ? kPickAlways : pick_key(x); },
+      lds, len, p.n_keep, [&](int i) { return w[i]; }, [&](int i, float x) { return (uint32_t)(i - p.n_first) < between ? pick_key(x) : kPickAlways; },
       [&](int at, int i, float x) {
         if (kRows > 0 && (at < lo || at >= hi)) return;
         kept[at] = i;
