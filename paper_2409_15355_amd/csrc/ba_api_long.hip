@@ -107,8 +107,8 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
     most_members = std::max<int64_t>(most_members, pl->groups.members[i]);
   }
   // A group's sequences in parts (nothing has to be added up: their weights are their own) where its keys do not fill the chip, of 64 rows at least.
-  // us, in one part and in several (of 32 / 64 / 128 rows at least): 46 answers of 4 rows on 1,141 keys 11.2 and 7.0 / 7.3 / 9.3; two groups of 28 of 16 rows on
-  // 1,096 keys 19.5 and 13.1 / 13.1 / 11.5; 16 of 32 rows on 2,000 keys 24.4 and 14.4 / 11.1 / 11.2.
+  // us, in one part and in several (of 32 / 64 / 128 rows at least): 46 answers of 4 rows on 1,141 keys 11.2 and 7.0 / 7.3 / 9.3; two groups of 28 of
+  // 16 rows on 1,096 keys 19.5 and 13.1 / 13.1 / 11.5; 16 of 32 rows on 2,000 keys 24.4 and 14.4 / 11.1 / 11.2.
   constexpr int64_t kRowsLeast = 64;
   const int64_t parts = items > 0 ? std::max<int64_t>(1, kWeightsSlots * num_cus() / items) : 1, padded = padded_rows(h, nq);
   pl->item_members = (int32_t)std::min(most_members, std::max((kRowsLeast + padded - 1) / padded, (most_members + parts - 1) / parts));
@@ -120,9 +120,10 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
   pl->groups.item0[pl->groups.n] = pl->prefix_items = (int32_t)std::min<int64_t>(items, INT32_MAX);
   pl->own_chunks = (int32_t)(((int64_t)max_len - least_prefix + keys - 1) / keys);
   const int64_t lists = (int64_t)pl->n_seqs * h->n_kv_heads;
-  // What a sequence has of its own is max_len less the shortest prefix at most, and mostly no more than max_len less the longest: with few rows there are workgroups
-  // for that, and they go on where there is more; a workgroup without keys costs its way to seq_len.  us, with workgroups for all and so: eight groups of 25 on 1,796 to
-  // 3,590 keys, up to 12 of their own 41.9 / 25.2; five of 40, 16 rows, on 481 to 963, up to 124 37.2 / 21.7.  (Two workgroups a sequence where 39 are needed: 130 / 165.)
+  // What a sequence has of its own is max_len less the shortest prefix at most, and mostly no more than max_len less the longest: with few rows there
+  // are workgroups for that, and they go on where there is more; a workgroup without keys costs its way to seq_len.  us, with workgroups for all and
+  // so: eight groups of 25 on 1,796 to 3,590 keys, up to 12 of their own 41.9 / 25.2; five of 40, 16 rows, on 481 to 963, up to 124 37.2 / 21.7.
+  // (Two workgroups a sequence where 39 are needed: 130 / 165.)
   if (!pl->many && pl->groups.n > 0 && lists > 0) {
     const int64_t mostly = std::max<int64_t>({((int64_t)max_len - most_prefix + keys - 1) / keys, 1, kWeightsOwn * num_cus() / lists});
     if (mostly < pl->own_chunks) pl->own_chunks = (int32_t)mostly, pl->own_go_on = true;
