@@ -232,8 +232,8 @@ __device__ __forceinline__ int pick_largest(PickLds<W> &l, int n, int want, Valu
   return (int)total;
 }
 // Calls f with the waves and the number of keys that a thread has to keep for lists of up to n.
-// us a call of eight lists, 4 / 8 / 16 waves: selection out of 2,000 pages 11.8 / 10.9 / 9.7, eviction out of 2,064 tokens 11.6 / 12.0 / 11.5; of 512
-// lists: selection out of up to 1,000 pages, 4 / 16 waves 8 / 12 (the kernel alone).
+// us a call of eight lists, 4 / 8 / 16 waves: selection out of 2,000 pages 11.8 / 10.9 / 9.7, eviction out of 2,064 tokens (rows in a
+// launch of their own) 11.6 / 12.0 / 11.5; of 512 lists: selection out of up to 1,000 pages, 4 / 16 waves 8 / 12 (the kernel alone).
 template <typename F>
 auto with_pick_shape(int64_t n, F &&f) {
   using std::integral_constant;
