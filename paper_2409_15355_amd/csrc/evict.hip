@@ -47,7 +47,7 @@ __device__ __forceinline__ void copy_rows(const EvictParams &p, int seq, int fir
 }
 
 // Bound by latency for a few lists (eight of 2,064 tokens, 512 rows of 128 each copied: a call 7.4 us), by the instructions of sixteen waves a list
-// for many (512 of up to 8,000 tokens 14.7 us: 45 % of the vector units' cycles; 9 MB).
+// for many (512 of up to 8,000 tokens 13.3 us: 49 % of the vector units' cycles; 9 MB).
 // kRows: head_dim, and rows are copied, too.  Then a list may have several workgroups: each of them makes the same choice, and writes and copies its part
 // of the rows, so nothing is handed on.  0: one workgroup a list, and no copies.
 template <int W, int E, int kRows>
