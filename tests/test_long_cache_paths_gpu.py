@@ -108,11 +108,11 @@ def test_key_weights_of_groups_of_unequal_prefixes(ba, hq, hkv, d, nq):  # noqa:
         assert bool((out[s, :, m:] == -7).all()) and bool(((out[s, :, :m].double() - want[s]).abs() <= off[s] + 1e-37).all()), s
 
 
-@pytest.mark.parametrize("d,keep", [(128, 512), (64, 1024)])
-def test_eviction_past_the_caches(ba, d, keep):  # noqa: F811
-    """Half a gigabyte that goes by once: every row at its place, and none beside."""
+@pytest.mark.parametrize("d,keep,n_seqs", [(128, 512, 64), (64, 1024, 64), (64, 64, 70), (128, 128, 40)])
+def test_eviction_of_many_lists(ba, d, keep, n_seqs):  # noqa: F811
+    """A quarter of a gigabyte and more that goes past the caches, or short lists in one launch: every row at its place, and none beside."""
     import torch
-    n_seqs, hkv, rows, to_rows = 64, 8, 16, 32
+    hkv, rows, to_rows = 8, 16, 32
     lens = [keep + 1 + s % 50 for s in range(n_seqs)]
     n, pages, to_pages = max(lens), -(-max(lens) // rows), keep // to_rows
     gen = torch.Generator(device="cuda").manual_seed(1)
