@@ -556,7 +556,7 @@ int32_t ba_page_bounds(const ba_heads *heads, const ba_paged_cache *cache,
  *   score(page) = max over the call's q_per_seq query rows i and heads h of the KV head of 2^(e_ih + e) sum_d max(c_ihd hi_d, c_ihd lo_d),
  * a bound on what any key of the page scores, of the query in 8 bits: c_ihd = round(q_ihd / 2^e_ih), to nearest, ties to even, within -127 .. 127, e_ih as
  * above for the row's values.  The sums are whole numbers and exact.  Of equal scores the earlier page.  Taken first, whatever they score: a sequence's first n_first
- * pages, its last n_last ones, and those that hold its newest q_per_seq tokens; n_select has room for all of these.  A page that is not there is not taken.
+ * pages, its last n_last ones, and those that hold its newest q_per_seq tokens; n_select (2^30 at most) has room for all of these.  A page that is not there is not taken.
  * selected_out: device ints, [n_seqs][n_kv_heads][n_select], numbers of pages within the sequence (entries of its row of the page
  * table), ascending, -1 behind the last.  scores_out: device floats, nullable, the same shape: their scores, -infinity behind the last.
  * ws: 256-byte aligned, at least ba_page_select_workspace_bytes() bytes (may be null when that is 0).

@@ -389,6 +389,7 @@ int32_t ba_page_select(const ba_heads *heads, const ba_paged_cache *cache, const
   const int64_t newest = ((int64_t)q_per_seq + cache->page_rows - 2) / cache->page_rows + 1;  // pages that a sequence's newest tokens may lie in
   if (n_first < 0 || n_last < 0 || n_select < 1 || n_first + std::max<int64_t>(n_last, newest) > n_select)
     return fail(BA_ERR_INVALID_ARG, "n_select has no room for the first, the last and the newest pages");
+  if (n_select > (1 << 30)) return fail(BA_ERR_UNSUPPORTED, "n_select beyond 2^30");  // (places of a list are counted on in 32 bits)
   if (n_seqs == 0) return BA_OK;
   if ((rc = check_tensor(q, "q", false, D, hq)) || (rc = check_lists(n_seqs, heads))) return rc;
   if (!seq_len || !selected_out) return fail(BA_ERR_INVALID_ARG, "seq_len / selected_out: null");
