@@ -12,7 +12,7 @@
  * - Tensors are DEVICE memory described by `ba_tensor`: element pointer, token and head
  *   strides in ELEMENTS, innermost head_dim contiguous.  The default packed layout is
  *   [tokens][heads][head_dim] (stride_head = head_dim, stride_tok = heads * head_dim).
- *   Base pointers and both strides must be 16-byte aligned.
+ *   Base pointers and both strides must be 16-byte aligned, token strides below 2^24 elements.
  * - Small metadata arrays (block offsets, per-block descriptors, cu_* arrays, q_to_kv,
  *   inv_freq) are HOST memory.  They are read and validated before the call returns
  *   and may be freed immediately afterwards.

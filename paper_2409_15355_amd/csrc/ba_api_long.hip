@@ -32,9 +32,6 @@ int32_t check_max_len(const ba_paged_cache *c, int32_t max_len) {
   if (c && max_len > (int64_t)c->max_pages * c->page_rows) return fail(BA_ERR_INVALID_ARG, "max_len reaches beyond the page table");
   return BA_OK;
 }
-int32_t check_row_stride(const ba_paged_cache *c) {
-  return std::max(c->k.stride_tok, c->v.stride_tok) < (int64_t)1 << 31 ? BA_OK : fail(BA_ERR_UNSUPPORTED, "cache: rows of 4 GB and more");
-}
 int32_t check_lists(int64_t n_seqs, const ba_heads *h) {
   return n_seqs * h->n_kv_heads <= kMaxPickWorkgroups ? BA_OK : fail(BA_ERR_UNSUPPORTED, "2^22 sequences and KV heads and more in one launch");
 }
@@ -46,7 +43,7 @@ void set_rows(PagedRowsParams *p, const ba_tensor *t, int64_t stride_page) {
   p->base = (const uint16_t *)t->ptr;
   p->sh = t->stride_head;
   p->page_b16 = (uint32_t)(stride_page / 8);
-  p->rb = (uint32_t)t->stride_tok * 2;
+  p->rb = (uint32_t)t->stride_tok * 2;  // (check_tensor: below 2^25)
 }
 void set_table(PagedTableParams *p, const ba_paged_cache *c) {
   p->table = c->page_table;
@@ -176,7 +173,7 @@ int32_t ba_paged_key_weights(const ba_heads *heads, const ba_paged_cache *cache,
                              float *weights_out, int64_t stride_weights, float decay, int32_t q_per_seq, const int32_t *seq_len, int32_t max_len,
                              int32_t n_groups, const int32_t *cu_group, const int32_t *prefix_len, void *ws, size_t ws_bytes, void *stream) {
   int32_t rc;
-  if ((rc = check_heads(heads, true)) || (rc = check_cache(cache, heads)) || (rc = check_row_stride(cache))) return rc;
+  if ((rc = check_heads(heads, true)) || (rc = check_cache(cache, heads))) return rc;
   const int32_t n_seqs = cache->n_seqs, hq = heads->n_q_heads, D = heads->head_dim;
   if ((rc = check_paged_sizes(heads, n_seqs, q_per_seq, max_len)) || (rc = check_groups(n_seqs, max_len, n_groups, cu_group, prefix_len))) return rc;
   if (!std::isfinite(decay)) return fail(BA_ERR_INVALID_ARG, "decay must be finite");
@@ -261,8 +258,7 @@ int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const
                        int64_t stride_out, int32_t *len_out, void *ws, size_t ws_bytes, void *stream_) {
   hipStream_t stream = (hipStream_t)stream_;
   int32_t rc;
-  if ((rc = check_heads(heads, false)) || (rc = check_cache(cache, heads)) || (rc = check_cache(to, heads)) || (rc = check_row_stride(cache)) ||
-      (rc = check_row_stride(to)) || (rc = check_max_len(cache, max_len)))
+  if ((rc = check_heads(heads, false)) || (rc = check_cache(cache, heads)) || (rc = check_cache(to, heads)) || (rc = check_max_len(cache, max_len)))
     return rc;
   const int32_t n_seqs = cache->n_seqs, hkv = heads->n_kv_heads, D = heads->head_dim;
   if (to->n_seqs != n_seqs) return fail(BA_ERR_INVALID_ARG, "to has %d sequences, the cache %d", to->n_seqs, n_seqs);
@@ -349,8 +345,7 @@ int32_t ba_paged_evict(const ba_heads *heads, const ba_paged_cache *cache, const
 int32_t ba_page_bounds(const ba_heads *heads, const ba_paged_cache *cache, const ba_page_bound_table *bounds, const int32_t *from_token,
                        const int32_t *seq_len, int32_t max_len, void *stream) {
   int32_t rc;
-  if ((rc = check_heads(heads, false)) || (rc = check_cache(cache, heads)) || (rc = check_row_stride(cache)) || (rc = check_max_len(cache, max_len)) ||
-      (rc = check_bounds(bounds)))
+  if ((rc = check_heads(heads, false)) || (rc = check_cache(cache, heads)) || (rc = check_max_len(cache, max_len)) || (rc = check_bounds(bounds)))
     return rc;
   const int32_t n_seqs = cache->n_seqs, hkv = heads->n_kv_heads;
   if (n_seqs == 0 || max_len == 0) return BA_OK;

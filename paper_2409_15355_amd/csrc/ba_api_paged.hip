@@ -376,6 +376,7 @@ void set_attention(PagedAttnParams *p, const ba_heads *heads, const ba_paged_cac
   p->k = (const uint16_t *)cache->k.ptr, p->v = (const uint16_t *)cache->v.ptr;
   p->k_sh = cache->k.stride_head, p->v_sh = cache->v.stride_head;
   p->k_page_b16 = (uint32_t)(cache->k_stride_page / 8), p->v_page_b16 = (uint32_t)(cache->v_stride_page / 8);
+  // (check_tensor: below 2^25, so sixteen rows lie within 32 bits, which is what the walks' row offsets have)
   p->k_rb = (uint32_t)cache->k.stride_tok * 2, p->v_rb = (uint32_t)cache->v.stride_tok * 2;
   p->page_table = cache->page_table + (int64_t)pl.seq0 * cache->stride_table;
   p->stride_table = cache->stride_table;
