@@ -94,8 +94,11 @@ void plan_weights(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t max_len
     pl->group_end = g;
     pl->n_seqs = cu_group[g] - pl->seq0;
   }
-  // us, the kernel for few rows and the one for many, 8 KV heads of 128: 1 sequence of 32,000 keys, 16 rows 14.6 / 16.8, 32 15.3 / 13.6, 48 19.2 / 19.4,
-  // 64 19.9 / 15.3, 128 28.2 / 20.2, 1,024 139 / 84; of 2,000, 32 rows 5.0 / 5.5, 64 5.9 / 6.8, 256 15.1 / 11.9, 1,024 52 / 36.
+  // By rows alone.  us, the kernel for few rows and the one for many, 8 KV heads of 128: 1 sequence of 32,000 keys, 16 rows 14.6 / 16.9, 24 14.9 / 17.0,
+  // 32 14.8 / 14.2, 48 16.9 / 19.3, 64 16.8 / 15.3, 128 22.9 / 18.7, 1,024 99 / 79; of 2,000, 16 rows 4.6 / 5.9, 32 5.1 / 6.0, 64 5.8 / 6.9, 128 7.7 / 8.5,
+  // 256 12.2 / 10.7, 1,024 40 / 14; 16 sequences on a shared prefix of 2,000, 16 rows 7.1 / 10.3, 32 9.2 / 9.9, 64 12.3 / 15.2, 128 18.3 / 20.0, of 8,000 13.6 / 23.5,
+  // 19.4 / 18.7, 30.6 / 25.4, 52 / 42; 64 on 30,000 111 / 216, 192 / 154, 356 / 274, 684 / 515.  So between 32 and 128 rows few keys cost 1 to 3 us more than
+  // they would have to, and 48 rows, whose second tile is half empty, up to 2.4.
   pl->many = nq * (h->n_q_heads / h->n_kv_heads) >= 32;
   const int32_t keys = pl->many ? kWeightsManyKeys : kWeightsFewKeys;
   int64_t items = 0, most_members = 1;

@@ -296,7 +296,8 @@ size_t plan_bytes(const PagedPlan &pl, const ba_heads *h, int32_t nq) {
 // what it writes and reads.  A key more is 0.011 us where an item has a compute unit to itself; two that share one take as long as one after the other.
 // us, 8 key heads of 128 and 4 rows, in 1 / 2 / 4 / 8 / 16 parts: 1 sequence of 256 keys 8.3 / 10.7 / 10.3, of 512 10.8 / 12.0 / 11.3 / 10.3, of 1,024
 // 16.1 / 14.3 / 12.4 / 10.7 / 10.4; 4 of 1,536 22.0 / 17.9 / 13.9 / 13.1 / 13.8; 12 of 1,536 22.7 / 20.9 / 21.5 / 22.8; 24 29.6 / 35.0 / 33.1 / 36.4 / 41.9;
-// 80 87 / 88 / 92 / 105; 64 of 384 21.3 / 28.5; 32 rows, 1 of 256 13.1 / 14.8, of 512 17.7 / 16.7 / 16.0 / 14.7.
+// 80 87 / 88 / 92 / 105; 64 of 384 21.3 / 28.5; 32 rows, 1 of 256 13.1 / 14.8, of 512 17.7 / 16.7 / 16.0 / 14.7.  (Fitted up to 32 rows; the other walk, for more, was
+// not timed.)
 void plan_selected(const ba_heads *h, int32_t n_seqs, int32_t nq, int32_t page_rows, int32_t keys, int cus, PagedPlan *pl) {
   memset(pl, 0, sizeof(*pl));
   const int64_t rows = (int64_t)nq * (h->n_q_heads / h->n_kv_heads), D = h->head_dim;

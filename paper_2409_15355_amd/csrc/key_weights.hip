@@ -111,11 +111,11 @@ __device__ __forceinline__ void lds_dma16_lane(const char *from, uint32_t lds_ba
 
 // ---- few rows a sequence: 32 keys a wave ----------------------------------------------------------------------------
 // A sequence's rows begin at a multiple of 4 (of 8 if it has more than 4): a quad of accumulators is one sequence's, and a tile of rows is
-// several's.  32 keys a wave, not 64: those leave registers for three workgroups a compute unit, and what a tile does for its rows -
+// several's.  32 keys a wave, not 64: those leave registers for five workgroups a compute unit, and what a tile does for its rows -
 // notes, masks, the weights of sequences that end in it - goes on in the others while one waits.
 // Bound by HBM where it shares a prefix: what every sequence was given before comes in, what it is given now goes out.  64 sequences of four rows on
 // 31,744 keys, 8 heads of 128, 64 keys a wave 88 us, 32 keys 60 (149 MB in, 66 out; vector units 39 %, matrix units 14 % of the cycles).  One token
-// of one sequence (2,064 keys): a launch, 4.7 us.
+// of one sequence (2,064 keys): a launch, a call takes 4.3 us.
 // kEven: without padding, and 32 rows on is the same head, so every tile lies as far from the one before.
 template <int D>
 struct FewLds {
@@ -297,7 +297,7 @@ __global__ __launch_bounds__(kWThreads, 4) void key_weights_kernel(KeyWeightsPar
 
 // ---- many rows a sequence: 64 keys a wave ---------------------------------------------------------------------------
 // A score costs its exponential (half the vector rate), a scaling and an addition.  Bound by vector and matrix units together: 1,024 rows over 32,000
-// keys, 8 heads of 128, 81 us (820 TFLOP/s), matrix units 42 %, vector units 56 % of the cycles, and by what the part may draw: a tile's products
+// keys, 8 heads of 128, 80 us (840 TFLOP/s), matrix units 42 %, vector units 56 % of the cycles, and by what the part may draw: a tile's products
 // between the exponentials of the one before, two waves a SIMD, take 24 % more cycles and the same time, at 2.26 GHz instead of 1.85.  With 32 keys a
 // wave 139: an LDS read a product, not for two.
 // kEven: a sequence's rows are whole tiles, and 32 rows on is the same head, so every tile lies as far from the one before.
